@@ -65,6 +65,8 @@ extern "C" {
 
 typedef int zq_dtype;
 enum { ZQ_F32 = 0, ZQ_F16 = 1, ZQ_BF16 = 2 };
+enum { ZQ_I32 = 3, ZQ_I64 = 4 };  /* token ids (embedding calls) */
+enum { ZQ_INT4 = 5 };             /* packed INT4 codes with block scales (gradient tables) */
 
 enum {
   ZQ_OK = 0,
@@ -72,10 +74,11 @@ enum {
   ZQ_E_BLOCK = -2,  /* block not a power of two in [32, 1024] */
   ZQ_E_DTYPE = -3,  /* unknown element dtype */
   ZQ_E_ALIGN = -4,  /* misaligned pointer */
-  ZQ_E_SIZE = -5,   /* negative element count */
+  ZQ_E_SIZE = -5,   /* negative element count, or a size the call does not take */
   ZQ_E_P = -6,      /* slice count outside [1, 1024] */
   ZQ_E_HIP = -7,    /* HIP kernel launch failed */
-  ZQ_E_ALIAS = -8   /* an output overlaps an input */
+  ZQ_E_ALIAS = -8,  /* an output overlaps an input or another output */
+  ZQ_E_MEMORY = -9  /* no host memory (zq_grad_plan_make) */
 };
 
 /* qwZ quantiser (Background, ZeRO++: quantise the weight shard to INT8 blocks
@@ -200,6 +203,116 @@ int qgz_reduce_level_gather_noalloc(const uint8_t* const* packed_slices, const f
  * should dequantise the gathered layer once and call a library GEMM. */
 int qwz_dequant_gemm(const void* x, zq_dtype xt, const int8_t* codes, const float* scales, int64_t M, int64_t N,
                      int64_t K, int32_t block, float* y, void* stream);
+
+/* ---- The embedding layer --------------------------------------------------
+ * Rows of an embedding table by token id, and the table's gradient.  The table is
+ * the first weight a rank gathers, and its gradient the largest it sends.
+ * For these calls element arrays (table, y, dy, dw) need only the alignment of
+ * their elements, ids that of theirs; rows may have any length up to 2^24.  An id
+ * that is not in [0, V) names no row: such a token (padding, say as -1) gets a row
+ * of zeros and takes no part in the gradient.
+ *
+ * zq_embedding: y[t][d] = cvt(fl(scale * table[ids[t]][d])).
+ *   ids   [T] of type it = ZQ_I32 or ZQ_I64 (read)
+ *   table [V][D] of dtype wt (read) -> y [T][D] of dtype yt (written) */
+int zq_embedding(const void* ids, zq_dtype it, int64_t T, const void* table, zq_dtype wt, int64_t V, int64_t D,
+                 float scale, void* y, zq_dtype yt, void* stream);
+
+/* qwz_embedding: the same from the gathered INT8 table (Design, Weight
+ * Partitioning), reading only the rows that occur:
+ *   y[t][d] = cvt(fl(scale * fl(codes[f] * scales[f / block]))),  f = ids[t]*D + d,
+ * i.e. with scale 1 the rows that qwz_dequantize writes.
+ *   codes [V*D], scales [ceil(V*D/block)] (read); block as everywhere. */
+int qwz_embedding(const void* ids, zq_dtype it, int64_t T, const int8_t* codes, const float* scales, int64_t V,
+                  int64_t D, int32_t block, float scale, void* y, zq_dtype yt, void* stream);
+
+/* zq_embedding_grad: the gradient of the table from the gradient dy of y, dense:
+ *   dw[v][d] = cvt(fl(scale * sum_{t: ids[t] = v} dy[t][d]))   zeros where v does not occur
+ * with accumulate != 0 added to what dw holds: dw[v][d] = cvt(fl(dw[v][d] + fl(scale *
+ * sum))), rows that do not occur untouched.  Sums are taken in binary32 in an order that
+ * follows from the ids alone (tokens ascending, whole 64s of them summed apart), so
+ * results are the same in every run.
+ *   dy [T][D] of dtype gt (read), dw [V][D] of dtype wt (written)
+ *   workspace: device memory of zq_embedding_grad_bytes(T, V, D) bytes or more, 16-byte
+ *   aligned, the call's own until it has run.  T, V <= 2^30 (ZQ_E_SIZE); a workspace
+ *   that is too small is ZQ_E_SIZE too. */
+int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, zq_dtype gt, int64_t V, int64_t D,
+                      float scale, int accumulate, void* dw, zq_dtype wt, void* workspace, int64_t workspace_bytes,
+                      void* stream);
+int64_t zq_embedding_grad_bytes(int64_t T, int64_t V, int64_t D); /* -1 for sizes outside the limits */
+
+/* ---- Gradient norm and clipping --------------------------------------------
+ * The norm of all of a rank's gradients, and their scaling down to a largest norm,
+ * over any number of tensors in one launch each.  A tensor is dense (n elements of
+ * dtype ZQ_F32, ZQ_F16 or ZQ_BF16; aligned to its elements) or an INT4 shard as the
+ * qgZ calls write it (dtype ZQ_INT4: data the packed codes at any address, scales
+ * its block scales), which is read as it is.
+ *   out  NULL: clipped in place (an INT4 shard: its scales); else out [n] of
+ *        out_dtype receives the clipped elements (an INT4 shard's dequantised)
+ * Outputs must not overlap each other or any tensor (in place: the tensor's own
+ * memory); a tensor listed twice therefore needs an out for each. */
+typedef struct {
+  void* data;
+  float* scales;     /* ZQ_INT4 only */
+  void* out;
+  int64_t n;
+  int32_t dtype;
+  int32_t out_dtype; /* with out */
+  int32_t block;     /* ZQ_INT4 only */
+  int32_t reserved;
+} zq_grad;
+
+/* Sizes of a table of tensors; filled by zq_grad_plan_make. */
+typedef struct {
+  int64_t bytes;       /* of the table */
+  int64_t norm_chunks;
+  int64_t clip_chunks;
+  int32_t count;
+  int32_t reserved;
+} zq_grad_plan;
+
+/* Host only.  zq_grad_plan_make checks the tensors (every argument error of the
+ * calls below is found here) and fills plan; zq_grad_plan_table writes plan->bytes of
+ * table to host memory.  The caller copies them to 16-byte aligned device memory,
+ * once for as long as the tensors stay where they are: the calls keep their partial
+ * sums in that copy and leave it ready for the next call.  Calls with one table must
+ * be ordered (one stream, or events); calls with different tables need not be. */
+int zq_grad_plan_make(const zq_grad* grads, int32_t count, zq_grad_plan* plan);
+int zq_grad_plan_table(const zq_grad* grads, const zq_grad_plan* plan, void* host_table);
+
+/* norm[0] = |scale| * sqrt(sum of the squares of all elements): squares and sums in
+ * binary64, in a fixed order, rounded once; NaN or infinite where an element is.
+ * `scale` undoes a loss scale or averages micro-batches.  plan on the host, table
+ * and norm (a float) on the device. */
+int zq_grad_norm(const zq_grad_plan* plan, void* table, float scale, float* norm, void* stream);
+
+/* Multiplies every element by c = fl(scale * min(1, fl(max_norm / fl(norm[0] + 1e-6)))),
+ * which is computed on the device from the norm there; a NaN norm makes every
+ * element NaN, an infinite one makes c = 0:
+ *   dense  out = cvt(fl(g * c))
+ *   INT4   scales = fl(s * c) in place, or out = cvt(fl(q * fl(s * c)))
+ * max_norm must be >= 0 (ZQ_E_SIZE).  In place with c = 1 nothing is read or written. */
+int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm, float max_norm, float scale,
+                 void* stream);
+
+/* ---- Products with an INT4 weight --------------------------------------------
+ * The few-row product of qwz_dequant_gemm for a weight in the INT4 format (4-bit
+ * codes, one scale a block: a layer, or the output head, kept quantised for
+ * generation), without dequantising it to memory:
+ *   y[m][n] = sum_k x[m][k] * q[n*K + k] * s[(n*K + k) / block]
+ * The weight is not narrowed: the codes' products are exact and summed in binary32 by
+ * the matrix cores, each scale multiplies its block's sum (or a part of it), and these
+ * are added in binary32, in a fixed order: within (K + 64) * 2^-23 * sum_k |x w| of
+ * the exact value, the same bits in every run.
+ *   x       [M][K] row-major, xt = ZQ_BF16 or ZQ_F16 (read)
+ *   packed  [ceil(N*K/2)] INT4 codes of the N x K weight, row-major, scales
+ *           [ceil(N*K/block)] floats (read)
+ *   y       [M][N] float row-major (written)
+ * K a multiple of 64, at most 2^22 (ZQ_E_SIZE); M, N >= 0 arbitrary; K = 0 writes
+ * zeros.  x and packed 16-byte aligned, scales and y 4-byte aligned.  Meant for few
+ * rows: the weight is read again for every 64 rows of x. */
+int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, const float* scales, int64_t M, int64_t N,
+                         int64_t K, int32_t block, float* y, void* stream);
 
 /* Size helpers (host only): number of scales ceil(n/block) (-1 on a bad
  * block or n < 0), and INT4 bytes ceil(n/2) (-1 for n < 0). */

@@ -9,9 +9,17 @@ kernel does.
 from ._lib import (  # noqa: F401
     LIB_PATH,
     STATUS,
+    GradTable,
     ZQError,
+    embedding,
+    embedding_grad,
+    embedding_grad_bytes,
     gather_tables,
+    grad_clip,
+    grad_norm,
+    grad_table,
     int4_bytes,
+    int4_dequant_gemm,
     lib,
     num_scales,
     qgz_dequantize,
@@ -22,5 +30,6 @@ from ._lib import (  # noqa: F401
     qgz_reduce_level_gather_noalloc,
     qwz_dequant_gemm,
     qwz_dequantize,
+    qwz_embedding,
     qwz_quantize,
 )

@@ -14,15 +14,30 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("ZQ_LIBRARY") or os.path.join(_PKG, "libzq.so")
 
 ZQ_F32, ZQ_F16, ZQ_BF16 = 0, 1, 2
+ZQ_I32, ZQ_I64, ZQ_INT4 = 3, 4, 5
 STATUS = {0: "ZQ_OK", -1: "ZQ_E_NULL", -2: "ZQ_E_BLOCK", -3: "ZQ_E_DTYPE", -4: "ZQ_E_ALIGN",
-          -5: "ZQ_E_SIZE", -6: "ZQ_E_P", -7: "ZQ_E_HIP", -8: "ZQ_E_ALIAS"}
+          -5: "ZQ_E_SIZE", -6: "ZQ_E_P", -7: "ZQ_E_HIP", -8: "ZQ_E_ALIAS", -9: "ZQ_E_MEMORY"}
 EXPORTS = ["qwz_quantize", "qwz_dequantize", "qgz_quantize", "qgz_reduce_level", "qgz_dequantize",
            "qgz_reduce_dequantize", "qgz_reduce_level_gather", "qgz_reduce_level_gather_noalloc",
-           "qwz_dequant_gemm", "zq_num_scales", "zq_int4_bytes", "zq_status_string"]
+           "qwz_dequant_gemm", "zq_embedding", "qwz_embedding", "zq_embedding_grad", "zq_embedding_grad_bytes",
+           "zq_grad_plan_make", "zq_grad_plan_table", "zq_grad_norm", "zq_grad_clip", "zq_int4_dequant_gemm",
+           "zq_num_scales", "zq_int4_bytes", "zq_status_string"]
 
 _TORCH_DT = {torch.float32: ZQ_F32, torch.float16: ZQ_F16, torch.bfloat16: ZQ_BF16}
 _DT_TORCH = {v: k for k, v in _TORCH_DT.items()}
+_ID_DT = {torch.int32: ZQ_I32, torch.int64: ZQ_I64}
 _lib = None
+
+
+class _Grad(ctypes.Structure):  # zq_grad
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class _GradPlan(ctypes.Structure):  # zq_grad_plan
+    _fields_ = [("bytes", ctypes.c_int64), ("norm_chunks", ctypes.c_int64), ("clip_chunks", ctypes.c_int64),
+                ("count", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class ZQError(RuntimeError):
@@ -39,7 +54,7 @@ def lib():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2501_04266_amd.build`")
     L = ctypes.CDLL(LIB_PATH)
-    vp, i64, i32, ci = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int
+    vp, i64, i32, ci, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_float
     sig = {
         "qwz_quantize": [vp, ci, i64, i32, vp, vp, vp],
         "qwz_dequantize": [vp, vp, i64, i32, vp, ci, vp],
@@ -50,12 +65,21 @@ def lib():
         "qwz_dequant_gemm": [vp, ci, vp, vp, i64, i64, i64, i32, vp, vp],
         "qgz_reduce_level_gather": [vp, vp, i32, i64, i32, vp, vp, vp],
         "qgz_reduce_level_gather_noalloc": [vp, vp, i32, i64, i32, vp, vp, vp],
+        "zq_embedding": [vp, ci, i64, vp, ci, i64, i64, f32, vp, ci, vp],
+        "qwz_embedding": [vp, ci, i64, vp, vp, i64, i64, i32, f32, vp, ci, vp],
+        "zq_embedding_grad": [vp, ci, i64, vp, ci, i64, i64, f32, ci, vp, ci, vp, i64, vp],
+        "zq_grad_plan_make": [vp, i32, vp],
+        "zq_grad_plan_table": [vp, vp, vp],
+        "zq_grad_norm": [vp, vp, f32, vp, vp],
+        "zq_grad_clip": [vp, vp, vp, f32, f32, vp],
+        "zq_int4_dequant_gemm": [vp, ci, vp, vp, i64, i64, i64, i32, vp, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
         fn.argtypes, fn.restype = args, ci
     L.zq_num_scales.argtypes, L.zq_num_scales.restype = [i64, i32], i64
     L.zq_int4_bytes.argtypes, L.zq_int4_bytes.restype = [i64], i64
+    L.zq_embedding_grad_bytes.argtypes, L.zq_embedding_grad_bytes.restype = [i64, i64, i64], i64
     L.zq_status_string.argtypes, L.zq_status_string.restype = [ci], ctypes.c_char_p
     _lib = L
     return L
@@ -309,4 +333,186 @@ def qwz_dequant_gemm(x, codes, scales, N, block=256, y=None, stream=None):
     _need(y, "y", M * N, _F32)
     _check(lib().qwz_dequant_gemm(_dev(x, "x"), _TORCH_DT[x.dtype], _dev(codes, "codes"), _dev(scales, "scales"),
                                   M, N, K, block, _dev(y, "y"), _stream(stream)), "qwz_dequant_gemm")
+    return y
+
+
+def embedding(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
+    """Rows of an embedding table by token id, times scale: out[..., :] =
+    scale * table[ids[...], :], rounded once to out_dtype (the table's if not
+    given).  ids int32 or int64 of any shape; an id outside [0, V) gives a row of
+    zeros (padding).  table [V, D] f32 / f16 / bf16 -> out [*ids.shape, D]."""
+    if table.dim() != 2:
+        raise ValueError("table must be 2-D [V, D]")
+    V, D = table.shape
+    T = ids.numel()
+    _need(ids, "ids", T, tuple(_ID_DT))
+    _need(table, "table", V * D, _ELEM)
+    if out is None:
+        out = torch.empty((*ids.shape, D), dtype=out_dtype or table.dtype, device=ids.device)
+    _need(out, "out", T * D, _ELEM)
+    _check(lib().zq_embedding(_dev(ids, "ids"), _ID_DT[ids.dtype], T, _dev(table, "table"), _TORCH_DT[table.dtype], V,
+                              D, scale, _dev(out, "out"), _TORCH_DT[out.dtype], _stream(stream)), "embedding")
+    return out
+
+
+def qwz_embedding(ids, codes, scales, V, D, block=256, scale=1.0, out_dtype=torch.bfloat16, out=None, stream=None):
+    """embedding from a table in the INT8 format (codes int8 [V*D], scales
+    [ceil(V*D/block)], as gathered): only the rows that occur are read and
+    dequantised.  With scale 1 they are the rows qwz_dequantize writes."""
+    T = ids.numel()
+    _need(ids, "ids", T, tuple(_ID_DT))
+    _need(codes, "codes", V * D, _I8)
+    _need(scales, "scales", _nsc(V * D, block), _F32)
+    if out is None:
+        out = torch.empty((*ids.shape, D), dtype=out_dtype, device=ids.device)
+    _need(out, "out", T * D, _ELEM)
+    _check(lib().qwz_embedding(_dev(ids, "ids"), _ID_DT[ids.dtype], T, _dev(codes, "codes"), _dev(scales, "scales"), V,
+                               D, block, scale, _dev(out, "out"), _TORCH_DT[out.dtype], _stream(stream)),
+           "qwz_embedding")
+    return out
+
+
+def embedding_grad_bytes(T, V, D):
+    """Bytes of workspace embedding_grad takes for T tokens and a V x D table."""
+    n = lib().zq_embedding_grad_bytes(T, V, D)
+    if n < 0:
+        raise ValueError(f"embedding_grad does not take T={T}, V={V}, D={D}")
+    return n
+
+
+def embedding_grad(ids, dy, V, scale=1.0, out_dtype=torch.float32, out=None, accumulate=False, workspace=None,
+                   stream=None):
+    """Gradient of the embedding table from dy [*ids.shape, D]: dense [V, D] of
+    out_dtype, row v the scaled sum of the rows of dy whose id is v (binary32, in a
+    fixed order), zeros where none is.  Ids outside [0, V) take no part.  With
+    accumulate the sums are added to `out` (required) and other rows stay as they
+    are.  workspace: uint8, embedding_grad_bytes(T, V, D) or more; allocated if not
+    given."""
+    T = ids.numel()
+    _need(ids, "ids", T, tuple(_ID_DT))
+    if dy.dim() < 1 or dy.numel() != T * dy.shape[-1]:
+        raise ValueError(f"dy has shape {tuple(dy.shape)}; expected {(*ids.shape, 'D')}")
+    D = dy.shape[-1]
+    _need(dy, "dy", T * D, _ELEM)
+    need = embedding_grad_bytes(T, V, D)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate adds to out: give it")
+        out = torch.empty((V, D), dtype=out_dtype, device=dy.device)
+    _need(out, "out", V * D, _ELEM)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        if stream is not None:
+            # allocated on the current stream, used on another: the allocator
+            # keeps it until that stream has passed the call
+            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+    _need(workspace, "workspace", need, _U8)
+    _check(lib().zq_embedding_grad(_dev(ids, "ids"), _ID_DT[ids.dtype], T, _dev(dy, "dy"), _TORCH_DT[dy.dtype], V, D,
+                                   scale, int(bool(accumulate)), _dev(out, "out"), _TORCH_DT[out.dtype],
+                                   _dev(workspace, "workspace"), workspace.numel(), _stream(stream)), "embedding_grad")
+    return out
+
+
+class GradTable:
+    """A rank's gradient tensors for grad_norm and grad_clip (grad_table makes it).
+    Holds the tensors; they may change their values, not their places.  Calls with
+    one table must be ordered (one stream, or events)."""
+
+    def __init__(self, tensors, outs, plan, table):
+        self.tensors, self.outs, self.plan, self.table = tensors, outs, plan, table
+
+
+def grad_table(grads, outs=None):
+    """GradTable of a list of gradients, built once for gradients that stay in
+    place.  A gradient is a dense tensor (f32 / f16 / bf16) or an INT4 shard as a
+    tuple (packed, scales, n, block).  outs: where grad_clip writes, an entry per
+    gradient: a tensor of as many elements, or None for in place (an INT4 shard's
+    scales; an INT4 shard with an out is dequantised into it)."""
+    grads = list(grads)
+    outs = [None] * len(grads) if outs is None else list(outs)
+    if len(outs) != len(grads):
+        raise ValueError(f"{len(outs)} outs for {len(grads)} gradients")
+    entries = (_Grad * max(1, len(grads)))()
+    dev = None
+    for i, (g, o, e) in enumerate(zip(grads, outs, entries)):
+        if isinstance(g, (tuple, list)):
+            packed, scales, n, block = g
+            _need(packed, f"grads[{i}] packed", int4_bytes(n), _U8)
+            _need(scales, f"grads[{i}] scales", _nsc(n, block), _F32)
+            e.data, e.scales = _dev(packed, f"grads[{i}] packed"), _dev(scales, f"grads[{i}] scales")
+            e.n, e.dtype, e.block = n, ZQ_INT4, block
+            at = packed.device
+        else:
+            _need(g, f"grads[{i}]", 0, _ELEM)
+            e.data, e.n, e.dtype = _dev(g, f"grads[{i}]"), g.numel(), _TORCH_DT[g.dtype]
+            at = g.device
+        if o is not None:
+            _need(o, f"outs[{i}]", e.n, _ELEM)
+            e.out, e.out_dtype = _dev(o, f"outs[{i}]"), _TORCH_DT[o.dtype]
+            if o.device != at:
+                raise ValueError(f"outs[{i}] is on {o.device}, its gradient on {at}")
+        if dev is not None and at != dev:
+            raise ValueError(f"grads[{i}] is on {at}, those before it on {dev}")
+        dev = at
+    if dev is None:
+        dev = torch.device("cuda", torch.cuda.current_device())
+    plan = _GradPlan()
+    _check(lib().zq_grad_plan_make(entries, len(grads), ctypes.byref(plan)), "grad_table")
+    host = torch.zeros(plan.bytes, dtype=torch.uint8)
+    _check(lib().zq_grad_plan_table(entries, ctypes.byref(plan), host.data_ptr()), "grad_table")
+    return GradTable(grads, outs, plan, host.to(dev))
+
+
+def _table(grads, stream):
+    """grads as a GradTable; one built here is kept until `stream` has passed."""
+    if isinstance(grads, GradTable):
+        return grads
+    t = grad_table(grads)
+    if stream is not None:
+        t.table.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+    return t
+
+
+def grad_norm(grads, scale=1.0, out=None, stream=None):
+    """The 2-norm of all gradients together, times |scale|: a float32 scalar tensor.
+    grads: a GradTable, or a list that grad_table takes (built for this call: it
+    copies a small table to the GPU).  Squares and sums are binary64, in a fixed
+    order."""
+    t = _table(grads, stream)
+    if out is None:
+        out = torch.empty(1, dtype=torch.float32, device=t.table.device).view(())
+    _need(out, "out", 1, _F32)
+    _check(lib().zq_grad_norm(ctypes.byref(t.plan), t.table.data_ptr(), scale, _dev(out, "out"), _stream(stream)),
+           "grad_norm")
+    return out
+
+
+def grad_clip(grads, norm, max_norm, scale=1.0, stream=None):
+    """Scales every gradient by scale * min(1, max_norm / (norm + 1e-6)), read from
+    `norm` (grad_norm's, called with the same scale) on the GPU.  Dense tensors and
+    INT4 shards' scales in place, or into the table's outs.  Returns the tensors
+    written: per gradient its out, itself, or an INT4 shard's scales."""
+    t = _table(grads, stream)
+    _need(norm, "norm", 1, _F32)
+    _check(lib().zq_grad_clip(ctypes.byref(t.plan), t.table.data_ptr(), _dev(norm, "norm"), max_norm, scale,
+                              _stream(stream)), "grad_clip")
+    return [o if o is not None else g[1] if isinstance(g, (tuple, list)) else g for g, o in zip(t.tensors, t.outs)]
+
+
+def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, stream=None):
+    """y[M, N] = x[M, K] @ W^T with W the N x K weight in the INT4 format (packed
+    uint8 [N*K/2] row-major, scales [ceil(N*K/block)]: qgz_quantize of the weight),
+    read as it is; meant for few rows.  x bf16 or fp16, y float32.  K must be a
+    multiple of 64."""
+    if x.dim() != 2:
+        raise ValueError("x must be 2-D [M, K]")
+    M, K = x.shape
+    _need(x, "x", M * K, (torch.bfloat16, torch.float16))
+    _need(packed, "packed", int4_bytes(N * K), _U8)
+    _need(scales, "scales", _nsc(N * K, block), _F32)
+    if y is None:
+        y = torch.empty((M, N), dtype=torch.float32, device=x.device)
+    _need(y, "y", M * N, _F32)
+    _check(lib().zq_int4_dequant_gemm(_dev(x, "x"), _TORCH_DT[x.dtype], _dev(packed, "packed"), _dev(scales, "scales"),
+                                      M, N, K, block, _dev(y, "y"), _stream(stream)), "int4_dequant_gemm")
     return y

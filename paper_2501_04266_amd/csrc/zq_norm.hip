@@ -1,0 +1,425 @@
+// zq_norm.hip -- the norm of a rank's gradients and their clipping, on gfx950.
+//
+//   norm = |scale| * sqrt(sum over all tensors of sum g^2)
+//   c    = fl(scale * min(1, fl(max_norm / fl(norm + 1e-6))))
+//   out  = cvt(fl(g * c))
+//
+// g are the elements of dense tensors, or q * s of INT4 shards as the reduce
+// levels leave them.  An INT4 shard needs no dequantised copy for either: its
+// sum is sum_b s_b^2 sum_{i in b} q_i^2, the inner sum in whole numbers (one
+// v_dot8_i32_i4 for 8 codes), and clipping it means scaling its scales.
+//
+// Bound by memory: each byte is read once (and, clipping, written once).  The
+// squares are summed in binary64, exactly squared binary32 values, so neither
+// overflow nor underflow of a square is met and the order of the sums does not
+// show in the binary32 result except by one rounding; the order is fixed all
+// the same.
+//
+// One launch covers all tensors: the table holds an entry per tensor with the
+// index of its first chunk (16 KiB of data), workgroup w takes the chunks [w n / W,
+// (w + 1) n / W) of all n and finds its first tensor by comparing against all entries
+// at once.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "zq.h"
+#include "zq_device.h"
+#include "zq_host.h"
+#include "zq_vec.h"
+
+#pragma clang fp contract(off)
+
+namespace zq {
+namespace {
+
+constexpr int kNormThreads = 256;
+constexpr int kNormGroups = 2048;     // workgroups at most: 8 a CU
+constexpr int64_t kChunkBytes = 16384;  // data of a chunk
+constexpr int kInt4 = 3;              // type code of an entry's INT4 data
+
+// One tensor of the table.  Read by every workgroup, so 48 bytes.
+struct Entry {
+  const char* data;
+  const float* scales;
+  char* out;
+  int64_t n;        // elements
+  int64_t chunk0;   // chunks of the entries before it
+  int8_t type, out_type, lgB, pad;
+  int32_t pad4;
+};
+static_assert(sizeof(Entry) == 48, "table layout");
+
+// elements of a chunk of `type`
+__host__ __device__ constexpr int64_t chunk_elems(int type) {
+  return type == kInt4 ? 2 * kChunkBytes : type == ZQ_F32 ? kChunkBytes / 4 : kChunkBytes / 2;
+}
+
+// Table: the counter of finished workgroups, their sums, the entries of the norm,
+// the entries of clipping (an INT4 shard clipped in place is its scales there).
+constexpr int64_t kSumsAt = 64, kEntriesAt = kSumsAt + 8 * kNormGroups;
+__host__ __device__ inline int64_t clip_at(int entries) { return kEntriesAt + (int64_t)entries * (int64_t)sizeof(Entry); }
+
+// index of the entry that holds chunk c (every thread gets it)
+__device__ __forceinline__ int find_entry(const Entry* entries, int count, int64_t c) {
+  __shared__ int found;
+  for (int i = threadIdx.x; i < count; i += kNormThreads) {
+    const int64_t a = entries[i].chunk0;
+    const int64_t b = i + 1 < count ? entries[i + 1].chunk0 : INT64_MAX;
+    if (a <= c && c < b) found = i;
+  }
+  __syncthreads();
+  return found;
+}
+
+template <int DT>
+__device__ __forceinline__ double sum_squares(const Entry& en, int64_t e0, int64_t e1) {
+  constexpr int E = 16 / dt_size<DT>();
+  double a = 0.0;
+  int64_t i = e0 + (int64_t)threadIdx.x * E;
+  for (; i + E <= e1; i += kNormThreads * E) {
+    float v[E];
+    if constexpr (DT == ZQ_F32) {
+      load_elems<DT, 4>(en.data, i, v);
+    } else {
+      load_elems<DT, 8>(en.data, i, v);
+    }
+#pragma unroll
+    for (int k = 0; k < E; ++k) a = __builtin_fma((double)v[k], (double)v[k], a);
+  }
+  for (; i < e1; ++i) {  // one thread: the elements of the last, short piece
+    float v[1];
+    load_elems<DT, 1>(en.data, i, v);
+    a = __builtin_fma((double)v[0], (double)v[0], a);
+  }
+  return a;
+}
+
+// 32 codes a thread and step: within one block, as blocks are multiples of 32
+__device__ __forceinline__ double sum_squares_int4(const Entry& en, int64_t e0, int64_t e1) {
+  double a = 0.0;
+  for (int64_t i = e0 + (int64_t)threadIdx.x * 32; i < e1; i += kNormThreads * 32) {
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    const char* p = en.data + i / 2;
+    if (i + 32 <= e1) {
+      load_words_any<false>(p, w);
+    } else {
+      for (int k = 0; i + k < e1; ++k) {
+        const uint32_t q = (uint8_t)p[k / 2] >> (4 * (k & 1)) & 15u;
+        w[k / 8] |= q << (4 * (k % 8));
+      }
+    }
+    int q2 = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q2 = __builtin_amdgcn_sdot8((int)w[k], (int)w[k], q2, false);
+    const double s = (double)en.scales[i >> en.lgB];
+    a = __builtin_fma(s * s, (double)q2, a);
+  }
+  return a;
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// sum over the workgroup, in thread 0
+__device__ __forceinline__ double group_sum(double v) {
+  __shared__ double part[kNormThreads / 64];
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0.0;
+  for (int w = 0; w < kNormThreads / 64; ++w) s += part[w];
+  __syncthreads();
+  return s;
+}
+
+__global__ void __launch_bounds__(kNormThreads)
+    k_grad_norm(char* __restrict__ table, int count, int64_t chunks, float scale, float* __restrict__ norm) {
+  const Entry* entries = reinterpret_cast<const Entry*>(table + kEntriesAt);
+  double* sums = reinterpret_cast<double*>(table + kSumsAt);
+  unsigned* counter = reinterpret_cast<unsigned*>(table);
+  const int64_t W = gridDim.x, w = blockIdx.x;
+  int64_t c = w * chunks / W;
+  const int64_t c1 = (w + 1) * chunks / W;
+  double a = 0.0;
+  if (c < c1) {
+    int i = find_entry(entries, count, c);
+    while (c < c1) {
+      const Entry en = entries[i];
+      const int64_t per = chunk_elems(en.type);
+      const int64_t e0 = (c - en.chunk0) * per;
+      const int64_t last = en.chunk0 + (en.n + per - 1) / per;  // the next entry's first chunk
+      const int64_t to = c1 < last ? c1 : last;
+      int64_t e1 = (to - en.chunk0) * per;
+      if (e1 > en.n) e1 = en.n;
+      switch (en.type) {
+        case ZQ_F32: a += sum_squares<ZQ_F32>(en, e0, e1); break;
+        case ZQ_F16: a += sum_squares<ZQ_F16>(en, e0, e1); break;
+        case ZQ_BF16: a += sum_squares<ZQ_BF16>(en, e0, e1); break;
+        default: a += sum_squares_int4(en, e0, e1); break;
+      }
+      c = to;
+      ++i;
+    }
+  }
+  a = group_sum(a);
+  // the last workgroup to finish adds the sums, in the order of the workgroups
+  __shared__ bool last;
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(&sums[w], a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)W - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  double t = 0.0;
+  for (int64_t k = threadIdx.x; k < W; k += kNormThreads)
+    t += __hip_atomic_load(&sums[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  t = group_sum(t);
+  if (threadIdx.x == 0) {
+    *norm = (float)(fabs((double)scale) * sqrt(t));
+    __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next call
+  }
+}
+
+template <int DT, int YT>
+__device__ __forceinline__ void scale_elems(const Entry& en, int64_t e0, int64_t e1, float c) {
+  constexpr int E = 16 / dt_size<DT>();
+  int64_t i = e0 + (int64_t)threadIdx.x * E;
+  for (; i + E <= e1; i += kNormThreads * E) {
+    float v[E];
+    if constexpr (DT == ZQ_F32) load_elems<DT, 4>(en.data, i, v);
+    else load_elems<DT, 8>(en.data, i, v);
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = v[k] * c;
+    store_elems<YT, E>(en.out, i, v);
+  }
+  for (; i < e1; ++i) {
+    float v[1];
+    load_elems<DT, 1>(en.data, i, v);
+    v[0] = v[0] * c;
+    store_elems<YT, 1>(en.out, i, v);
+  }
+}
+
+// the INT4 shard dequantised with its scales times c: fl(q * fl(s * c))
+template <int YT>
+__device__ __forceinline__ void scale_int4(const Entry& en, int64_t e0, int64_t e1, float c) {
+  constexpr int E = 8;
+  int64_t i = e0 + (int64_t)threadIdx.x * E;
+  for (; i + E <= e1; i += kNormThreads * E) {
+    uint32_t w[1];
+    load_words_any<false>(en.data + i / 2, w);
+    const float s = en.scales[i >> en.lgB] * c;
+    float v[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) v[k] = (float)((int32_t)(w[0] << (28 - 4 * k)) >> 28) * s;
+    store_elems<YT, E>(en.out, i, v);
+  }
+  for (; i < e1; ++i) {
+    const uint32_t q = (uint8_t)en.data[i / 2] >> (4 * (i & 1));
+    float v[1] = {(float)((int32_t)(q << 28) >> 28) * (en.scales[i >> en.lgB] * c)};
+    store_elems<YT, 1>(en.out, i, v);
+  }
+}
+
+template <int YT>
+__device__ __forceinline__ void scale_to(const Entry& en, int64_t e0, int64_t e1, float c) {
+  switch (en.type) {
+    case ZQ_F32: scale_elems<ZQ_F32, YT>(en, e0, e1, c); break;
+    case ZQ_F16: scale_elems<ZQ_F16, YT>(en, e0, e1, c); break;
+    case ZQ_BF16: scale_elems<ZQ_BF16, YT>(en, e0, e1, c); break;
+    default: scale_int4<YT>(en, e0, e1, c); break;
+  }
+}
+
+__global__ void __launch_bounds__(kNormThreads)
+    k_grad_clip(const char* __restrict__ table, int norm_count, int count, int64_t chunks,
+                const float* __restrict__ norm, float max_norm, float scale) {
+  const Entry* entries = reinterpret_cast<const Entry*>(table + clip_at(norm_count));
+  const float ratio = max_norm / (*norm + 1e-6f);
+  // a NaN ratio stays: min would drop it
+  const float c = scale * (ratio > 1.0f ? 1.0f : ratio);
+  const int64_t W = gridDim.x, w = blockIdx.x;
+  int64_t k = w * chunks / W;
+  const int64_t k1 = (w + 1) * chunks / W;
+  if (k >= k1) return;
+  int i = find_entry(entries, count, k);
+  while (k < k1) {
+    const Entry en = entries[i];
+    const int64_t per = chunk_elems(en.type);
+    const int64_t e0 = (k - en.chunk0) * per;
+    const int64_t last = en.chunk0 + (en.n + per - 1) / per;
+    const int64_t to = k1 < last ? k1 : last;
+    int64_t e1 = (to - en.chunk0) * per;
+    if (e1 > en.n) e1 = en.n;
+    // in place and nothing to scale: the tensor stays as it is
+    if (!(en.out == en.data && c == 1.0f)) {
+      switch (en.out_type) {
+        case ZQ_F32: scale_to<ZQ_F32>(en, e0, e1, c); break;
+        case ZQ_F16: scale_to<ZQ_F16>(en, e0, e1, c); break;
+        default: scale_to<ZQ_BF16>(en, e0, e1, c); break;
+      }
+    }
+    k = to;
+    ++i;
+  }
+}
+
+// ---------------------------------------------------------------- table
+
+int64_t data_bytes(int64_t n, int type) { return type == kInt4 ? (n + 1) / 2 : n * elem_bytes(type); }
+
+int check(const zq_grad& g) {
+  if (g.n < 0 || g.n > INT64_MAX / 16) return ZQ_E_SIZE;
+  const bool int4 = g.dtype == ZQ_INT4;
+  if (!int4 && !dtype_ok(g.dtype)) return ZQ_E_DTYPE;
+  if (g.out && !dtype_ok(g.out_dtype)) return ZQ_E_DTYPE;
+  if (int4 && log2_block(g.block) < 0) return ZQ_E_BLOCK;
+  if (g.n == 0) return ZQ_OK;
+  if (!g.data || (int4 && !g.scales)) return ZQ_E_NULL;
+  if (!int4 && !aligned(g.data, elem_bytes(g.dtype))) return ZQ_E_ALIGN;
+  if (int4 && !aligned(g.scales, 4)) return ZQ_E_ALIGN;
+  if (g.out && !aligned(g.out, elem_bytes(g.out_dtype))) return ZQ_E_ALIGN;
+  // in place, the type stays
+  if (!int4 && g.out == g.data && g.out_dtype != g.dtype) return ZQ_E_ALIAS;
+  return ZQ_OK;
+}
+
+Entry norm_entry(const zq_grad& g) {
+  Entry e = {};
+  e.data = static_cast<const char*>(g.data);
+  e.scales = g.scales;
+  e.n = g.n;
+  e.type = (int8_t)(g.dtype == ZQ_INT4 ? kInt4 : g.dtype);
+  e.lgB = (int8_t)(g.dtype == ZQ_INT4 ? log2_block(g.block) : 0);
+  return e;
+}
+Entry clip_entry(const zq_grad& g) {
+  Entry e = norm_entry(g);
+  if (g.out) {
+    e.out = static_cast<char*>(g.out);
+    e.out_type = (int8_t)g.out_dtype;
+  } else if (g.dtype == ZQ_INT4) {
+    e.data = reinterpret_cast<const char*>(g.scales);
+    e.out = reinterpret_cast<char*>(g.scales);
+    e.scales = nullptr;
+    e.n = num_scales(g.n, g.block);
+    e.type = e.out_type = ZQ_F32;
+  } else {
+    e.out = static_cast<char*>(g.data);
+    e.out_type = e.type;
+  }
+  return e;
+}
+int64_t chunks_of(const Entry& e) { return (e.n + chunk_elems(e.type) - 1) / chunk_elems(e.type); }
+
+// Outputs must not overlap each other nor another tensor's data: the ranges in
+// the order of their addresses, each output against what starts before its end.
+int check_overlaps(const zq_grad* grads, int32_t count) {
+  struct Span {
+    uintptr_t from, to;
+    int tensor;
+    bool out;
+  };
+  std::vector<Span> spans;
+  spans.reserve(3 * (size_t)count);
+  auto put = [&](const void* p, int64_t bytes, int tensor, bool out) {
+    if (p && bytes > 0) spans.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, tensor, out});
+  };
+  for (int32_t i = 0; i < count; ++i) {
+    const zq_grad& g = grads[i];
+    const Entry n = norm_entry(g), c = clip_entry(g);
+    if (g.n == 0) continue;
+    const bool in_place = c.out == (g.dtype == ZQ_INT4 && !g.out ? (const char*)g.scales : (const char*)g.data);
+    put(c.out, c.n * elem_bytes(c.out_type), i, true);
+    if (!(in_place && g.dtype != ZQ_INT4)) put(n.data, data_bytes(n.n, n.type), i, false);
+    if (g.dtype == ZQ_INT4 && g.out) put(g.scales, 4 * num_scales(g.n, g.block), i, false);
+  }
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
+  // the furthest end of outputs, and of anything, among the spans before
+  uintptr_t out_to = 0, any_to = 0;
+  for (const Span& s : spans) {
+    if (s.from < out_to || (s.out && s.from < any_to)) return ZQ_E_ALIAS;
+    any_to = std::max(any_to, s.to);
+    if (s.out) out_to = std::max(out_to, s.to);
+  }
+  return ZQ_OK;
+}
+
+int plan_table(const zq_grad* grads, int32_t count, zq_grad_plan* plan) {
+  if (!plan || (count > 0 && !grads)) return ZQ_E_NULL;
+  if (count < 0) return ZQ_E_SIZE;
+  zq_grad_plan p = {};
+  p.count = count;
+  for (int32_t i = 0; i < count; ++i) {
+    const int rc = check(grads[i]);
+    if (rc != ZQ_OK) return rc;
+    p.norm_chunks += chunks_of(norm_entry(grads[i]));
+    p.clip_chunks += chunks_of(clip_entry(grads[i]));
+  }
+  const int rc = check_overlaps(grads, count);
+  if (rc != ZQ_OK) return rc;
+  p.bytes = clip_at(count) + (int64_t)count * (int64_t)sizeof(Entry);
+  *plan = p;
+  return ZQ_OK;
+}
+
+unsigned groups_for(int64_t chunks) { return (unsigned)(chunks < kNormGroups ? (chunks < 1 ? 1 : chunks) : kNormGroups); }
+
+}  // namespace
+}  // namespace zq
+
+extern "C" {
+
+using namespace zq;
+
+int zq_grad_plan_make(const zq_grad* grads, int32_t count, zq_grad_plan* plan) {
+  try {
+    return plan_table(grads, count, plan);
+  } catch (...) {  // no memory for the overlap check
+    return ZQ_E_MEMORY;
+  }
+}
+
+int zq_grad_plan_table(const zq_grad* grads, const zq_grad_plan* plan, void* host_table) {
+  if (!plan || !host_table || (plan->count > 0 && !grads)) return ZQ_E_NULL;
+  char* t = static_cast<char*>(host_table);
+  std::fill(t, t + kEntriesAt, (char)0);
+  Entry* norm = reinterpret_cast<Entry*>(t + kEntriesAt);
+  Entry* clip = reinterpret_cast<Entry*>(t + clip_at(plan->count));
+  int64_t n = 0, c = 0;
+  for (int32_t i = 0; i < plan->count; ++i) {
+    norm[i] = norm_entry(grads[i]);
+    clip[i] = clip_entry(grads[i]);
+    norm[i].chunk0 = n;
+    clip[i].chunk0 = c;
+    n += chunks_of(norm[i]);
+    c += chunks_of(clip[i]);
+  }
+  return ZQ_OK;
+}
+
+int zq_grad_norm(const zq_grad_plan* plan, void* table, float scale, float* norm, void* stream) {
+  if (!plan || !table || !norm) return ZQ_E_NULL;
+  if (!aligned(table, 16) || !aligned(norm, 4)) return ZQ_E_ALIGN;
+  return launch(&k_grad_norm, groups_for(plan->norm_chunks), kNormThreads, static_cast<hipStream_t>(stream),
+                static_cast<char*>(table), plan->count, plan->norm_chunks, scale, norm);
+}
+
+int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm, float max_norm, float scale,
+                 void* stream) {
+  if (!plan || !table || !norm) return ZQ_E_NULL;
+  if (!aligned(table, 16) || !aligned(norm, 4)) return ZQ_E_ALIGN;
+  if (!(max_norm >= 0.0f)) return ZQ_E_SIZE;
+  if (plan->clip_chunks == 0) return ZQ_OK;
+  return launch(&k_grad_clip, groups_for(plan->clip_chunks), kNormThreads, static_cast<hipStream_t>(stream),
+                static_cast<const char*>(table), plan->count, plan->count, plan->clip_chunks, norm, max_norm, scale);
+}
+
+}  // extern "C"
