@@ -12,6 +12,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "zq.h"
 #include "zq_device.h"
 #include "zq_host.h"
@@ -107,61 +109,106 @@ __global__ void __launch_bounds__(kEmbedThreads)
 // The order of every sum follows from the ids alone: no atomics on sums.
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kMaxRange = 512;   // rows of a workgroup's range (counts: 32 KiB of LDS)
+constexpr int kRangeBits = 9, kMaxRange = 1 << kRangeBits;  // rows of a workgroup's range at most (36 KiB of LDS)
 constexpr int kPart = 64;        // positions of a partial sum
 constexpr int64_t kMaxTokens = 1 << 30;
 
-// Adds this lane's row to the wave's counts: the lanes of one row in one step.
-// Returns the row's count before this group's, plus the lanes of the row
-// before this one (the lane's place among the row's tokens of this wave).
-__device__ __forceinline__ int take_place(int* counts, bool in, int row, int bits) {
-  const int lane = threadIdx.x & 63;
-  uint64_t peers = __ballot(in);
-  for (int b = 0; b < bits; ++b) {
-    const uint64_t set = __ballot(row >> b & 1);
-    peers &= row >> b & 1 ? set : ~set;
+// This lane's place among the tokens of its row: the row's count so far (in the
+// wave's `counts`) and the lanes of the same row before it; the counts move on.
+// The lanes of one row are found by comparing the rows bit by bit.
+__device__ __forceinline__ int take_place(int* counts, bool in, int row) {
+  const uint64_t all = __ballot(in);
+  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+#pragma unroll
+  for (int b = 0; b < kRangeBits; ++b) {
+    const uint32_t mine = (uint32_t)((int32_t)((uint32_t)row << (31 - b)) >> 31);
+    const uint64_t set = __ballot(mine != 0);
+    lo &= ~((uint32_t)set ^ mine);
+    hi &= ~((uint32_t)(set >> 32) ^ mine);
   }
   int place = 0;
   if (in) {
-    const int before = __popcll(peers & ((1ull << lane) - 1));
+    const int before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
     const int base = counts[row];
     place = base + before;
-    if (before == 0) counts[row] = base + __popcll(peers);
+    if (before == 0) counts[row] = base + __popc(lo) + __popc(hi);
   }
   // the next group's reads come after this group's writes
   __builtin_amdgcn_wave_barrier();
   return place;
 }
 
+constexpr int kSortSteps = 8;   // groups of 64 ids that a wave loads at a time
+constexpr int kCopies = 4;      // of a row's counts: lanes that count the same row meet less often
+constexpr int kSortLds = (kSortWaves + 2 * kCopies) * kMaxRange * 4;
+
+// Workgroup (r, p) writes the tokens of part p that belong to rows [r kMaxRange, (r +
+// 1) kMaxRange).  It counts its rows' tokens in all parts by itself.
+template <typename Id>
 __global__ void __launch_bounds__(kSortThreads)
-    k_sort_ids(const void* __restrict__ ids, bool wide, int T, int64_t V, int range, int bits, int* __restrict__ start,
+    k_sort_ids(const Id* __restrict__ ids, int T, int64_t V, int parts, int* __restrict__ start,
                int* __restrict__ order) {
-  extern __shared__ int counts[];  // kSortWaves x range
-  __shared__ int before[kSortWaves], sums[kSortWaves];
+  // counts of the own part's tokens by wave, of those of the parts before it and after it
+  __shared__ int counts[kSortLds / 4];
+  __shared__ int less_of[kSortWaves], sums[kSortWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t lo = (int64_t)blockIdx.x * range;
-  const int rows = (int)(V - lo < range ? V - lo : range);
-  int* mine = counts + wave * range;
-  for (int i = threadIdx.x; i < kSortWaves * range; i += kSortThreads) counts[i] = 0;
+  int* const mine = counts + wave * kMaxRange;
+  int* const before = counts + kSortWaves * kMaxRange;  // [row][copy]
+  int* const after = before + kCopies * kMaxRange;
+  const int p = blockIdx.x % parts;
+  const int lo = (int)(blockIdx.x / parts) * kMaxRange;
+  const int rows = (int)(V - lo < kMaxRange ? V - lo : kMaxRange);
+  for (int i = threadIdx.x; i < kSortLds / 16; i += kSortThreads)
+    reinterpret_cast<u32x4*>(counts)[i] = u32x4{0u, 0u, 0u, 0u};
   __syncthreads();
 
-  const int part = ((T + kSortWaves - 1) / kSortWaves + 63) & ~63;
-  const int64_t t0 = (int64_t)wave * part, t1 = t0 + part < T ? t0 + part : T;
+  // part q: tokens [16 q sub, 16 (q + 1) sub), wave w its w-th sixteenth, of whole groups
+  const int sub = ((T + parts * kSortWaves - 1) / (parts * kSortWaves) + 63) & ~63;
+  const int groups = sub / 64;
+  // The rows of kSortSteps groups, those of part q from group f on and then those of
+  // the next parts.  All loads go out before the first id is looked at (where there is
+  // no token the last one is read).  What is no row, or no token, compares above every row.
+  auto read = [&](int q, int f, int(&row)[kSortSteps], int(&part)[kSortSteps]) {
+    Id id[kSortSteps];
+    unsigned at[kSortSteps];
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u) {
+      at[u] = q < parts ? (unsigned)((q * kSortWaves + wave) * sub + f * 64) + lane : ~0u;
+      id[u] = ids[at[u] < (unsigned)T ? at[u] : (unsigned)T - 1];
+      part[u] = q;
+      if (++f == groups) f = 0, ++q;
+    }
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u)
+      row[u] = at[u] < (unsigned)T && (uint64_t)(int64_t)id[u] < (uint64_t)V ? (int)id[u] : 0x7fffffff;
+  };
   int less = 0;
-  for (int64_t t = t0 + lane; t - lane < t1; t += 64) {
-    const int64_t id = t < t1 ? id_at(ids, wide, t) : -1;
-    const bool in = id >= lo && id < lo + rows;
-    less += id >= 0 && id < lo;
-    if (__ballot(in)) take_place(mine, in, in ? (int)(id - lo) : 0, bits);
+  for (int g = 0; g < parts * groups && T > 0; g += kSortSteps) {
+    int row[kSortSteps], part[kSortSteps];
+    read(g / groups, g % groups, row, part);
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u) {
+      less += row[u] < lo;
+      const unsigned rel = (unsigned)(row[u] - lo);
+      const bool own = part[u] == p;
+      const int from = own ? wave * kMaxRange : kSortWaves * kMaxRange + (part[u] < p ? 0 : kCopies * kMaxRange);
+      if (rel < (unsigned)rows) atomicAdd(&counts[from + (own ? rel : rel * kCopies + lane % kCopies)], 1);
+    }
   }
   for (int o = 32; o; o >>= 1) less += __shfl_xor(less, o);
-  if (lane == 0) before[wave] = less;
+  if (lane == 0) less_of[wave] = less;
   __syncthreads();
 
-  // counts -> places: rows in order, and within a row the waves
-  int total = 0;
-  if (threadIdx.x < (unsigned)rows)
-    for (int w = 0; w < kSortWaves; ++w) total += counts[w * range + threadIdx.x];
+  // counts -> places: rows in order, and within a row the parts, then the waves
+  const int i = threadIdx.x;
+  int own[kSortWaves], earlier = 0, total = 0;
+  if (i < rows) {
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) own[w] = counts[w * kMaxRange + i], total += own[w];
+#pragma unroll
+    for (int k = 0; k < kCopies; ++k) earlier += before[i * kCopies + k], total += after[i * kCopies + k];
+    total += earlier;
+  }
   int upto = total;
   for (int o = 1; o < 64; o <<= 1) {
     const int v = __shfl_up(upto, o);
@@ -170,106 +217,174 @@ __global__ void __launch_bounds__(kSortThreads)
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
   int place = upto - total;
+#pragma unroll
   for (int w = 0; w < kSortWaves; ++w) {
-    place += before[w];
+    place += less_of[w];
     if (w < wave) place += sums[w];
   }
-  if (threadIdx.x < (unsigned)rows) {
-    start[lo + threadIdx.x] = place;
-    if (lo + threadIdx.x == V - 1) start[V] = place + total;
+  if (i < rows) {
+    if (p == 0) {
+      start[lo + i] = place;
+      if (lo + i == V - 1) start[V] = place + total;
+    }
+    place += earlier;
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const int c = counts[w * range + threadIdx.x];
-      counts[w * range + threadIdx.x] = place;
-      place += c;
+      counts[w * kMaxRange + i] = place;
+      place += own[w];
     }
   }
   __syncthreads();
 
-  for (int64_t t = t0 + lane; t - lane < t1; t += 64) {
-    const int64_t id = t < t1 ? id_at(ids, wide, t) : -1;
-    const bool in = id >= lo && id < lo + rows;
-    if (__ballot(in)) {
-      const int at = take_place(mine, in, in ? (int)(id - lo) : 0, bits);
-      if (in) order[at] = (int)t;
+  for (int f = 0; f < groups && T > 0; f += kSortSteps) {
+    int row[kSortSteps], part[kSortSteps];
+    read(p, f, row, part);
+#pragma unroll
+    for (int u = 0; u < kSortSteps; ++u) {
+      const unsigned rel = (unsigned)(row[u] - lo);
+      const bool in = rel < (unsigned)rows && part[u] == p;
+      if (__ballot(in)) {
+        const int at = take_place(mine, in, in ? (int)rel : 0);
+        if (in) order[at] = (p * kSortWaves + wave) * sub + (f + u) * 64 + lane;
+      }
     }
   }
 }
 
-// sum of the rows of dy at positions [p, end) of the order, from `acc` on
+// A wave of the two kernels below works on 64 pieces of E columns of one row.  Which
+// row and which of its `per` waves: one binary64 product, as in locate().
+struct WaveRow {
+  int64_t row;
+  int sub;
+};
+__device__ __forceinline__ WaveRow wave_row(int per, double inv_per) {
+  const int64_t w = (int64_t)blockIdx.x * (kEmbedThreads / 64) + (threadIdx.x >> 6);
+  int64_t row = (int64_t)((double)w * inv_per);
+  int64_t sub = w - row * per;
+  if (sub < 0) --row, sub += per;
+  else if (sub >= per) ++row, sub -= per;
+  return {__builtin_amdgcn_readfirstlane((int)row), __builtin_amdgcn_readfirstlane((int)sub)};
+}
+
+// First column of piece c of C: the row's last piece starts E before its end.
+// Lanes past the last piece repeat it and store nothing.
+template <int E>
+__device__ __forceinline__ int64_t piece_column(int c, int C, int64_t D) {
+  return c < C - 1 ? (int64_t)c * E : D - E;
+}
+
+// acc += N rows of `type` at element offsets at[u], in their order; all loads go out
+// before the first addition
+template <int DT, int E, int N>
+__device__ __forceinline__ void add_rows(const void* base, const int64_t (&at)[N], float (&acc)[E]) {
+  float v[N][E];
+#pragma unroll
+  for (int u = 0; u < N; ++u) load_elems<DT, E>(base, at[u], v[u]);
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int i = 0; i < E; ++i) acc[i] += v[u][i];
+}
+
+// Adds the rows of dy at positions [p, end) of the order to acc, in this order.  The
+// wave reads its positions' tokens 64 at a time, one a lane.  p and end are the same in
+// all lanes.
 template <int GT, int E>
 __device__ __forceinline__ void add_tokens(const void* dy, const int* order, int p, int end, int64_t D, int64_t d,
                                            float (&acc)[E]) {
-  for (; p < end; ++p) {
-    float v[E];
-    load_elems<GT, E>(dy, (int64_t)order[p] * D + d, v);
+  const int lane = threadIdx.x & 63;
+  for (; p < end; p += 64) {
+    const int n = end - p < 64 ? end - p : 64;
+    const int tokens = lane < n ? order[p + lane] : 0;
+    auto batch = [&](int b, auto count) {
+      constexpr int N = decltype(count)::value;
+      int64_t at[N];
 #pragma unroll
-    for (int i = 0; i < E; ++i) acc[i] += v[i];
+      for (int u = 0; u < N; ++u) at[u] = (int64_t)__builtin_amdgcn_readlane(tokens, b + u) * D + d;
+      add_rows<GT, E, N>(dy, at, acc);
+    };
+    int b = 0;
+    for (; b + 8 <= n; b += 8) batch(b, std::integral_constant<int, 8>{});
+    if (n - b >= 4) batch(b, std::integral_constant<int, 4>{}), b += 4;
+    if (n - b >= 2) batch(b, std::integral_constant<int, 2>{}), b += 2;
+    if (n - b >= 1) batch(b, std::integral_constant<int, 1>{});
   }
 }
 
 template <int GT, int E>
 __global__ void __launch_bounds__(kEmbedThreads)
     k_grad_parts(const void* __restrict__ ids, bool wide, const void* __restrict__ dy, const int* __restrict__ start,
-                 const int* __restrict__ order, int64_t V, int64_t D, int C, int cols, float* __restrict__ parts) {
-  const int64_t j = blockIdx.x / cols;
-  const int c = (int)(blockIdx.x % cols) * kEmbedThreads + threadIdx.x;
-  const int64_t p0 = j * kPart;
-  if (p0 + kPart > start[V]) return;
+                 const int* __restrict__ order, int64_t segs, int64_t V, int64_t D, int C, int per, double inv_per,
+                 float* __restrict__ parts) {
+  const WaveRow w = wave_row(per, inv_per);
+  const int64_t p0 = w.row * kPart;
+  if (w.row >= segs || p0 + kPart > start[V]) return;
   if (id_at(ids, wide, order[p0]) != id_at(ids, wide, order[p0 + kPart - 1])) return;
-  if (c >= C) return;
-  const int64_t d0 = (int64_t)c * E, d = d0 + E > D ? D - E : d0;
-  float acc[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) acc[i] = 0.0f;
+  const int c = w.sub * 64 + (threadIdx.x & 63);
+  const int64_t d = piece_column<E>(c, C, D);
+  float acc[E] = {};
   add_tokens<GT, E>(dy, order, (int)p0, (int)p0 + kPart, D, d, acc);
-  store_elems<ZQ_F32, E>(parts, j * D + d, acc);
+  if (c < C) store_elems<ZQ_F32, E>(parts, w.row * D + d, acc);
 }
 
+// The result is written past the caches: it is read again only once it is whole, and
+// its writing otherwise costs the reads of dy their place (50,000 x 6,144 in binary32,
+// 16,384 tokens: 348 us with plain stores, 215 so).  One piece a lane: with two or four
+// of them 248 and 264 us.
 template <int GT, int YT, int E, bool ADD>
 __global__ void __launch_bounds__(kEmbedThreads)
     k_grad_rows(const void* __restrict__ dy, const int* __restrict__ start, const int* __restrict__ order,
-                const float* __restrict__ parts, int64_t V, int64_t D, int C, double inv_c, float scale,
+                const float* __restrict__ parts, int64_t V, int64_t D, int C, int per, double inv_per, float scale,
                 void* __restrict__ dw) {
-  const Piece p = locate(blockIdx.x, C, inv_c);
-  if (p.row >= V) return;
-  const int s = start[p.row], e = start[p.row + 1];
+  const WaveRow w = wave_row(per, inv_per);
+  if (w.row >= V) return;
+  const int s = start[w.row], e = start[w.row + 1];
   if (ADD && s == e) return;
-  const int64_t d0 = (int64_t)p.piece * E;
-  const int64_t d = d0 + E > D ? D - E : d0;
-  float acc[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) acc[i] = 0.0f;
+  const int c = w.sub * 64 + (threadIdx.x & 63);
+  const int64_t d = piece_column<E>(c, C, D);
+  float acc[E] = {};
   if (s < e) {
     const int j0 = (s + kPart - 1) / kPart, j1 = e / kPart;
+    const int head = j0 < j1 ? j0 * kPart : e;  // whole 64s of this row: parts [j0, j1)
+    add_tokens<GT, E>(dy, order, s, head, D, d, acc);
     if (j0 < j1) {
-      add_tokens<GT, E>(dy, order, s, j0 * kPart, D, d, acc);
-      for (int j = j0; j < j1; ++j) {
-        float v[E];
-        load_elems<ZQ_F32, E>(parts, (int64_t)j * D + d, v);
+      auto add_parts = [&](int j, auto count) {
+        constexpr int N = decltype(count)::value;
+        int64_t at[N];
 #pragma unroll
-        for (int i = 0; i < E; ++i) acc[i] += v[i];
-      }
+        for (int u = 0; u < N; ++u) at[u] = (int64_t)(j + u) * D + d;
+        add_rows<ZQ_F32, E, N>(parts, at, acc);
+      };
+      int j = j0;
+      for (; j + 16 <= j1; j += 16) add_parts(j, std::integral_constant<int, 16>{});
+      for (; j + 4 <= j1; j += 4) add_parts(j, std::integral_constant<int, 4>{});
+      for (; j < j1; ++j) add_parts(j, std::integral_constant<int, 1>{});
       add_tokens<GT, E>(dy, order, j1 * kPart, e, D, d, acc);
-    } else {
-      add_tokens<GT, E>(dy, order, s, e, D, d, acc);
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) acc[i] = scale * acc[i];
   }
+  if (c >= C) return;
   if constexpr (ADD) {
+    // where E does not divide D the row's last piece overlaps the one before it: the
+    // shared elements are that one's to add
+    const int skip = c == C - 1 ? (int)((int64_t)C * E - D) : 0;
     float old[E];
-    // the row's last piece overlaps the one before it where E does not divide D:
-    // the shared elements are the earlier piece's to add
-    const int skip = (int)(d0 - d);
-    load_elems<YT, E>(dw, p.row * D + d, old);
+    load_elems<YT, E>(dw, w.row * D + d, old);
+    if (skip == 0) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      if (i < skip) continue;
-      float one[1] = {old[i] + acc[i]};
-      store_elems<YT, 1>(dw, p.row * D + d + i, one);
+      for (int i = 0; i < E; ++i) acc[i] = old[i] + acc[i];
+      store_elems<YT, E>(dw, w.row * D + d, acc);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        if (i < skip) continue;
+        const float one[1] = {old[i] + acc[i]};
+        store_elems<YT, 1>(dw, w.row * D + d + i, one);
+      }
     }
   } else {
-    store_elems<YT, E>(dw, p.row * D + d, acc);
+    store_elems<YT, E, true>(dw, w.row * D + d, acc);
   }
 }
 
@@ -289,29 +404,37 @@ EmbedKernel embed_kernel(int wt, int yt) {
                         : embed_kernel_to<ZQ_BF16, E>(yt);
 }
 
-using PartsKernel = void (*)(const void*, bool, const void*, const int*, const int*, int64_t, int64_t, int, int,
-                             float*);
+using PartsKernel = void (*)(const void*, bool, const void*, const int*, const int*, int64_t, int64_t, int64_t, int,
+                             int, double, float*);
 template <int E>
 PartsKernel parts_kernel(int gt) {
   return gt == ZQ_F32 ? &k_grad_parts<ZQ_F32, E> : gt == ZQ_F16 ? &k_grad_parts<ZQ_F16, E> : &k_grad_parts<ZQ_BF16, E>;
 }
-using RowsKernel = void (*)(const void*, const int*, const int*, const float*, int64_t, int64_t, int, double, float,
-                            void*);
+using RowsKernel = void (*)(const void*, const int*, const int*, const float*, int64_t, int64_t, int, int, double,
+                            float, void*);
 template <int GT, int YT, int E>
 RowsKernel rows_kernel_add(bool add) {
   return add ? &k_grad_rows<GT, YT, E, true> : &k_grad_rows<GT, YT, E, false>;
 }
-template <int GT, int E>
-RowsKernel rows_kernel_to(int yt, bool add) {
-  return yt == ZQ_F32   ? rows_kernel_add<GT, ZQ_F32, E>(add)
-         : yt == ZQ_F16 ? rows_kernel_add<GT, ZQ_F16, E>(add)
-                        : rows_kernel_add<GT, ZQ_BF16, E>(add);
+// columns of a piece: 16 bytes of the result (1 column where rows are shorter than 8)
+template <int YT>
+constexpr int piece_of() {
+  return 16 / dt_size<YT>();
 }
-template <int E>
-RowsKernel rows_kernel(int gt, int yt, bool add) {
-  return gt == ZQ_F32   ? rows_kernel_to<ZQ_F32, E>(yt, add)
-         : gt == ZQ_F16 ? rows_kernel_to<ZQ_F16, E>(yt, add)
-                        : rows_kernel_to<ZQ_BF16, E>(yt, add);
+template <int GT, int YT>
+RowsKernel rows_kernel_for(bool short_rows, bool add) {
+  return short_rows ? rows_kernel_add<GT, YT, 1>(add) : rows_kernel_add<GT, YT, piece_of<YT>()>(add);
+}
+template <int GT>
+RowsKernel rows_kernel_to(int yt, bool short_rows, bool add) {
+  return yt == ZQ_F32   ? rows_kernel_for<GT, ZQ_F32>(short_rows, add)
+         : yt == ZQ_F16 ? rows_kernel_for<GT, ZQ_F16>(short_rows, add)
+                        : rows_kernel_for<GT, ZQ_BF16>(short_rows, add);
+}
+RowsKernel rows_kernel(int gt, int yt, bool short_rows, bool add) {
+  return gt == ZQ_F32   ? rows_kernel_to<ZQ_F32>(yt, short_rows, add)
+         : gt == ZQ_F16 ? rows_kernel_to<ZQ_F16>(yt, short_rows, add)
+                        : rows_kernel_to<ZQ_BF16>(yt, short_rows, add);
 }
 
 constexpr int64_t kMaxRow = 1 << 24;  // elements of a table row
@@ -386,27 +509,43 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
   char* ws = static_cast<char*>(workspace);
   int* start = reinterpret_cast<int*>(ws);
   int* order = reinterpret_cast<int*>(ws + start_bytes(V));
-  float* parts = reinterpret_cast<float*>(ws + start_bytes(V) + order_bytes(T));
-  const int E = D < 8 ? 1 : 8;
-  const int64_t C = (D + E - 1) / E, cols = (C + kEmbedThreads - 1) / kEmbedThreads;
-  // rows of a sorting workgroup: a power of two that gives about 256 of them
-  int range = 1, bits = 0;
-  while (range < kMaxRange && (int64_t)range * 256 < V) range *= 2, ++bits;
-  const int64_t sorts = (V + range - 1) / range, segs = T / kPart;
-  const int64_t grid = grid_for(V * C, kEmbedThreads);
-  if (grid == 0 || segs * cols > kMaxGrid) return ZQ_E_SIZE;
+  float* sums = reinterpret_cast<float*>(ws + start_bytes(V) + order_bytes(T));
+  // waves of a row: 64 pieces each
+  struct Split {
+    int64_t C, per;
+    unsigned grid(int64_t rows) const { return (unsigned)grid_for(rows * per, kEmbedThreads / 64); }
+  };
+  auto split = [&](int E) {
+    const int64_t C = (D + E - 1) / E;
+    return Split{C, (C + 63) / 64};
+  };
+  const bool short_rows = D < 8;
+  const Split rs = split(short_rows ? 1 : wt == ZQ_F32 ? 4 : 8), ps = split(short_rows ? 1 : 8);
+  const int64_t segs = T / kPart;
+  if (rs.grid(V) == 0 || ps.grid(segs) == 0) return ZQ_E_SIZE;
+  // Sorting workgroups: ranges of 512 rows, times parts of the tokens.  Every
+  // workgroup reads all ids (about T ranges parts 4e-7 us), while the parts share out
+  // the work on the tokens of a range that most tokens fall into (T / parts 6e-4 us):
+  // the least sum is at the square root of 1,700 / ranges.
+  const int64_t ranges = (V + kMaxRange - 1) / kMaxRange;
+  int parts = 1;
+  while (parts < 16 && (int64_t)(parts + 1) * 1024 <= T && (2 * parts + 1) * (2 * parts + 1) * ranges < 4 * 1700) ++parts;
+  const int64_t sorts = ranges * parts;
+  if (sorts > kMaxGrid) return ZQ_E_SIZE;
 
   hipStream_t st = static_cast<hipStream_t>(stream);
-  int rc = launch_grid(&k_sort_ids, dim3((unsigned)sorts), kSortThreads, kSortWaves * range * 4, st, ids, it == ZQ_I64, (int)T,
-                      V, range, bits, start, order);
+  int rc = it == ZQ_I64 ? launch(&k_sort_ids<int64_t>, (unsigned)sorts, kSortThreads, st,
+                                 static_cast<const int64_t*>(ids), (int)T, V, parts, start, order)
+                        : launch(&k_sort_ids<int32_t>, (unsigned)sorts, kSortThreads, st,
+                                 static_cast<const int32_t*>(ids), (int)T, V, parts, start, order);
   if (rc != ZQ_OK) return rc;
   if (segs > 0) {
-    rc = launch(E == 8 ? parts_kernel<8>(gt) : parts_kernel<1>(gt), (unsigned)(segs * cols), kEmbedThreads, st, ids,
-                it == ZQ_I64, dy, start, order, V, D, (int)C, (int)cols, parts);
+    rc = launch(short_rows ? parts_kernel<1>(gt) : parts_kernel<8>(gt), ps.grid(segs), kEmbedThreads, st, ids,
+                it == ZQ_I64, dy, start, order, segs, V, D, (int)ps.C, (int)ps.per, 1.0 / (double)ps.per, sums);
     if (rc != ZQ_OK) return rc;
   }
-  return launch(E == 8 ? rows_kernel<8>(gt, wt, accumulate != 0) : rows_kernel<1>(gt, wt, accumulate != 0),
-                (unsigned)grid, kEmbedThreads, st, dy, start, order, parts, V, D, (int)C, 1.0 / (double)C, scale, dw);
+  return launch(rows_kernel(gt, wt, short_rows, accumulate != 0), rs.grid(V), kEmbedThreads, st, dy, start, order, sums,
+                V, D, (int)rs.C, (int)rs.per, 1.0 / (double)rs.per, scale, dw);
 }
 
 }  // extern "C"

@@ -59,9 +59,9 @@ __host__ __device__ constexpr int64_t chunk_elems(int type) {
   return type == kInt4 ? 2 * kChunkBytes : type == ZQ_F32 ? kChunkBytes / 4 : kChunkBytes / 2;
 }
 
-// Table: the counter of finished workgroups, their sums, the entries of the norm,
-// the entries of clipping (an INT4 shard clipped in place is its scales there).
-constexpr int64_t kSumsAt = 64, kEntriesAt = kSumsAt + 8 * kNormGroups;
+// Table: the workgroups' sums, the entries of the norm, the entries of clipping (an
+// INT4 shard clipped in place is its scales there).
+constexpr int64_t kSumsAt = 0, kEntriesAt = kSumsAt + 8 * kNormGroups;
 __host__ __device__ inline int64_t clip_at(int entries) { return kEntriesAt + (int64_t)entries * (int64_t)sizeof(Entry); }
 
 // index of the entry that holds chunk c (every thread gets it)
@@ -76,48 +76,79 @@ __device__ __forceinline__ int find_entry(const Entry* entries, int count, int64
   return found;
 }
 
+// Loads in flight: a thread issues those of kSteps pieces (16 bytes each, the
+// workgroup's 4 KiB apart) before it uses the first.
+constexpr int kSteps = 4;
+
 template <int DT>
 __device__ __forceinline__ double sum_squares(const Entry& en, int64_t e0, int64_t e1) {
-  constexpr int E = 16 / dt_size<DT>();
-  double a = 0.0;
-  int64_t i = e0 + (int64_t)threadIdx.x * E;
-  for (; i + E <= e1; i += kNormThreads * E) {
+  constexpr int E = 16 / dt_size<DT>(), STEP = kNormThreads * E;
+  double a = 0.0, b = 0.0;
+  auto add = [&](const uint32_t(&w)[4]) {
     float v[E];
-    if constexpr (DT == ZQ_F32) {
-      load_elems<DT, 4>(en.data, i, v);
-    } else {
-      load_elems<DT, 8>(en.data, i, v);
-    }
+    widen<DT>(w, v);
 #pragma unroll
-    for (int k = 0; k < E; ++k) a = __builtin_fma((double)v[k], (double)v[k], a);
+    for (int k = 0; k < E; k += 2) {
+      a = __builtin_fma((double)v[k], (double)v[k], a);
+      b = __builtin_fma((double)v[k + 1], (double)v[k + 1], b);
+    }
+  };
+  int64_t i = e0 + (int64_t)threadIdx.x * E;
+  for (; i + (kSteps - 1) * STEP + E <= e1; i += kSteps * STEP) {
+    uint32_t w[kSteps][4];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) load_words_any<true>(en.data + (i + u * STEP) * dt_size<DT>(), w[u]);
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) add(w[u]);
+  }
+  for (; i + E <= e1; i += STEP) {
+    uint32_t w[4];
+    load_words_any<true>(en.data + i * dt_size<DT>(), w);
+    add(w);
   }
   for (; i < e1; ++i) {  // one thread: the elements of the last, short piece
     float v[1];
     load_elems<DT, 1>(en.data, i, v);
     a = __builtin_fma((double)v[0], (double)v[0], a);
   }
-  return a;
+  return a + b;
 }
 
 // 32 codes a thread and step: within one block, as blocks are multiples of 32
 __device__ __forceinline__ double sum_squares_int4(const Entry& en, int64_t e0, int64_t e1) {
+  constexpr int E = 32, STEP = kNormThreads * E;
   double a = 0.0;
-  for (int64_t i = e0 + (int64_t)threadIdx.x * 32; i < e1; i += kNormThreads * 32) {
+  auto add = [&](const uint32_t(&w)[4], float scale) {
+    int q2 = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q2 = __builtin_amdgcn_sdot8((int)w[k], (int)w[k], q2, false);
+    const double s = (double)scale;
+    a = __builtin_fma(s * s, (double)q2, a);
+  };
+  int64_t i = e0 + (int64_t)threadIdx.x * E;
+  for (; i + (kSteps - 1) * STEP + E <= e1; i += kSteps * STEP) {
+    uint32_t w[kSteps][4];
+    float s[kSteps];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      load_words_any<true>(en.data + (i + u * STEP) / 2, w[u]);
+      s[u] = en.scales[(i + u * STEP) >> en.lgB];
+    }
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) add(w[u], s[u]);
+  }
+  for (; i < e1; i += STEP) {
     uint32_t w[4] = {0u, 0u, 0u, 0u};
     const char* p = en.data + i / 2;
-    if (i + 32 <= e1) {
-      load_words_any<false>(p, w);
+    if (i + E <= e1) {
+      load_words_any<true>(p, w);
     } else {
       for (int k = 0; i + k < e1; ++k) {
         const uint32_t q = (uint8_t)p[k / 2] >> (4 * (k & 1)) & 15u;
         w[k / 8] |= q << (4 * (k % 8));
       }
     }
-    int q2 = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) q2 = __builtin_amdgcn_sdot8((int)w[k], (int)w[k], q2, false);
-    const double s = (double)en.scales[i >> en.lgB];
-    a = __builtin_fma(s * s, (double)q2, a);
+    add(w, en.scales[i >> en.lgB]);
   }
   return a;
 }
@@ -143,7 +174,6 @@ __global__ void __launch_bounds__(kNormThreads)
     k_grad_norm(char* __restrict__ table, int count, int64_t chunks, float scale, float* __restrict__ norm) {
   const Entry* entries = reinterpret_cast<const Entry*>(table + kEntriesAt);
   double* sums = reinterpret_cast<double*>(table + kSumsAt);
-  unsigned* counter = reinterpret_cast<unsigned*>(table);
   const int64_t W = gridDim.x, w = blockIdx.x;
   int64_t c = w * chunks / W;
   const int64_t c1 = (w + 1) * chunks / W;
@@ -169,35 +199,50 @@ __global__ void __launch_bounds__(kNormThreads)
     }
   }
   a = group_sum(a);
-  // the last workgroup to finish adds the sums, in the order of the workgroups
-  __shared__ bool last;
-  if (threadIdx.x == 0) {
-    __hip_atomic_store(&sums[w], a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)W - 1;
-  }
-  __syncthreads();
-  if (!last) return;
-  double t = 0.0;
-  for (int64_t k = threadIdx.x; k < W; k += kNormThreads)
-    t += __hip_atomic_load(&sums[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  t = group_sum(t);
-  if (threadIdx.x == 0) {
-    *norm = (float)(fabs((double)scale) * sqrt(t));
-    __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next call
-  }
+  if (threadIdx.x != 0) return;
+  if (W == 1) *norm = (float)(fabs((double)scale) * sqrt(a));
+  else sums[w] = a;
 }
 
+// the workgroups' sums, in their order
+__global__ void __launch_bounds__(kNormThreads)
+    k_norm_finish(const char* __restrict__ table, int groups, float scale, float* __restrict__ norm) {
+  const double* sums = reinterpret_cast<const double*>(table + kSumsAt);
+  double v[kNormGroups / kNormThreads], t = 0.0;
+#pragma unroll
+  for (int u = 0; u < kNormGroups / kNormThreads; ++u) {
+    const int k = u * kNormThreads + threadIdx.x;
+    v[u] = k < groups ? sums[k] : 0.0;
+  }
+#pragma unroll
+  for (int u = 0; u < kNormGroups / kNormThreads; ++u) t += v[u];
+  t = group_sum(t);
+  if (threadIdx.x == 0) *norm = (float)(fabs((double)scale) * sqrt(t));
+}
+
+// E elements a thread and step: 16 bytes written, or read where that is less
 template <int DT, int YT>
 __device__ __forceinline__ void scale_elems(const Entry& en, int64_t e0, int64_t e1, float c) {
-  constexpr int E = 16 / dt_size<DT>();
-  int64_t i = e0 + (int64_t)threadIdx.x * E;
-  for (; i + E <= e1; i += kNormThreads * E) {
+  constexpr int E = DT == ZQ_F32 || YT == ZQ_F32 ? 4 : 8, STEP = kNormThreads * E, N = E * dt_size<DT>() / 4;
+  auto put = [&](int64_t i, const uint32_t(&w)[N]) {
     float v[E];
-    if constexpr (DT == ZQ_F32) load_elems<DT, 4>(en.data, i, v);
-    else load_elems<DT, 8>(en.data, i, v);
+    widen<DT>(w, v);
 #pragma unroll
     for (int k = 0; k < E; ++k) v[k] = v[k] * c;
     store_elems<YT, E>(en.out, i, v);
+  };
+  int64_t i = e0 + (int64_t)threadIdx.x * E;
+  for (; i + (kSteps - 1) * STEP + E <= e1; i += kSteps * STEP) {
+    uint32_t w[kSteps][N];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) load_words_any<false>(en.data + (i + u * STEP) * dt_size<DT>(), w[u]);
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) put(i + u * STEP, w[u]);
+  }
+  for (; i + E <= e1; i += STEP) {
+    uint32_t w[N];
+    load_words_any<false>(en.data + i * dt_size<DT>(), w);
+    put(i, w);
   }
   for (; i < e1; ++i) {
     float v[1];
@@ -210,16 +255,50 @@ __device__ __forceinline__ void scale_elems(const Entry& en, int64_t e0, int64_t
 // the INT4 shard dequantised with its scales times c: fl(q * fl(s * c))
 template <int YT>
 __device__ __forceinline__ void scale_int4(const Entry& en, int64_t e0, int64_t e1, float c) {
-  constexpr int E = 8;
-  int64_t i = e0 + (int64_t)threadIdx.x * E;
-  for (; i + E <= e1; i += kNormThreads * E) {
-    uint32_t w[1];
-    load_words_any<false>(en.data + i / 2, w);
-    const float s = en.scales[i >> en.lgB] * c;
+  constexpr int E = 8, STEP = kNormThreads * E;
+  const int lane = threadIdx.x & 63;
+  auto put = [&](int64_t i, uint32_t w, float scale) {
+    const float s = scale * c;
     float v[E];
 #pragma unroll
-    for (int k = 0; k < E; ++k) v[k] = (float)((int32_t)(w[0] << (28 - 4 * k)) >> 28) * s;
+    for (int k = 0; k < E; ++k) v[k] = (float)((int32_t)(w << (28 - 4 * k)) >> 28) * s;
     store_elems<YT, E>(en.out, i, v);
+  };
+  // the wave's 512 elements at once: binary32 ones in two halves of 256, in which
+  // lane l stores the four of word l / 2, so that a store covers whole lines
+  auto put_wave = [&](int64_t i, uint32_t w, float scale) {
+    if constexpr (YT == ZQ_F32) {
+      const float s = scale * c;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int from = 32 * h + (lane >> 1);
+        const uint32_t q = __shfl(w, from) >> (16 * (lane & 1));
+        const float t = __shfl(s, from);
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = (float)((int32_t)(q << (28 - 4 * k)) >> 28) * t;
+        store_elems<YT, 4>(en.out, i - 8 * lane + 256 * h + 4 * lane, v);
+      }
+    } else {
+      put(i, w, scale);
+    }
+  };
+  int64_t i = e0 + (int64_t)threadIdx.x * E;
+  for (; i - lane * E + (kSteps - 1) * STEP + 64 * E <= e1; i += kSteps * STEP) {  // whole waves
+    uint32_t w[kSteps][1];
+    float s[kSteps];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      load_words_any<false>(en.data + (i + u * STEP) / 2, w[u]);
+      s[u] = en.scales[(i + u * STEP) >> en.lgB];
+    }
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) put_wave(i + u * STEP, w[u][0], s[u]);
+  }
+  for (; i + E <= e1; i += STEP) {
+    uint32_t w[1];
+    load_words_any<false>(en.data + i / 2, w);
+    put(i, w[0], en.scales[i >> en.lgB]);
   }
   for (; i < e1; ++i) {
     const uint32_t q = (uint8_t)en.data[i / 2] >> (4 * (i & 1));
@@ -370,7 +449,10 @@ int plan_table(const zq_grad* grads, int32_t count, zq_grad_plan* plan) {
   return ZQ_OK;
 }
 
-unsigned groups_for(int64_t chunks) { return (unsigned)(chunks < kNormGroups ? (chunks < 1 ? 1 : chunks) : kNormGroups); }
+// A workgroup a chunk, up to kNormGroups of them.
+unsigned groups_for(int64_t chunks) {
+  return (unsigned)(chunks < kNormGroups ? (chunks < 1 ? 1 : chunks) : kNormGroups);
+}
 
 }  // namespace
 }  // namespace zq
@@ -408,8 +490,15 @@ int zq_grad_plan_table(const zq_grad* grads, const zq_grad_plan* plan, void* hos
 int zq_grad_norm(const zq_grad_plan* plan, void* table, float scale, float* norm, void* stream) {
   if (!plan || !table || !norm) return ZQ_E_NULL;
   if (!aligned(table, 16) || !aligned(norm, 4)) return ZQ_E_ALIGN;
-  return launch(&k_grad_norm, groups_for(plan->norm_chunks), kNormThreads, static_cast<hipStream_t>(stream),
-                static_cast<char*>(table), plan->count, plan->norm_chunks, scale, norm);
+  // One launch up to 4 chunks (one workgroup reads them), else a second one that
+  // adds the workgroups' sums.  (The last workgroup to finish adding them in the same
+  // launch needs a release and an acquire by every workgroup: 60 us for 2,048.)
+  const unsigned groups = plan->norm_chunks <= 4 ? 1u : groups_for(plan->norm_chunks);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int rc = launch(&k_grad_norm, groups, kNormThreads, st, static_cast<char*>(table), plan->count,
+                        plan->norm_chunks, scale, norm);
+  if (rc != ZQ_OK || groups == 1) return rc;
+  return launch(&k_norm_finish, 1u, kNormThreads, st, static_cast<const char*>(table), (int)groups, scale, norm);
 }
 
 int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm, float max_norm, float scale,
