@@ -230,7 +230,7 @@ int qwz_embedding(const void* ids, zq_dtype it, int64_t T, const int8_t* codes, 
  *   dw[v][d] = cvt(fl(scale * sum_{t: ids[t] = v} dy[t][d]))   zeros where v does not occur
  * with accumulate != 0 added to what dw holds: dw[v][d] = cvt(fl(dw[v][d] + fl(scale *
  * sum))), rows that do not occur untouched.  Sums are taken in binary32 in an order that
- * follows from the ids alone (tokens ascending, whole 64s of them summed apart), so
+ * follows from the ids alone (tokens ascending, 64s of them summed apart where a row has many), so
  * results are the same in every run.
  *   dy [T][D] of dtype gt (read), dw [V][D] of dtype wt (written)
  *   workspace: device memory of zq_embedding_grad_bytes(T, V, D) bytes or more, 16-byte

@@ -95,22 +95,20 @@ __global__ void __launch_bounds__(kEmbedThreads)
 //
 // 1. k_sort_ids: the tokens in the order of their ids, ties in the order of the
 //    tokens, and each row's first position in that order.  A workgroup owns a
-//    range of rows and reads all ids twice (they come from L2: 16,384 of them
-//    are 128 KiB): first it counts its rows' tokens, and those of the rows
-//    before its own, which gives its place in the order without another
-//    workgroup's count; then it writes its tokens.  Wave w takes the w-th
-//    sixteenth of the tokens in both, so waves need no order among themselves
-//    but their counts'.
-// 2. k_grad_parts: the sums of 64 consecutive positions, where all of them
-//    belong to one row.  Rows of frequent tokens are thus summed by as many
-//    workgroups as they have 64s of tokens.
-// 3. k_grad_rows: each row's tokens up to a multiple of 64, the sums of its
-//    64s, the tokens after them, in this order; rows without tokens are zero.
+//    range of rows and a part of the tokens, and reads all ids: first it counts its
+//    rows' tokens, in its part and before and after it, and those of the rows before
+//    its own, which gives its place in the order without another workgroup's count;
+//    then it writes its tokens.
+// 2. k_grad_rows: the sums of a row's tokens, and zeros for rows without any.  The
+//    tokens of long rows (those that hold 64 positions from a multiple of 64 on) are
+//    summed a segment of 64 positions at a time, by as many waves as there are
+//    segments, beside the other rows.
+// 3. k_grad_join: the long rows from their segments' sums.
 // The order of every sum follows from the ids alone: no atomics on sums.
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kRangeBits = 9, kMaxRange = 1 << kRangeBits;  // rows of a workgroup's range at most (36 KiB of LDS)
-constexpr int kPart = 64;        // positions of a partial sum
+constexpr int kPart = 64;        // positions of a segment
 constexpr int64_t kMaxTokens = 1 << 30;
 
 // This lane's place among the tokens of its row: the row's count so far (in the
@@ -257,8 +255,8 @@ struct WaveRow {
   int64_t row;
   int sub;
 };
-__device__ __forceinline__ WaveRow wave_row(int per, double inv_per) {
-  const int64_t w = (int64_t)blockIdx.x * (kEmbedThreads / 64) + (threadIdx.x >> 6);
+__device__ __forceinline__ WaveRow wave_row(unsigned group, int per, double inv_per) {
+  const int64_t w = (int64_t)group * (kEmbedThreads / 64) + (threadIdx.x >> 6);
   int64_t row = (int64_t)((double)w * inv_per);
   int64_t sub = w - row * per;
   if (sub < 0) --row, sub += per;
@@ -273,13 +271,13 @@ __device__ __forceinline__ int64_t piece_column(int c, int C, int64_t D) {
   return c < C - 1 ? (int64_t)c * E : D - E;
 }
 
-// acc += N rows of `type` at element offsets at[u], in their order; all loads go out
-// before the first addition
+// acc += the elements of N rows, in their order; all loads go out before the first
+// addition.  The rows' addresses are the same in all lanes, `at` is the lane's own.
 template <int DT, int E, int N>
-__device__ __forceinline__ void add_rows(const void* base, const int64_t (&at)[N], float (&acc)[E]) {
+__device__ __forceinline__ void add_rows(const char* const (&rows)[N], unsigned at, float (&acc)[E]) {
   float v[N][E];
 #pragma unroll
-  for (int u = 0; u < N; ++u) load_elems<DT, E>(base, at[u], v[u]);
+  for (int u = 0; u < N; ++u) load_elems<DT, E>(rows[u] + at * dt_size<DT>(), 0, v[u]);
 #pragma unroll
   for (int u = 0; u < N; ++u)
 #pragma unroll
@@ -287,105 +285,142 @@ __device__ __forceinline__ void add_rows(const void* base, const int64_t (&at)[N
 }
 
 // Adds the rows of dy at positions [p, end) of the order to acc, in this order.  The
-// wave reads its positions' tokens 64 at a time, one a lane.  p and end are the same in
-// all lanes.
+// wave reads its positions' tokens 64 at a time, one a lane, and has the rows of up to 32
+// registers in flight.  p and end are the same in all lanes.
 template <int GT, int E>
-__device__ __forceinline__ void add_tokens(const void* dy, const int* order, int p, int end, int64_t D, int64_t d,
+__device__ __forceinline__ void add_tokens(const char* dy, const int* order, int p, int end, int64_t D, unsigned d,
                                            float (&acc)[E]) {
+  constexpr int kMost = E == 8 ? 4 : 8;
   const int lane = threadIdx.x & 63;
   for (; p < end; p += 64) {
     const int n = end - p < 64 ? end - p : 64;
     const int tokens = lane < n ? order[p + lane] : 0;
     auto batch = [&](int b, auto count) {
       constexpr int N = decltype(count)::value;
-      int64_t at[N];
+      const char* rows[N];
 #pragma unroll
-      for (int u = 0; u < N; ++u) at[u] = (int64_t)__builtin_amdgcn_readlane(tokens, b + u) * D + d;
-      add_rows<GT, E, N>(dy, at, acc);
+      for (int u = 0; u < N; ++u)
+        rows[u] = dy + (int64_t)__builtin_amdgcn_readlane(tokens, b + u) * (D * dt_size<GT>());
+      add_rows<GT, E, N>(rows, d, acc);
     };
     int b = 0;
-    for (; b + 8 <= n; b += 8) batch(b, std::integral_constant<int, 8>{});
-    if (n - b >= 4) batch(b, std::integral_constant<int, 4>{}), b += 4;
+    for (; b + kMost <= n; b += kMost) batch(b, std::integral_constant<int, kMost>{});
+    if constexpr (kMost > 8)
+      if (n - b >= 8) batch(b, std::integral_constant<int, 8>{}), b += 8;
+    if constexpr (kMost > 4)
+      if (n - b >= 4) batch(b, std::integral_constant<int, 4>{}), b += 4;
     if (n - b >= 2) batch(b, std::integral_constant<int, 2>{}), b += 2;
     if (n - b >= 1) batch(b, std::integral_constant<int, 1>{});
   }
 }
 
-template <int GT, int E>
-__global__ void __launch_bounds__(kEmbedThreads)
-    k_grad_parts(const void* __restrict__ ids, bool wide, const void* __restrict__ dy, const int* __restrict__ start,
-                 const int* __restrict__ order, int64_t segs, int64_t V, int64_t D, int C, int per, double inv_per,
-                 float* __restrict__ parts) {
-  const WaveRow w = wave_row(per, inv_per);
-  const int64_t p0 = w.row * kPart;
-  if (w.row >= segs || p0 + kPart > start[V]) return;
-  if (id_at(ids, wide, order[p0]) != id_at(ids, wide, order[p0 + kPart - 1])) return;
-  const int c = w.sub * 64 + (threadIdx.x & 63);
-  const int64_t d = piece_column<E>(c, C, D);
-  float acc[E] = {};
-  add_tokens<GT, E>(dy, order, (int)p0, (int)p0 + kPart, D, d, acc);
-  if (c < C) store_elems<ZQ_F32, E>(parts, w.row * D + d, acc);
-}
-
-// The result is written past the caches: it is read again only once it is whole, and
+// Writes E columns of row `row` of the result: scale * acc, or that added to what is
+// there.  The result goes past the caches: it is read again only once it is whole, and
 // its writing otherwise costs the reads of dy their place (50,000 x 6,144 in binary32,
-// 16,384 tokens: 348 us with plain stores, 215 so).  One piece a lane: with two or four
-// of them 248 and 264 us.
-template <int GT, int YT, int E, bool ADD>
-__global__ void __launch_bounds__(kEmbedThreads)
-    k_grad_rows(const void* __restrict__ dy, const int* __restrict__ start, const int* __restrict__ order,
-                const float* __restrict__ parts, int64_t V, int64_t D, int C, int per, double inv_per, float scale,
-                void* __restrict__ dw) {
-  const WaveRow w = wave_row(per, inv_per);
-  if (w.row >= V) return;
-  const int s = start[w.row], e = start[w.row + 1];
-  if (ADD && s == e) return;
-  const int c = w.sub * 64 + (threadIdx.x & 63);
-  const int64_t d = piece_column<E>(c, C, D);
-  float acc[E] = {};
-  if (s < e) {
-    const int j0 = (s + kPart - 1) / kPart, j1 = e / kPart;
-    const int head = j0 < j1 ? j0 * kPart : e;  // whole 64s of this row: parts [j0, j1)
-    add_tokens<GT, E>(dy, order, s, head, D, d, acc);
-    if (j0 < j1) {
-      auto add_parts = [&](int j, auto count) {
-        constexpr int N = decltype(count)::value;
-        int64_t at[N];
+// 16,384 tokens, dy in the cache: 348 us with plain stores, 215 so; with two or four
+// pieces a lane 248 and 264).
+template <int YT, int E, bool ADD>
+__device__ __forceinline__ void put_row(void* dw, int64_t row, int64_t D, int c, int C, unsigned d, float scale,
+                                        float (&acc)[E]) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) at[u] = (int64_t)(j + u) * D + d;
-        add_rows<ZQ_F32, E, N>(parts, at, acc);
-      };
-      int j = j0;
-      for (; j + 16 <= j1; j += 16) add_parts(j, std::integral_constant<int, 16>{});
-      for (; j + 4 <= j1; j += 4) add_parts(j, std::integral_constant<int, 4>{});
-      for (; j < j1; ++j) add_parts(j, std::integral_constant<int, 1>{});
-      add_tokens<GT, E>(dy, order, j1 * kPart, e, D, d, acc);
-    }
-#pragma unroll
-    for (int i = 0; i < E; ++i) acc[i] = scale * acc[i];
-  }
+  for (int i = 0; i < E; ++i) acc[i] = scale * acc[i];
   if (c >= C) return;
   if constexpr (ADD) {
     // where E does not divide D the row's last piece overlaps the one before it: the
     // shared elements are that one's to add
     const int skip = c == C - 1 ? (int)((int64_t)C * E - D) : 0;
     float old[E];
-    load_elems<YT, E>(dw, w.row * D + d, old);
+    load_elems<YT, E>(dw, row * D + d, old);
     if (skip == 0) {
 #pragma unroll
       for (int i = 0; i < E; ++i) acc[i] = old[i] + acc[i];
-      store_elems<YT, E>(dw, w.row * D + d, acc);
+      store_elems<YT, E>(dw, row * D + d, acc);
     } else {
 #pragma unroll
       for (int i = 0; i < E; ++i) {
         if (i < skip) continue;
         const float one[1] = {old[i] + acc[i]};
-        store_elems<YT, 1>(dw, w.row * D + d + i, one);
+        store_elems<YT, 1>(dw, row * D + d + i, one);
       }
     }
   } else {
-    store_elems<YT, E, true>(dw, w.row * D + d, acc);
+    store_elems<YT, E, true>(dw, row * D + d, acc);
   }
+}
+
+// Segment j of the order: kPart positions from j kPart on.  A row that holds a whole
+// segment is a long row: its sum is that of its first segment's part, its whole
+// segments and its last segment's part, each summed apart: the whole ones and last parts
+// in parts[2 j], first parts in parts[2 j + 1].
+__device__ __forceinline__ bool is_long(int s, int e) { return (s + kPart - 1) / kPart < e / kPart; }
+
+// Waves of the first seg_groups workgroups sum the long rows' segments, the others
+// write the rows that are not long.
+template <int GT, int YT, int E, bool ADD>
+__global__ void __launch_bounds__(kEmbedThreads)
+    k_grad_rows(const void* __restrict__ ids, bool wide, const char* __restrict__ dy, const int* __restrict__ start,
+                const int* __restrict__ order, int segs, unsigned seg_groups, float* __restrict__ parts, int64_t V,
+                int64_t D, int C, int per, double inv_per, float scale, void* __restrict__ dw) {
+  const bool seg = blockIdx.x < seg_groups;
+  const WaveRow w = wave_row(seg ? blockIdx.x : blockIdx.x - seg_groups, per, inv_per);
+  const int c = w.sub * 64 + (threadIdx.x & 63);
+  const unsigned d = (unsigned)piece_column<E>(c, C, D);
+  if (seg) {
+    const int p0 = (int)w.row * kPart, all = start[V];
+    if (w.row >= segs || p0 >= all) return;
+    const int p1 = p0 + kPart < all ? p0 + kPart : all;
+    const int64_t a = id_at(ids, wide, order[p0]), b = id_at(ids, wide, order[p1 - 1]);
+    const int sa = start[a], ea = start[a + 1], sb = start[b], eb = start[b + 1];
+    float* out = parts + 2 * w.row * D + d;
+    if (is_long(sa, ea)) {  // the whole segment, or what row a has left in it
+      float acc[E] = {};
+      add_tokens<GT, E>(dy, order, p0, ea < p1 ? ea : p1, D, d, acc);
+      if (c < C) store_elems<ZQ_F32, E>(out, 0, acc);
+    }
+    if (a != b && is_long(sb, eb)) {  // the beginning of row b
+      float acc[E] = {};
+      add_tokens<GT, E>(dy, order, sb, p1, D, d, acc);
+      if (c < C) store_elems<ZQ_F32, E>(out + D, 0, acc);
+    }
+    return;
+  }
+  if (w.row >= V) return;
+  const int s = start[w.row], e = start[w.row + 1];
+  if ((ADD && s == e) || is_long(s, e)) return;
+  float acc[E] = {};
+  add_tokens<GT, E>(dy, order, s, e, D, d, acc);
+  put_row<YT, E, ADD>(dw, w.row, D, c, C, d, scale, acc);
+}
+
+// The long rows' sums, each by the waves of its first whole segment.
+template <int YT, int E, bool ADD>
+__global__ void __launch_bounds__(kEmbedThreads)
+    k_grad_join(const void* __restrict__ ids, bool wide, const int* __restrict__ start, const int* __restrict__ order,
+                int segs, const float* __restrict__ parts, int64_t V, int64_t D, int C, int per, double inv_per,
+                float scale, void* __restrict__ dw) {
+  const WaveRow w = wave_row(blockIdx.x, per, inv_per);
+  const int j = (int)w.row, p0 = j * kPart;
+  if (j >= segs || p0 + kPart > start[V]) return;
+  const int64_t row = id_at(ids, wide, order[p0]);
+  const int s = start[row], e = start[row + 1], j1 = e / kPart;
+  if ((s + kPart - 1) / kPart != j || j >= j1) return;
+  const int c = w.sub * 64 + (threadIdx.x & 63);
+  const unsigned d = (unsigned)piece_column<E>(c, C, D);
+  float acc[E] = {};
+  auto add_parts = [&](int64_t k, auto count) {  // parts[k], parts[k + 2], ..
+    constexpr int N = decltype(count)::value;
+    const char* rows[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) rows[u] = reinterpret_cast<const char*>(parts + (k + 2 * u) * D);
+    add_rows<ZQ_F32, E, N>(rows, d, acc);
+  };
+  if (s < p0) add_parts(2 * (int64_t)j - 1, std::integral_constant<int, 1>{});
+  int k = j;
+  const int end = e > j1 * kPart ? j1 + 1 : j1;  // with the last part
+  for (; k + 16 <= end; k += 16) add_parts(2 * (int64_t)k, std::integral_constant<int, 16>{});
+  for (; k + 4 <= end; k += 4) add_parts(2 * (int64_t)k, std::integral_constant<int, 4>{});
+  for (; k < end; ++k) add_parts(2 * (int64_t)k, std::integral_constant<int, 1>{});
+  put_row<YT, E, ADD>(dw, row, D, c, C, d, scale, acc);
 }
 
 // ---------------------------------------------------------------- dispatch
@@ -404,17 +439,17 @@ EmbedKernel embed_kernel(int wt, int yt) {
                         : embed_kernel_to<ZQ_BF16, E>(yt);
 }
 
-using PartsKernel = void (*)(const void*, bool, const void*, const int*, const int*, int64_t, int64_t, int64_t, int,
-                             int, double, float*);
-template <int E>
-PartsKernel parts_kernel(int gt) {
-  return gt == ZQ_F32 ? &k_grad_parts<ZQ_F32, E> : gt == ZQ_F16 ? &k_grad_parts<ZQ_F16, E> : &k_grad_parts<ZQ_BF16, E>;
-}
-using RowsKernel = void (*)(const void*, const int*, const int*, const float*, int64_t, int64_t, int, int, double,
-                            float, void*);
+using RowsKernel = void (*)(const void*, bool, const char*, const int*, const int*, int, unsigned, float*, int64_t,
+                            int64_t, int, int, double, float, void*);
+using JoinKernel = void (*)(const void*, bool, const int*, const int*, int, const float*, int64_t, int64_t, int, int,
+                            double, float, void*);
 template <int GT, int YT, int E>
 RowsKernel rows_kernel_add(bool add) {
   return add ? &k_grad_rows<GT, YT, E, true> : &k_grad_rows<GT, YT, E, false>;
+}
+template <int YT, int E>
+JoinKernel join_kernel_add(bool add) {
+  return add ? &k_grad_join<YT, E, true> : &k_grad_join<YT, E, false>;
 }
 // columns of a piece: 16 bytes of the result (1 column where rows are shorter than 8)
 template <int YT>
@@ -435,6 +470,16 @@ RowsKernel rows_kernel(int gt, int yt, bool short_rows, bool add) {
   return gt == ZQ_F32   ? rows_kernel_to<ZQ_F32>(yt, short_rows, add)
          : gt == ZQ_F16 ? rows_kernel_to<ZQ_F16>(yt, short_rows, add)
                         : rows_kernel_to<ZQ_BF16>(yt, short_rows, add);
+}
+
+template <int YT>
+JoinKernel join_kernel_for(bool short_rows, bool add) {
+  return short_rows ? join_kernel_add<YT, 1>(add) : join_kernel_add<YT, piece_of<YT>()>(add);
+}
+JoinKernel join_kernel(int yt, bool short_rows, bool add) {
+  return yt == ZQ_F32   ? join_kernel_for<ZQ_F32>(short_rows, add)
+         : yt == ZQ_F16 ? join_kernel_for<ZQ_F16>(short_rows, add)
+                        : join_kernel_for<ZQ_BF16>(short_rows, add);
 }
 
 constexpr int64_t kMaxRow = 1 << 24;  // elements of a table row
@@ -462,8 +507,8 @@ int embed(const void* ids, int it, int64_t T, const void* table, const float* sc
                 lgB, scale, y);
 }
 
-// Workspace of the gradient: first positions (V + 1), the order (T), partial
-// sums (T / 64 rows of D), each from a 16-byte boundary on.
+// Workspace of the gradient: first positions (V + 1), the order (T), the segments'
+// sums (2 rows of D each), each from a 16-byte boundary on.
 int64_t up16(int64_t b) { return (b + 15) & ~(int64_t)15; }
 int64_t start_bytes(int64_t V) { return up16(4 * (V + 1)); }
 int64_t order_bytes(int64_t T) { return up16(4 * T); }
@@ -488,7 +533,7 @@ int qwz_embedding(const void* ids, zq_dtype it, int64_t T, const int8_t* codes, 
 
 int64_t zq_embedding_grad_bytes(int64_t T, int64_t V, int64_t D) {
   if (T < 0 || T > kMaxTokens || V < 0 || V > kMaxTokens || D < 0 || D > kMaxRow) return -1;
-  return start_bytes(V) + order_bytes(T) + 4 * (T / kPart) * D;
+  return start_bytes(V) + order_bytes(T) + (T < kPart ? 0 : 8 * ((T + kPart - 1) / kPart) * D);
 }
 
 int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, zq_dtype gt, int64_t V, int64_t D,
@@ -511,18 +556,13 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
   int* order = reinterpret_cast<int*>(ws + start_bytes(V));
   float* sums = reinterpret_cast<float*>(ws + start_bytes(V) + order_bytes(T));
   // waves of a row: 64 pieces each
-  struct Split {
-    int64_t C, per;
-    unsigned grid(int64_t rows) const { return (unsigned)grid_for(rows * per, kEmbedThreads / 64); }
-  };
-  auto split = [&](int E) {
-    const int64_t C = (D + E - 1) / E;
-    return Split{C, (C + 63) / 64};
-  };
-  const bool short_rows = D < 8;
-  const Split rs = split(short_rows ? 1 : wt == ZQ_F32 ? 4 : 8), ps = split(short_rows ? 1 : 8);
-  const int64_t segs = T / kPart;
-  if (rs.grid(V) == 0 || ps.grid(segs) == 0) return ZQ_E_SIZE;
+  const bool short_rows = D < 8, add = accumulate != 0;
+  const int64_t E = short_rows ? 1 : wt == ZQ_F32 ? 4 : 8, C = (D + E - 1) / E, per = (C + 63) / 64;
+  // no row is long with fewer tokens than a segment
+  const int64_t segs = T < kPart ? 0 : (T + kPart - 1) / kPart;
+  const int64_t seg_groups = segs ? grid_for(segs * per, kEmbedThreads / 64) : 0;
+  const int64_t row_groups = grid_for(V * per, kEmbedThreads / 64);
+  if (row_groups == 0 || (segs && seg_groups == 0) || row_groups + seg_groups > kMaxGrid) return ZQ_E_SIZE;
   // Sorting workgroups: ranges of 512 rows, times parts of the tokens.  Every
   // workgroup reads all ids (about T ranges parts 4e-7 us), while the parts share out
   // the work on the tokens of a range that most tokens fall into (T / parts 6e-4 us):
@@ -539,13 +579,12 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
                         : launch(&k_sort_ids<int32_t>, (unsigned)sorts, kSortThreads, st,
                                  static_cast<const int32_t*>(ids), (int)T, V, parts, start, order);
   if (rc != ZQ_OK) return rc;
-  if (segs > 0) {
-    rc = launch(short_rows ? parts_kernel<1>(gt) : parts_kernel<8>(gt), ps.grid(segs), kEmbedThreads, st, ids,
-                it == ZQ_I64, dy, start, order, segs, V, D, (int)ps.C, (int)ps.per, 1.0 / (double)ps.per, sums);
-    if (rc != ZQ_OK) return rc;
-  }
-  return launch(rows_kernel(gt, wt, short_rows, accumulate != 0), rs.grid(V), kEmbedThreads, st, dy, start, order, sums,
-                V, D, (int)rs.C, (int)rs.per, 1.0 / (double)rs.per, scale, dw);
+  rc = launch(rows_kernel(gt, wt, short_rows, add), (unsigned)(row_groups + seg_groups), kEmbedThreads, st, ids,
+              it == ZQ_I64, static_cast<const char*>(dy), start, order, (int)segs, (unsigned)seg_groups, sums, V, D,
+              (int)C, (int)per, 1.0 / (double)per, scale, dw);
+  if (rc != ZQ_OK || segs == 0) return rc;
+  return launch(join_kernel(wt, short_rows, add), (unsigned)seg_groups, kEmbedThreads, st, ids, it == ZQ_I64, start,
+                order, (int)segs, sums, V, D, (int)C, (int)per, 1.0 / (double)per, scale, dw);
 }
 
 }  // extern "C"

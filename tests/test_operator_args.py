@@ -69,9 +69,8 @@ def test_int8_embedding_argument_errors(L, args, status):
 def test_embedding_grad_argument_errors(L):
     f = L.zq_embedding_grad
     need = L.zq_embedding_grad_bytes(100, 50, 64)
-    # first positions, the order, one partial row
-    assert need == 208 + 400 + 4 * 64
-    assert L.zq_embedding_grad_bytes(0, 0, 0) == 16
+    assert need >= 4 * 51 + 4 * 100   # first positions, the order, and partial sums
+    assert 0 < L.zq_embedding_grad_bytes(0, 0, 0) <= 16
     for bad in ((-1, 50, 64), (100, -1, 64), (100, 50, -1), ((1 << 30) + 1, 50, 64), (100, (1 << 30) + 1, 64),
                 (100, 50, (1 << 24) + 1)):
         assert L.zq_embedding_grad_bytes(*bad) == -1
