@@ -310,7 +310,7 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
  *   y       [M][N] float row-major (written)
  * K a multiple of 64, at most 2^22 (ZQ_E_SIZE); M, N >= 0 arbitrary; K = 0 writes
  * zeros.  x and packed 16-byte aligned, scales and y 4-byte aligned.  Meant for few
- * rows: the weight is read again for every 64 rows of x. */
+ * rows: the weight is read again for every 32 rows of x. */
 int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, const float* scales, int64_t M, int64_t N,
                          int64_t K, int32_t block, float* y, void* stream);
 

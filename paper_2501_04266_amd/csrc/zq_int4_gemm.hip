@@ -43,20 +43,12 @@ __device__ __forceinline__ f32x4_t mfma(u32x4 a, u32x4 b, f32x4_t c) {
                                                   0, 0);
 }
 
-// q / 16 for the low nibble (two's complement) of byte BYTE of w: one
-// instruction, exact
+// q / 16 for the low nibble (two's complement) of byte BYTE of w: one instruction,
+// exact.  The builtin and no inline asm: the compiler has to know of these writes to
+// keep them off the registers that an MFMA still in flight will write.
 template <int BYTE>
 __device__ __forceinline__ float sixteenth(uint32_t w) {
-  float f;
-  if constexpr (BYTE == 0)
-    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(f) : "v"(w));
-  else if constexpr (BYTE == 1)
-    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(f) : "v"(w));
-  else if constexpr (BYTE == 2)
-    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(f) : "v"(w));
-  else
-    asm("v_cvt_off_f32_i4_sdwa %0, %1 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(f) : "v"(w));
-  return f;
+  return __builtin_amdgcn_cvt_off_f32_i4((int)(w >> (8 * BYTE) & 0xffu));
 }
 
 // two values of at most 8 significant bits as XT, packed low-first (exact)
@@ -69,7 +61,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // the 8 codes of a word as an MFMA operand, in sixteenths
 template <int XT>
 __device__ __forceinline__ u32x4 operand(uint32_t w) {
-  const uint32_t h = w >> 4;
+  uint32_t h = w >> 4;
+  asm("" : "+v"(h));  // one shift: left to itself the compiler takes each upper nibble out of w by one of its own
   return u32x4{pack2<XT>(sixteenth<0>(w), sixteenth<0>(h)), pack2<XT>(sixteenth<1>(w), sixteenth<1>(h)),
                pack2<XT>(sixteenth<2>(w), sixteenth<2>(h)), pack2<XT>(sixteenth<3>(w), sixteenth<3>(h))};
 }
@@ -85,158 +78,381 @@ __device__ __forceinline__ u32x4 transposed(u32x4 w) {
   return u32x4{p[0], p[1], q[0], q[1]};
 }
 
-// MT, NT: 16-row tiles of x and of the weight; W: waves; D: pieces (256 codes of
-// each of the wave's rows) in flight; G: codes summed before their scale is
-// applied (they lie in one block).  `range`: codes of K whose x is in LDS at a
-// time, those of `per` rounds of the waves, or all of K.
-template <int XT, int MT, int NT, int W, int D, int G>
-__global__ void __launch_bounds__(64 * W)
-    k_int4_rows(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
-                int64_t M, int64_t N, int64_t K, int lgB, int range, int per,
-                float* __restrict__ y) {
-  extern __shared__ u32x4 lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * (16 * NT), m0 = (int64_t)blockIdx.y * (16 * MT);
-  const int rows = (int)(N - n0 < 16 * NT ? N - n0 : 16 * NT);
-  const int mrows = (int)(M - m0 < 16 * MT ? M - m0 : 16 * MT);
-  const int kk = (int)K;
-  const __amdgpu_buffer_rsrc_t wres = __builtin_amdgcn_make_buffer_rsrc(
-      (void*)(packed + n0 * (K / 2)), (short)0, rows * (kk / 2), kRawBuffer);
-  const int64_t s0 = (n0 * K) >> lgB, s1 = ((n0 + rows) * K + (1 << lgB) - 1) >> lgB;
-  const __amdgpu_buffer_rsrc_t sres =
-      __builtin_amdgcn_make_buffer_rsrc((void*)(scales + s0), (short)0, (int)((s1 - s0) * 4), kRawBuffer);
-  const uint32_t fbase = (uint32_t)((n0 * K) & ((1ll << lgB) - 1));  // of the first row in its block
+constexpr int kWaves = 8;
+constexpr int kPiece = 256;  // codes of a weight row that a wave takes at a time: a 128-byte line
+constexpr int kGemmThreads = 64 * kWaves;
+__host__ __device__ inline int pieces_of(int64_t K) { return K == 0 ? 1 : (int)((K + kPiece - 1) / kPiece); }
 
-  constexpr int SC = 256 / G;  // scales of a row's piece
-  const int pieces = (kk + 255) / 256;
-  u32x4 wr[D][NT][2];
-  float sr[D][NT][SC];
-  auto load = [&](int d, int piece) {
-    const int k0 = piece * 256;
+// The weight as a wave streams it.  A load takes half a piece (128 codes) of 16 rows:
+// lane l has 32 codes of row l / 4, from code 32 (l % 4) on, so that 4 lanes in a row
+// read 64 bytes in a row (with a row for each of 16 lanes in a row the same loads take
+// four times as long in the address unit), and the scale of those codes, which lie in
+// one block.
+// Slots of D pieces are in flight; load() fills one with the next piece: the waves
+// share out a group's K, and a workgroup's groups of 16 NT rows are gridDim.x apart.
+template <int NT, int D>
+struct Weight {
+  u32x4 codes[D][NT][2];
+  float scale[D][NT][2];
+
+  const uint8_t* packed;
+  const float* scales;
+  int64_t N, K;
+  int lgB, groups, rounds, group, round;
+  // of the group being loaded
+  __amdgpu_buffer_rsrc_t wres, sres;
+  uint32_t first;  // the first row's place in its block
+  uint32_t row0;   // this lane's first code, in the group's flat order
+
+  __device__ __forceinline__ Weight(const uint8_t* p, const float* s, int64_t n, int64_t k, int lg, int gr)
+      : packed(p), scales(s), N(n), K(k), lgB(lg), groups(gr),
+        rounds((pieces_of(k) + kWaves - 1) / kWaves), group(blockIdx.x), round(0) {
+    const int lane = threadIdx.x & 63;
+    row0 = (uint32_t)(lane >> 2) * (uint32_t)k + 32u * (lane & 3);
+    turn_to_group();
+  }
+  __device__ __forceinline__ void turn_to_group() {
+    // past the last group: empty resources; the same loads go out, so that the number
+    // of loads in flight is known at every wait, and bring zeros
+    const bool any = group < groups;
+    const int64_t n0 = any ? (int64_t)group * (16 * NT) : 0;
+    const int rows = any ? (int)(N - n0 < 16 * NT ? N - n0 : 16 * NT) : 0;
+    wres = __builtin_amdgcn_make_buffer_rsrc((void*)(packed + n0 * (K / 2)), (short)0, rows * (int)(K / 2), kRawBuffer);
+    const int64_t f0 = n0 * K, s0 = f0 >> lgB, s1 = (f0 + (int64_t)rows * K + (1 << lgB) - 1) >> lgB;
+    sres = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + s0), (short)0, (int)((s1 - s0) * 4), kRawBuffer);
+    first = (uint32_t)(f0 & ((1ll << lgB) - 1));
+  }
+  __device__ __forceinline__ void load(int d) {
+    const uint32_t k0 = (uint32_t)((round * kWaves + (int)(threadIdx.x >> 6)) * kPiece);
+    const uint32_t left = (uint32_t)K > k0 ? (uint32_t)K - k0 : 0u, mine = 32u * (threadIdx.x & 3);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int row = 16 * t + c;
+      // rows past the last are outside the resources: zeros
+      const uint32_t f = row0 + 16 * t * (uint32_t)K + k0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int k = k0 + 128 * h + 32 * g;
-        const uint32_t off = k < kk && row < rows ? (uint32_t)(row * (kk / 2) + k / 2) : kOutside;
-        wr[d][t][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wres, (int)off, 0, 0));
+        const bool in = mine + 128u * h < left;
+        const uint32_t off = in ? f / 2 + 64u * h : kOutside;
+        codes[d][t][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wres, (int)off, 0, 0));
+        const uint32_t soff = in ? ((f + first + 128u * h) >> lgB) * 4 : kOutside;
+        scale[d][t][h] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sres, (int)soff, 0, 0));
       }
+    }
+    if (++round == rounds) {
+      round = 0;
+      group += gridDim.x;
+      turn_to_group();
+    }
+  }
+};
+
+// x rows m0 .. m0 + mrows in LDS, whole; elements past K, which meet zero codes, are
+// zeros.  Rows are an odd number of 16-byte units long, so that lanes that read one
+// column of 8 rows meet distinct banks.  `between` runs once the first loads are out.
+// What there is no place for goes to the unit after the last row: a load whose result
+// is left in its registers makes the compiler wait for all loads wherever these are
+// used again, in each turn of the loops below.
+__device__ __forceinline__ int x_stride(int64_t K) { return pieces_of(K) * (kPiece / 8) + 1; }
+template <typename F>
+__device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres, int mrows, int64_t K, F between) {
+  constexpr int U = 4;
+  const int stride = x_stride(K), kk = (int)K;
+  const unsigned row = (unsigned)stride - 1, units = (unsigned)mrows * row;  // 16-byte units: below 2^14
+  u32x4 v[U];
+  auto read = [&](unsigned at) {
 #pragma unroll
-      for (int q = 0; q < SC; ++q) {
-        const int k = k0 + G * q;
-        const uint32_t off =
-            k < kk && row < rows ? (((uint32_t)row * (uint32_t)kk + (uint32_t)k + fbase) >> lgB) * 4 : kOutside;
-        sr[d][t][q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sres, (int)off, 0, 0));
-      }
+    for (int u = 0; u < U; ++u) {
+      const unsigned i = at + u * kGemmThreads, m = i / row, k = 8 * (i - m * row);
+      const uint32_t off = i < units && k < (unsigned)kk ? (m * (unsigned)kk + k) * 2 : kOutside;
+      v[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xres, (int)off, 0, 0));
     }
   };
-  // x[m0 ..][k0 .. k0 + range) into LDS, rows 16 bytes apart beyond their length
-  // (so that 8 lanes' 16-byte reads of one column fall into distinct banks)
-  const int stride = range / 8 + 1;
-  auto stage = [&](int k0) {
-    const int len = (kk - k0 < range ? kk - k0 : range) / 8;
-    for (int m = wave; m < mrows; m += W) {
-      const uint16_t* row = x + (m0 + m) * K + k0;
-      for (int i = lane; i < len; i += 64) lds[m * stride + i] = *reinterpret_cast<const u32x4*>(row + 8 * i);
-      // what the last, half step of K multiplies with zero codes
-      if (len * 8 < range)
-        for (int i = len + lane; i < len + 32 && i < range / 8; i += 64) lds[m * stride + i] = u32x4{0u, 0u, 0u, 0u};
+  auto write = [&](unsigned at) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const unsigned i = at + u * kGemmThreads;
+      lds[i < units ? i + i / row : (unsigned)(mrows * stride)] = v[u];
     }
+  };
+  read(threadIdx.x);
+  between();
+  write(threadIdx.x);
+  for (unsigned at = threadIdx.x + U * kGemmThreads; at < units; at += U * kGemmThreads) {
+    read(at);
+    write(at);
+  }
+}
+
+// ---------------------------------------------------------------- up to 4 rows of x
+//
+// The transposed words of a half piece make 4 operands w of 16 columns: column c is row
+// 4 w + c / 4 of the weight and its codes 32 (c % 4) .. + 32.  The other operand holds x
+// for each of the four ranges of codes: row 4 s + m is x[m] at 32 s .. + 32.  Of the
+// product's 16 x 16 sums those with s = c % 4 count, a quarter: lane (c, g) has them,
+// elements m, where g = c % 4.  The matrix cores have room for that (16 cycles of 250),
+// and no lane needs codes that another one loaded, beyond the transposition.  Each column
+// has one scale, whatever the block size.
+template <int XT, int MR, int D>
+__global__ void __launch_bounds__(kGemmThreads)
+    k_int4_few(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
+               int64_t M, int64_t N, int64_t K, int lgB, int groups, float* __restrict__ y) {
+  extern __shared__ u32x4 lds[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int kk = (int)K, mrows = (int)M, stride = x_stride(K);
+  Weight<1, D> wt(packed, scales, N, K, lgB, groups);
+  const int rounds = wt.rounds;
+  stage_x(lds, __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * kk * 2, kRawBuffer), mrows, K, [&] {
+#pragma unroll
+    for (int d = 0; d < D; ++d) wt.load(d);
+  });
+  // rows past M repeat the last one; their sums are not stored
+  const u32x4* const xat = lds + ((lane & 3) < mrows ? lane & 3 : mrows - 1) * stride + 4 * (c >> 2) + g;
+
+  float acc[4][MR];
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int m = 0; m < MR; ++m) acc[w][m] = 0.0f;
+  auto multiply = [&](int d, int h, int k0) {
+    const u32x4 xf = xat[k0 / 8];
+    const u32x4 words = transposed(wt.codes[d][0][h]);
+    // the scales of lane 16 w + c for every g
+    const uint32_t sv = f2u(wt.scale[d][0][h]);
+    auto ab = __builtin_amdgcn_permlane32_swap(sv, sv, false, false);
+    auto s01 = __builtin_amdgcn_permlane16_swap(ab[0], ab[0], false, false);
+    auto s23 = __builtin_amdgcn_permlane16_swap(ab[1], ab[1], false, false);
+    const float s[4] = {u2f(s01[0]), u2f(s01[1]), u2f(s23[0]), u2f(s23[1])};
+    f32x4_t part[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) part[w] = mfma<XT>(xf, operand<XT>(words[w]), f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int m = 0; m < MR; ++m) acc[w][m] = __builtin_fmaf(part[w][m], s[w], acc[w][m]);
   };
 
-  f32x4_t acc[MT][NT];
+  float* const sums = reinterpret_cast<float*>(lds + mrows * stride);
+  constexpr int kOne = 4 * MR * 16;  // a wave's sums: of the four ranges, MR x 16 each
+  int group = blockIdx.x, round = 0, turn = 0;
+  auto finish = [&] {
+    float* const part = sums + turn * (kWaves * kOne);
+    if (g == (c & 3)) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
+      for (int m = 0; m < MR; ++m)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int w = 0; w < 4; ++w) part[wave * kOne + (g * MR + m) * 16 + 4 * w + (c >> 2)] = acc[w][m];
+    }
+    __syncthreads();
+    const int64_t n = (int64_t)group * 16 + (threadIdx.x & 15);
+    const int m = threadIdx.x >> 4;
+    if (m < mrows && n < N) {
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) v += part[w * kOne + s * MR * 16 + threadIdx.x];
+      y[m * N + n] = 16.0f * v;
+    }
+    turn ^= 1;  // the next group's sums go beside these, which may still be read
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int i = 0; i < MR; ++i) acc[w][i] = 0.0f;
+  };
+
+  __syncthreads();
+  // The D steps have one way out, after the last: with one after each the compiler
+  // waits for all loads in every turn.  Steps past the last group multiply zeros.
+  do {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      const int k0 = (round * kWaves + wave) * kPiece;
+      if (k0 < kk) multiply(d, 0, k0), multiply(d, 1, k0 + 128);
+      wt.load(d);
+      if (++round == rounds) {
+        if (group < groups) finish();
+        round = 0;
+        group += gridDim.x;
+      }
+    }
+  } while (group < groups);
+}
+
+// ---------------------------------------------------------------- more rows
+//
+// MT: 16-row tiles of x.  G: codes summed before their scale is applied (they lie in one
+// block).  The codes and scales go to the lanes that need them through LDS (one
+// permutation of the wave): lane (c, g) takes the 32 codes of row c from 32 g on.
+// XL: all of x is in LDS, from before the first group on.  Otherwise it is read from
+// the caches, half a piece ahead, permuted like the codes; a group then has several
+// tiles, which share it.
+template <int XT, int MT, int NT, int D, int G, bool XL>
+__global__ void __launch_bounds__(kGemmThreads)
+    k_int4_rows(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
+                int64_t M, int64_t N, int64_t K, int lgB, int groups, float* __restrict__ y) {
+  extern __shared__ u32x4 lds[];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
+  const int mrows = (int)(M - m0 < 16 * MT ? M - m0 : 16 * MT);
+  const int kk = (int)K, stride = x_stride(K);
+  const __amdgpu_buffer_rsrc_t xres =
+      __builtin_amdgcn_make_buffer_rsrc((void*)(x + m0 * K), (short)0, mrows * kk * 2, kRawBuffer);
+  Weight<NT, D> wt(packed, scales, N, K, lgB, groups);
+  const int rounds = wt.rounds;
+  auto from = [&](int source, uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * source, (int)v);
+  };
+
+  // Lane (c, g) multiplies in MFMA j of a half piece: elements 32 g + 8 j on, where the
+  // codes may stay as they are loaded; else, with the words transposed, 32 j + 8 g on.
+  constexpr bool kAsLoaded = G == 128 && XL;
+  constexpr int XG = kAsLoaded ? 32 : 8, XJ = kAsLoaded ? 8 : 32;
   int xrow[MT];  // rows past M repeat the last one; their sums are not stored
 #pragma unroll
-  for (int i = 0; i < MT; ++i) xrow[i] = (16 * i + c < mrows ? 16 * i + c : mrows - 1) * stride + g;
-
-  auto multiply = [&](int d, int k0) {  // k0: in the staged range
+  for (int i = 0; i < MT; ++i) xrow[i] = 16 * i + c < mrows ? 16 * i + c : mrows - 1;
+  u32x4 xv[XL ? 1 : 2][MT][4];
+  auto read_x = [&](int buf, int k0) {  // the half piece from k0 on; lane l: row l / 4, 8 elements at 32 j + 8 (l % 4)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      u32x4 wt[NT];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) wt[t] = transposed(wr[d][t][h]);
-      f32x4_t part[MT][NT];
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        u32x4 xf[MT];
+        const int k = k0 + 32 * j + 8 * (lane & 3);
+        const uint32_t off = k < kk ? ((uint32_t)(16 * i + (lane >> 2)) * (uint32_t)kk + (uint32_t)k) * 2 : kOutside;
+        xv[buf][i][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xres, (int)off, 0, 0));
+      }
+  };
+  auto load_all = [&] {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) xf[i] = lds[xrow[i] + (k0 + 128 * h + 32 * j) / 8];
+    for (int d = 0; d < D; ++d) wt.load(d);
+  };
+  if constexpr (XL) stage_x(lds, xres, mrows, K, load_all);
+  else load_all();
+
+  f32x4_t acc[MT][NT];
+  auto clear = [&] {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  };
+  auto multiply = [&](int d, int h, int k0) {  // half h of the piece in slot d; k0: its first code
+    u32x4 xf[MT][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (XL) {
+          xf[i][j] = lds[xrow[i] * stride + (k0 + XG * g + XJ * j) / 8];
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) xf[i][j][q] = from(4 * c + g, xv[h][i][j][q]);
+        }
+      }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      u32x4 words;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) words[q] = from(4 * c + g, wt.codes[d][t][h][q]);
+      if constexpr (!kAsLoaded) words = transposed(words);
+      float s[128 / G];
+#pragma unroll
+      for (int q = 0; q < 128 / G; ++q) s[q] = u2f(from(4 * c + q * (G / 32), f2u(wt.scale[d][t][h])));
+      f32x4_t part[MT];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
         const bool first = (32 * j) % G == 0, done = (32 * j + 32) % G == 0;
+        const u32x4 wf = operand<XT>(words[j]);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const u32x4 wf = operand<XT>(wt[t][j]);
+        for (int i = 0; i < MT; ++i) {
+          part[i] = mfma<XT>(xf[i][j], wf, first ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part[i]);
+          if (done) {
 #pragma unroll
-          for (int i = 0; i < MT; ++i) {
-            part[i][t] = mfma<XT>(xf[i], wf, first ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part[i][t]);
-            if (done) {
-              const float s = sr[d][t][(128 * h + 32 * j) / G];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[i][t][e] = __builtin_fmaf(part[i][t][e], s, acc[i][t][e]);
-            }
+            for (int e = 0; e < 4; ++e) acc[i][t][e] = __builtin_fmaf(part[i][e], s[32 * j / G], acc[i][t][e]);
           }
         }
       }
     }
   };
 
-  const int rounds = (pieces + W - 1) / W;
+  // ---- the waves' sums, in the order of the waves; D element e of lane (c, g): row
+  // 4 g + e of x, weight row c
+  float* const sums = reinterpret_cast<float*>(lds + (XL ? mrows * stride : 0));
+  int group = blockIdx.x, round = 0, turn = 0;
+  auto finish = [&] {
+    float* const part = sums + turn * (kWaves * mrows * 16 * NT);
 #pragma unroll
-  for (int d = 0; d < D; ++d) load(d, d * W + wave);
-  for (int r0 = 0; r0 < rounds; r0 += D) {
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int m = 16 * i + 4 * g + e;
+        if (m < mrows)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) part[(wave * mrows + m) * (16 * NT) + 16 * t + c] = acc[i][t][e];
+      }
+    __syncthreads();
+    const int64_t n0 = (int64_t)group * (16 * NT);
+    for (int o = threadIdx.x; o < mrows * 16 * NT; o += kGemmThreads) {
+      const int m = o / (16 * NT), n = o % (16 * NT);
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) v += part[w * mrows * (16 * NT) + o];
+      if (n0 + n < N) y[(m0 + m) * N + n0 + n] = 16.0f * v;
+    }
+    turn ^= 1;  // the next group's sums go beside these, which may still be read
+    clear();
+  };
+
+  clear();
+  if constexpr (XL) __syncthreads();
+  else read_x(0, wave * kPiece);
+  // The D steps have one way out, after the last: with one after each the compiler
+  // waits for all loads in every turn.  Steps past the last group multiply zeros.
+  do {
 #pragma unroll
     for (int d = 0; d < D; ++d) {
-      const int r = r0 + d;
-      if (r < rounds) {
-        if (r % per == 0) {
-          if (r > 0) __syncthreads();
-          stage(r * W * 256);
-          __syncthreads();
-        }
-        const int k0 = (r * W + wave) * 256;
-        if (k0 < kk) multiply(d, k0 - r / per * per * (256 * W));
-        load(d, (r + D) * W + wave);
+      const int k0 = (round * kWaves + wave) * kPiece;
+      if constexpr (XL) {
+        if (k0 < kk) multiply(d, 0, k0), multiply(d, 1, k0 + 128);
+      } else {
+        read_x(1, k0 + 128);
+        if (k0 < kk) multiply(d, 0, k0);
+        read_x(0, round + 1 == rounds ? wave * kPiece : k0 + kWaves * kPiece);
+        if (k0 < kk) multiply(d, 1, k0 + 128);
+      }
+      wt.load(d);
+      if (++round == rounds) {
+        if (group < groups) finish();
+        round = 0;
+        group += gridDim.x;
       }
     }
-  }
-
-  // the waves' sums, in the order of the waves; D element e of lane (c, g): row
-  // 4 g + e of x, weight row c
-  __syncthreads();
-  float* part = reinterpret_cast<float*>(lds);
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        part[((wave * MT + i) * 16 + 4 * g + e) * (16 * NT) + 16 * t + c] = acc[i][t][e];
-  __syncthreads();
-  for (int o = threadIdx.x; o < 256 * MT * NT; o += 64 * W) {
-    const int m = o / (16 * NT), n = o % (16 * NT);
-    if (m >= mrows || n >= rows) continue;
-    float v = 0.0f;
-    for (int w = 0; w < W; ++w) v += part[(w * MT * 16 + m) * (16 * NT) + n];
-    y[(m0 + m) * N + n0 + n] = 16.0f * v;
-  }
+  } while (group < groups);
 }
 
-using Int4Kernel = void (*)(const uint16_t*, const uint8_t*, const float*, int64_t, int64_t, int64_t, int, int, int,
-                            float*);
+using Int4Kernel = void (*)(const uint16_t*, const uint8_t*, const float*, int64_t, int64_t, int64_t, int, int, float*);
 
-template <int XT, int MT, int NT, int W, int D>
+template <int XT, int MT, int NT, int D, bool XL>
 Int4Kernel int4_kernel_for(int G) {
-  return G == 128  ? &k_int4_rows<XT, MT, NT, W, D, 128>
-         : G == 64 ? &k_int4_rows<XT, MT, NT, W, D, 64>
-                   : &k_int4_rows<XT, MT, NT, W, D, 32>;
+  return G == 128  ? &k_int4_rows<XT, MT, NT, D, 128, XL>
+         : G == 64 ? &k_int4_rows<XT, MT, NT, D, 64, XL>
+                   : &k_int4_rows<XT, MT, NT, D, 32, XL>;
+}
+template <int XT>
+Int4Kernel int4_few_kernel(int64_t M) {
+  return M == 1 ? &k_int4_few<XT, 1, 3> : M == 2 ? &k_int4_few<XT, 2, 3> : &k_int4_few<XT, 4, 3>;
+}
+template <int XT>
+Int4Kernel int4_kernel(bool xl, int MT, int NT, int G) {
+  if (xl) return MT == 1 ? int4_kernel_for<XT, 1, 1, 3, true>(G) : int4_kernel_for<XT, 2, 1, 3, true>(G);
+  if (MT == 1)
+    return NT == 1   ? int4_kernel_for<XT, 1, 1, 3, false>(G)
+           : NT == 2 ? int4_kernel_for<XT, 1, 2, 2, false>(G)
+                     : int4_kernel_for<XT, 1, 4, 2, false>(G);
+  return NT == 1 ? int4_kernel_for<XT, 2, 1, 3, false>(G) : int4_kernel_for<XT, 2, 2, 2, false>(G);
 }
 
 constexpr int64_t kInt4MaxK = 1 << 22;  // 64 rows of codes stay below 2^31 bytes
-constexpr int kInt4Waves = 8;
+constexpr int64_t kLds = 160 * 1024, kCus = 256;
 
 }  // namespace
 }  // namespace zq
@@ -255,22 +471,32 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
   if (any_overlap({{y, 4 * M * N}}, {{x, 2 * M * K}, {packed, N * K / 2}, {scales, 4 * num_scales(N * K, block)}}))
     return ZQ_E_ALIAS;
 
-  constexpr int W = kInt4Waves;
-  const int MT = 1, NT = 1;
+  const int MT = M <= 16 ? 1 : 2;
+  const int64_t mrows = M < 16 * MT ? M : 16 * MT, mgroups = (M + 16 * MT - 1) / (16 * MT);
+  // codes under one scale: 128 from a multiple of 128 on lie in one block only where
+  // rows start at multiples of 128
   const int G = block >= 128 && K % 128 == 0 ? 128 : block >= 64 ? 64 : 32;
-  const int64_t mrows = M < 16 * MT ? M : 16 * MT;
-  // all of K in LDS where it fits 64 KiB, else whole rounds of it
-  int64_t range = (K + 255) / 256 * 256, per = (K + 256 * W - 1) / (256 * W);
-  if (mrows * (2 * range + 16) > 65536) {
-    per = (65536 / mrows - 16) / 2 / (256 * W);
-    if (per < 1) per = 1;
-    range = per * 256 * W;
+  // x in LDS where it leaves room for the waves' sums
+  const int few = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 0;
+  const int64_t pieces = pieces_of(K), xbytes = mrows * (pieces * (kPiece / 8) + 1) * 16;
+  const int64_t sbytes = 2 * kWaves * 16 * 4 * (few ? 4 * few : mrows);
+  const bool xl = xbytes + sbytes <= kLds;
+  const int64_t tiles = (N + 15) / 16;
+  const int NT = xl || tiles <= 512 ? 1 : tiles <= 1024 || MT == 2 ? 2 : 4;
+  const int64_t groups = (tiles + NT - 1) / NT;
+  if (groups > kMaxGrid || mgroups > 65535) return ZQ_E_SIZE;
+  const int64_t lds = xl ? xbytes + sbytes : 2 * kWaves * 16 * 4 * mrows * NT;
+  // x in LDS: as many workgroups as are resident at once, each with as many groups as
+  // the others
+  int64_t grid = groups;
+  if (xl) {
+    const int64_t room = kLds / lds > 2 ? 2 : kLds / lds;
+    const int64_t turns = (groups + room * kCus - 1) / (room * kCus);
+    grid = (groups + turns - 1) / turns;
   }
-  int64_t lds = mrows * (2 * range + 16);
-  if (lds < 4 * 256 * MT * NT * W) lds = 4 * 256 * MT * NT * W;
-  const int64_t grid = (N + 16 * NT - 1) / (16 * NT), gridm = (M + 16 * MT - 1) / (16 * MT);
-  if (grid > kMaxGrid || gridm > 65535) return ZQ_E_SIZE;
-  Int4Kernel k = xt == ZQ_BF16 ? int4_kernel_for<ZQ_BF16, 1, 1, W, 3>(G) : int4_kernel_for<ZQ_F16, 1, 1, W, 3>(G);
-  return launch_grid(k, dim3((unsigned)grid, (unsigned)gridm), 64u * W, (unsigned)lds, static_cast<hipStream_t>(stream),
-                   static_cast<const uint16_t*>(x), packed, scales, M, N, K, lgB, (int)range, (int)per, y);
+  const Int4Kernel k = xl && few ? (xt == ZQ_BF16 ? int4_few_kernel<ZQ_BF16>(M) : int4_few_kernel<ZQ_F16>(M))
+                                 : (xt == ZQ_BF16 ? int4_kernel<ZQ_BF16>(xl, MT, NT, G) : int4_kernel<ZQ_F16>(xl, MT, NT, G));
+  return launch_grid(k, dim3((unsigned)grid, (unsigned)mgroups), (unsigned)kGemmThreads, (unsigned)lds,
+                     static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(x), packed, scales, M, N, K, lgB,
+                     (int)groups, y);
 }
