@@ -87,9 +87,7 @@ __host__ __device__ inline int pieces_of(int64_t K) { return K == 0 ? 1 : (int)(
 // lane l has 32 codes of row l / 4, from code 32 (l % 4) on, so that 4 lanes in a row
 // read 64 bytes in a row (with a row for each of 16 lanes in a row the same loads take
 // four times as long in the address unit), and the scale of those codes, which lie in
-// one block.
-// Slots of D pieces are in flight; load() fills one with the next piece: the waves
-// share out a group's K, and a workgroup's groups of 16 NT rows are gridDim.x apart.
+// one block.  Slots of D pieces of NT x 16 rows are in flight.
 template <int NT, int D>
 struct Weight {
   u32x4 codes[D][NT][2];
@@ -98,20 +96,20 @@ struct Weight {
   const uint8_t* packed;
   const float* scales;
   int64_t N, K;
-  int lgB, groups, rounds, group, round;
+  int lgB, groups;
   // of the group being loaded
   __amdgpu_buffer_rsrc_t wres, sres;
-  uint32_t first;  // the first row's place in its block
+  uint32_t first;  // its first row's place in its block
   uint32_t row0;   // this lane's first code, in the group's flat order
+  int end;         // pieces that start before this have codes for the lane
 
   __device__ __forceinline__ Weight(const uint8_t* p, const float* s, int64_t n, int64_t k, int lg, int gr)
-      : packed(p), scales(s), N(n), K(k), lgB(lg), groups(gr),
-        rounds((pieces_of(k) + kWaves - 1) / kWaves), group(blockIdx.x), round(0) {
+      : packed(p), scales(s), N(n), K(k), lgB(lg), groups(gr) {
     const int lane = threadIdx.x & 63;
     row0 = (uint32_t)(lane >> 2) * (uint32_t)k + 32u * (lane & 3);
-    turn_to_group();
+    end = (int)k - 32 * (lane & 3);
   }
-  __device__ __forceinline__ void turn_to_group() {
+  __device__ __forceinline__ void turn_to(int group) {
     // past the last group: empty resources; the same loads go out, so that the number
     // of loads in flight is known at every wait, and bring zeros
     const bool any = group < groups;
@@ -122,26 +120,20 @@ struct Weight {
     sres = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + s0), (short)0, (int)((s1 - s0) * 4), kRawBuffer);
     first = (uint32_t)(f0 & ((1ll << lgB) - 1));
   }
-  __device__ __forceinline__ void load(int d) {
-    const uint32_t k0 = (uint32_t)((round * kWaves + (int)(threadIdx.x >> 6)) * kPiece);
-    const uint32_t left = (uint32_t)K > k0 ? (uint32_t)K - k0 : 0u, mine = 32u * (threadIdx.x & 3);
+  // the piece from code k0 of the group's rows on; rows past the last, and codes past K,
+  // are outside the resources: zeros
+  __device__ __forceinline__ void load(int d, uint32_t k0) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      // rows past the last are outside the resources: zeros
       const uint32_t f = row0 + 16 * t * (uint32_t)K + k0;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const bool in = mine + 128u * h < left;
+        const bool in = (int)k0 < end - 128 * h;
         const uint32_t off = in ? f / 2 + 64u * h : kOutside;
         codes[d][t][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wres, (int)off, 0, 0));
         const uint32_t soff = in ? ((f + first + 128u * h) >> lgB) * 4 : kOutside;
         scale[d][t][h] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sres, (int)soff, 0, 0));
       }
-    }
-    if (++round == rounds) {
-      round = 0;
-      group += gridDim.x;
-      turn_to_group();
     }
   }
 };
@@ -158,11 +150,15 @@ __device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres,
   constexpr int U = 4;
   const int stride = x_stride(K), kk = (int)K;
   const unsigned row = (unsigned)stride - 1, units = (unsigned)mrows * row;  // 16-byte units: below 2^14
+  // a unit's row: the quotient is a half over the row length or more away from the next
+  // whole number, the product off by 2^-23 of it
+  const float inv = 1.0f / (float)row;
+  auto row_of = [&](unsigned i) { return (unsigned)(((float)i + 0.5f) * inv); };
   u32x4 v[U];
   auto read = [&](unsigned at) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const unsigned i = at + u * kGemmThreads, m = i / row, k = 8 * (i - m * row);
+      const unsigned i = at + u * kGemmThreads, m = row_of(i), k = 8 * (i - m * row);
       const uint32_t off = i < units && k < (unsigned)kk ? (m * (unsigned)kk + k) * 2 : kOutside;
       v[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xres, (int)off, 0, 0));
     }
@@ -171,7 +167,7 @@ __device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres,
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const unsigned i = at + u * kGemmThreads;
-      lds[i < units ? i + i / row : (unsigned)(mrows * stride)] = v[u];
+      lds[i < units ? i + row_of(i) : (unsigned)(mrows * stride)] = v[u];
     }
   };
   read(threadIdx.x);
@@ -183,59 +179,83 @@ __device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres,
   }
 }
 
-// ---------------------------------------------------------------- up to 4 rows of x
+// ---------------------------------------------------------------- few rows of x
 //
 // The transposed words of a half piece make 4 operands w of 16 columns: column c is row
-// 4 w + c / 4 of the weight and its codes 32 (c % 4) .. + 32.  The other operand holds x
-// for each of the four ranges of codes: row 4 s + m is x[m] at 32 s .. + 32.  Of the
-// product's 16 x 16 sums those with s = c % 4 count, a quarter: lane (c, g) has them,
-// elements m, where g = c % 4.  The matrix cores have room for that (16 cycles of 250),
-// and no lane needs codes that another one loaded, beyond the transposition.  Each column
-// has one scale, whatever the block size.
+// 4 w + c / 4 of the weight and its codes 32 (c % 4) .. + 32.  The other operand holds 4
+// rows of x for each of the four ranges of codes: row 4 s + m is x[m] at 32 s .. + 32.  Of
+// the product's 16 x 16 sums those with s = c % 4 count, a quarter: lane (c, g) has them,
+// elements m, where g = c % 4.  The matrix cores have room for that (16 cycles of about
+// 150 per operand), and no lane needs codes that another one loaded, beyond the
+// transposition.  Each column has one scale, whatever the block size.
+// MR: rows of x, 1, 2 or a multiple of 4.
+__host__ __device__ constexpr int few_sums(int MR) { return 4 * MR * 16; }  // a wave's: MR x 16 of each range
+__host__ __device__ constexpr int few_buffers(int MR) { return MR <= 4 ? 2 : 1; }
 template <int XT, int MR, int D>
 __global__ void __launch_bounds__(kGemmThreads)
     k_int4_few(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
                int64_t M, int64_t N, int64_t K, int lgB, int groups, float* __restrict__ y) {
+  constexpr int MG = MR <= 4 ? 1 : MR / 4, MQ = MR < 4 ? MR : 4;
   extern __shared__ u32x4 lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15;
+  const int g = lane >> 4;
   const int kk = (int)K, mrows = (int)M, stride = x_stride(K);
+  const int rounds = (pieces_of(K) + kWaves - 1) / kWaves;
   Weight<1, D> wt(packed, scales, N, K, lgB, groups);
-  const int rounds = wt.rounds;
+  int load_group = blockIdx.x, load_round = 0;
+  wt.turn_to(load_group);
+  auto load = [&](int d) {
+    wt.load(d, (uint32_t)((load_round * kWaves + wave) * kPiece));
+    if (++load_round == rounds) load_round = 0, wt.turn_to(load_group += gridDim.x);
+  };
   stage_x(lds, __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * kk * 2, kRawBuffer), mrows, K, [&] {
 #pragma unroll
-    for (int d = 0; d < D; ++d) wt.load(d);
+    for (int d = 0; d < D; ++d) load(d);
   });
-  // rows past M repeat the last one; their sums are not stored
-  const u32x4* const xat = lds + ((lane & 3) < mrows ? lane & 3 : mrows - 1) * stride + 4 * (c >> 2) + g;
+  const u32x4* xat[MG];  // rows past M repeat the last one; their sums are not stored
+#pragma unroll
+  for (int q = 0; q < MG; ++q) {
+    const int m = 4 * q + (lane & 3);
+    xat[q] = lds + (m < mrows ? m : mrows - 1) * stride + 4 * (c >> 2) + g;
+  }
 
   float acc[4][MR];
-#pragma unroll
-  for (int w = 0; w < 4; ++w)
-#pragma unroll
-    for (int m = 0; m < MR; ++m) acc[w][m] = 0.0f;
-  auto multiply = [&](int d, int h, int k0) {
-    const u32x4 xf = xat[k0 / 8];
-    const u32x4 words = transposed(wt.codes[d][0][h]);
-    // the scales of lane 16 w + c for every g
-    const uint32_t sv = f2u(wt.scale[d][0][h]);
-    auto ab = __builtin_amdgcn_permlane32_swap(sv, sv, false, false);
-    auto s01 = __builtin_amdgcn_permlane16_swap(ab[0], ab[0], false, false);
-    auto s23 = __builtin_amdgcn_permlane16_swap(ab[1], ab[1], false, false);
-    const float s[4] = {u2f(s01[0]), u2f(s01[1]), u2f(s23[0]), u2f(s23[1])};
-    f32x4_t part[4];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) part[w] = mfma<XT>(xf, operand<XT>(words[w]), f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
+  auto clear = [&] {
 #pragma unroll
     for (int w = 0; w < 4; ++w)
 #pragma unroll
-      for (int m = 0; m < MR; ++m) acc[w][m] = __builtin_fmaf(part[w][m], s[w], acc[w][m]);
+      for (int m = 0; m < MR; ++m) acc[w][m] = 0.0f;
+  };
+  auto multiply = [&](int d, int h, int k0) {
+    u32x4 xf[MG];
+#pragma unroll
+    for (int q = 0; q < MG; ++q) xf[q] = xat[q][k0 / 8];
+    const u32x4 words = transposed(wt.codes[d][0][h]);
+    float s[4];  // the scale of lane 16 w + c
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      s[w] = u2f((uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * w + c), (int)f2u(wt.scale[d][0][h])));
+    f32x4_t part[4][MG];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const u32x4 wf = operand<XT>(words[w]);
+#pragma unroll
+      for (int q = 0; q < MG; ++q) part[w][q] = mfma<XT>(xf[q], wf, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int q = 0; q < MG; ++q)
+#pragma unroll
+        for (int m = 0; m < MQ; ++m) acc[w][4 * q + m] = __builtin_fmaf(part[w][q][m], s[w], acc[w][4 * q + m]);
   };
 
   float* const sums = reinterpret_cast<float*>(lds + mrows * stride);
-  constexpr int kOne = 4 * MR * 16;  // a wave's sums: of the four ranges, MR x 16 each
+  constexpr int kOne = few_sums(MR);
   int group = blockIdx.x, round = 0, turn = 0;
   auto finish = [&] {
     float* const part = sums + turn * (kWaves * kOne);
+    if (few_buffers(MR) == 1) __syncthreads();
     if (g == (c & 3)) {
 #pragma unroll
       for (int m = 0; m < MR; ++m)
@@ -253,13 +273,11 @@ __global__ void __launch_bounds__(kGemmThreads)
         for (int s = 0; s < 4; ++s) v += part[w * kOne + s * MR * 16 + threadIdx.x];
       y[m * N + n] = 16.0f * v;
     }
-    turn ^= 1;  // the next group's sums go beside these, which may still be read
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-#pragma unroll
-      for (int i = 0; i < MR; ++i) acc[w][i] = 0.0f;
+    if (few_buffers(MR) == 2) turn ^= 1;  // the next group's sums go beside these, which may still be read
+    clear();
   };
 
+  clear();
   __syncthreads();
   // The D steps have one way out, after the last: with one after each the compiler
   // waits for all loads in every turn.  Steps past the last group multiply zeros.
@@ -268,7 +286,7 @@ __global__ void __launch_bounds__(kGemmThreads)
     for (int d = 0; d < D; ++d) {
       const int k0 = (round * kWaves + wave) * kPiece;
       if (k0 < kk) multiply(d, 0, k0), multiply(d, 1, k0 + 128);
-      wt.load(d);
+      load(d);
       if (++round == rounds) {
         if (group < groups) finish();
         round = 0;
@@ -291,14 +309,21 @@ __global__ void __launch_bounds__(kGemmThreads)
     k_int4_rows(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
                 int64_t M, int64_t N, int64_t K, int lgB, int groups, float* __restrict__ y) {
   extern __shared__ u32x4 lds[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15;
+  const int g = lane >> 4;
   const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
   const int mrows = (int)(M - m0 < 16 * MT ? M - m0 : 16 * MT);
   const int kk = (int)K, stride = x_stride(K);
   const __amdgpu_buffer_rsrc_t xres =
       __builtin_amdgcn_make_buffer_rsrc((void*)(x + m0 * K), (short)0, mrows * kk * 2, kRawBuffer);
   Weight<NT, D> wt(packed, scales, N, K, lgB, groups);
-  const int rounds = wt.rounds;
+  const int rounds = (pieces_of(K) + kWaves - 1) / kWaves;
+  int load_group = blockIdx.x, load_round = 0;
+  wt.turn_to(load_group);
+  auto load = [&](int d) {
+    wt.load(d, (uint32_t)((load_round * kWaves + wave) * kPiece));
+    if (++load_round == rounds) load_round = 0, wt.turn_to(load_group += gridDim.x);
+  };
   auto from = [&](int source, uint32_t v) {
     return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * source, (int)v);
   };
@@ -323,7 +348,7 @@ __global__ void __launch_bounds__(kGemmThreads)
   };
   auto load_all = [&] {
 #pragma unroll
-    for (int d = 0; d < D; ++d) wt.load(d);
+    for (int d = 0; d < D; ++d) load(d);
   };
   if constexpr (XL) stage_x(lds, xres, mrows, K, load_all);
   else load_all();
@@ -419,7 +444,7 @@ __global__ void __launch_bounds__(kGemmThreads)
         read_x(0, round + 1 == rounds ? wave * kPiece : k0 + kWaves * kPiece);
         if (k0 < kk) multiply(d, 1, k0 + 128);
       }
-      wt.load(d);
+      load(d);
       if (++round == rounds) {
         if (group < groups) finish();
         round = 0;
@@ -438,20 +463,19 @@ Int4Kernel int4_kernel_for(int G) {
                    : &k_int4_rows<XT, MT, NT, D, 32, XL>;
 }
 template <int XT>
-Int4Kernel int4_few_kernel(int64_t M) {
-  return M == 1 ? &k_int4_few<XT, 1, 3> : M == 2 ? &k_int4_few<XT, 2, 3> : &k_int4_few<XT, 4, 3>;
+Int4Kernel int4_few_kernel(int few) {
+  return few == 1   ? &k_int4_few<XT, 1, 2>
+         : few == 2 ? &k_int4_few<XT, 2, 2>
+                    : &k_int4_few<XT, 4, 2>;
 }
 template <int XT>
 Int4Kernel int4_kernel(bool xl, int MT, int NT, int G) {
-  if (xl) return MT == 1 ? int4_kernel_for<XT, 1, 1, 3, true>(G) : int4_kernel_for<XT, 2, 1, 3, true>(G);
-  if (MT == 1)
-    return NT == 1   ? int4_kernel_for<XT, 1, 1, 3, false>(G)
-           : NT == 2 ? int4_kernel_for<XT, 1, 2, 2, false>(G)
-                     : int4_kernel_for<XT, 1, 4, 2, false>(G);
+  if (xl) return MT == 1 ? int4_kernel_for<XT, 1, 1, 2, true>(G) : int4_kernel_for<XT, 2, 1, 2, true>(G);
+  if (MT == 1) return NT == 1 ? int4_kernel_for<XT, 1, 1, 3, false>(G) : int4_kernel_for<XT, 1, 2, 2, false>(G);
   return NT == 1 ? int4_kernel_for<XT, 2, 1, 3, false>(G) : int4_kernel_for<XT, 2, 2, 2, false>(G);
 }
 
-constexpr int64_t kInt4MaxK = 1 << 22;  // 64 rows of codes stay below 2^31 bytes
+constexpr int64_t kInt4MaxK = 1 << 22;  // 32 rows of x and 16 of codes stay below 2^31 bytes
 constexpr int64_t kLds = 160 * 1024, kCus = 256;
 
 }  // namespace
@@ -477,24 +501,18 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
   // rows start at multiples of 128
   const int G = block >= 128 && K % 128 == 0 ? 128 : block >= 64 ? 64 : 32;
   // x in LDS where it leaves room for the waves' sums
-  const int few = M <= 1 ? 1 : M <= 2 ? 2 : M <= 4 ? 4 : 0;
-  const int64_t pieces = pieces_of(K), xbytes = mrows * (pieces * (kPiece / 8) + 1) * 16;
-  const int64_t sbytes = 2 * kWaves * 16 * 4 * (few ? 4 * few : mrows);
+  const int few = M <= 2 ? (int)M : M <= 4 ? 4 : 0;
+  const int64_t xbytes = mrows * (pieces_of(K) * (kPiece / 8) + 1) * 16;
+  const int64_t sbytes = few ? few_buffers(few) * kWaves * few_sums(few) * 4 : 2 * kWaves * 16 * mrows * 4;
   const bool xl = xbytes + sbytes <= kLds;
   const int64_t tiles = (N + 15) / 16;
-  const int NT = xl || tiles <= 512 ? 1 : tiles <= 1024 || MT == 2 ? 2 : 4;
+  const int NT = xl || tiles <= 512 ? 1 : 2;
   const int64_t groups = (tiles + NT - 1) / NT;
-  if (groups > kMaxGrid || mgroups > 65535) return ZQ_E_SIZE;
+  if (groups > kMaxGrid / 2 || mgroups > 65535) return ZQ_E_SIZE;
   const int64_t lds = xl ? xbytes + sbytes : 2 * kWaves * 16 * 4 * mrows * NT;
-  // x in LDS: as many workgroups as are resident at once, each with as many groups as
-  // the others
-  int64_t grid = groups;
-  if (xl) {
-    const int64_t room = kLds / lds > 2 ? 2 : kLds / lds;
-    const int64_t turns = (groups + room * kCus - 1) / (room * kCus);
-    grid = (groups + turns - 1) / turns;
-  }
-  const Int4Kernel k = xl && few ? (xt == ZQ_BF16 ? int4_few_kernel<ZQ_BF16>(M) : int4_few_kernel<ZQ_F16>(M))
+  // x in LDS: as many workgroups as are resident at once
+  const int64_t room = (lds <= kLds / 2 ? 2 : 1) * kCus, grid = xl && groups > room ? room : groups;
+  const Int4Kernel k = xl && few ? (xt == ZQ_BF16 ? int4_few_kernel<ZQ_BF16>(few) : int4_few_kernel<ZQ_F16>(few))
                                  : (xt == ZQ_BF16 ? int4_kernel<ZQ_BF16>(xl, MT, NT, G) : int4_kernel<ZQ_F16>(xl, MT, NT, G));
   return launch_grid(k, dim3((unsigned)grid, (unsigned)mgroups), (unsigned)kGemmThreads, (unsigned)lds,
                      static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(x), packed, scales, M, N, K, lgB,
