@@ -48,7 +48,7 @@ struct Entry {
   const float* scales;
   char* out;
   int64_t n;        // elements
-  int64_t chunk0;   // chunks of the entries before it
+  int64_t chunk0;   // chunks (clipping: pieces) of the entries before it
   int8_t type, out_type, lgB, pad;
   int32_t pad4;
 };
@@ -60,9 +60,10 @@ __host__ __device__ constexpr int64_t chunk_elems(int type) {
 }
 
 // Table: the workgroups' sums, the entries of the norm, the entries of clipping (an
-// INT4 shard clipped in place is its scales there).
+// INT4 shard clipped in place is its scales there), the entry of each piece of clipping.
 constexpr int64_t kSumsAt = 0, kEntriesAt = kSumsAt + 8 * kNormGroups;
 __host__ __device__ inline int64_t clip_at(int entries) { return kEntriesAt + (int64_t)entries * (int64_t)sizeof(Entry); }
+__host__ __device__ inline int64_t map_at(int entries) { return clip_at(entries) + (int64_t)entries * (int64_t)sizeof(Entry); }
 
 // index of the entry that holds chunk c (every thread gets it)
 __device__ __forceinline__ int find_entry(const Entry* entries, int count, int64_t c) {
@@ -220,133 +221,107 @@ __global__ void __launch_bounds__(kNormThreads)
   if (threadIdx.x == 0) *norm = (float)(fabs((double)scale) * sqrt(t));
 }
 
-// E elements a thread and step: 16 bytes written, or read where that is less
+// ---- clipping: a workgroup per piece of kClipElems elements.  Pieces are small and
+// workgroups start in their order, so that the result is written nearly in address
+// order (50 million bf16 elements into binary32: TODO us; in 2,048 streams far apart,
+// as the norm reads, 51 to 60).
+constexpr int kClipElems = 4096;
+constexpr int kClipSteps = kClipElems / kNormThreads / 4;
+
+// 4 elements a thread and step, so that a binary32 store of the wave covers whole lines
 template <int DT, int YT>
-__device__ __forceinline__ void scale_elems(const Entry& en, int64_t e0, int64_t e1, float c) {
-  constexpr int E = DT == ZQ_F32 || YT == ZQ_F32 ? 4 : 8, STEP = kNormThreads * E, N = E * dt_size<DT>() / 4;
+__device__ __forceinline__ void scale_elems(const Entry& en, int64_t e0, float c) {
+  constexpr int N = dt_size<DT>();  // words of 4 elements
   auto put = [&](int64_t i, const uint32_t(&w)[N]) {
-    float v[E];
+    float v[4];
     widen<DT>(w, v);
 #pragma unroll
-    for (int k = 0; k < E; ++k) v[k] = v[k] * c;
-    store_elems<YT, E>(en.out, i, v);
+    for (int k = 0; k < 4; ++k) v[k] = v[k] * c;
+    store_elems<YT, 4, true>(en.out, i, v);
   };
-  int64_t i = e0 + (int64_t)threadIdx.x * E;
-  for (; i + (kSteps - 1) * STEP + E <= e1; i += kSteps * STEP) {
-    uint32_t w[kSteps][N];
+  const int64_t i = e0 + threadIdx.x * 4;
+  if (e0 + kClipElems <= en.n) {
+    uint32_t w[kClipSteps][N];
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) load_words_any<false>(en.data + (i + u * STEP) * dt_size<DT>(), w[u]);
+    for (int u = 0; u < kClipSteps; ++u)
+      load_words_any<false>(en.data + (i + u * (4 * kNormThreads)) * dt_size<DT>(), w[u]);
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) put(i + u * STEP, w[u]);
+    for (int u = 0; u < kClipSteps; ++u) put(i + u * (4 * kNormThreads), w[u]);
+    return;
   }
-  for (; i + E <= e1; i += STEP) {
-    uint32_t w[N];
-    load_words_any<false>(en.data + i * dt_size<DT>(), w);
-    put(i, w);
-  }
-  for (; i < e1; ++i) {
-    float v[1];
-    load_elems<DT, 1>(en.data, i, v);
-    v[0] = v[0] * c;
-    store_elems<YT, 1>(en.out, i, v);
+  for (int u = 0; u < kClipSteps; ++u) {
+    int64_t k = i + u * (4 * kNormThreads);
+    if (k + 4 <= en.n) {
+      uint32_t w[N];
+      load_words_any<false>(en.data + k * dt_size<DT>(), w);
+      put(k, w);
+    } else {
+      for (; k < en.n && k < i + u * (4 * kNormThreads) + 4; ++k) {
+        float v[1];
+        load_elems<DT, 1>(en.data, k, v);
+        v[0] = v[0] * c;
+        store_elems<YT, 1>(en.out, k, v);
+      }
+    }
   }
 }
 
 // the INT4 shard dequantised with its scales times c: fl(q * fl(s * c))
 template <int YT>
-__device__ __forceinline__ void scale_int4(const Entry& en, int64_t e0, int64_t e1, float c) {
-  constexpr int E = 8, STEP = kNormThreads * E;
-  const int lane = threadIdx.x & 63;
-  auto put = [&](int64_t i, uint32_t w, float scale) {
-    const float s = scale * c;
-    float v[E];
+__device__ __forceinline__ void scale_int4(const Entry& en, int64_t e0, float c) {
+  auto value = [](uint32_t q, int k, float s) { return (float)((int32_t)(q << (28 - 4 * k)) >> 28) * s; };
+  const int64_t i = e0 + threadIdx.x * 4;
+  if (e0 + kClipElems <= en.n) {
+    uint32_t q[kClipSteps];
+    float s[kClipSteps];
 #pragma unroll
-    for (int k = 0; k < E; ++k) v[k] = (float)((int32_t)(w << (28 - 4 * k)) >> 28) * s;
-    store_elems<YT, E>(en.out, i, v);
-  };
-  // the wave's 512 elements at once: binary32 ones in two halves of 256, in which
-  // lane l stores the four of word l / 2, so that a store covers whole lines
-  auto put_wave = [&](int64_t i, uint32_t w, float scale) {
-    if constexpr (YT == ZQ_F32) {
-      const float s = scale * c;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int from = 32 * h + (lane >> 1);
-        const uint32_t q = __shfl(w, from) >> (16 * (lane & 1));
-        const float t = __shfl(s, from);
-        float v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = (float)((int32_t)(q << (28 - 4 * k)) >> 28) * t;
-        store_elems<YT, 4>(en.out, i - 8 * lane + 256 * h + 4 * lane, v);
-      }
-    } else {
-      put(i, w, scale);
-    }
-  };
-  int64_t i = e0 + (int64_t)threadIdx.x * E;
-  for (; i - lane * E + (kSteps - 1) * STEP + 64 * E <= e1; i += kSteps * STEP) {  // whole waves
-    uint32_t w[kSteps][1];
-    float s[kSteps];
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-      load_words_any<false>(en.data + (i + u * STEP) / 2, w[u]);
-      s[u] = en.scales[(i + u * STEP) >> en.lgB];
+    for (int u = 0; u < kClipSteps; ++u) {
+      const int64_t k = i + u * (4 * kNormThreads);
+      q[u] = *reinterpret_cast<const u16_any*>(en.data + k / 2);
+      s[u] = en.scales[k >> en.lgB];
     }
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) put_wave(i + u * STEP, w[u][0], s[u]);
+    for (int u = 0; u < kClipSteps; ++u) {
+      const float t = s[u] * c;
+      const float v[4] = {value(q[u], 0, t), value(q[u], 1, t), value(q[u], 2, t), value(q[u], 3, t)};
+      store_elems<YT, 4, true>(en.out, i + u * (4 * kNormThreads), v);
+    }
+    return;
   }
-  for (; i + E <= e1; i += STEP) {
-    uint32_t w[1];
-    load_words_any<false>(en.data + i / 2, w);
-    put(i, w[0], en.scales[i >> en.lgB]);
-  }
-  for (; i < e1; ++i) {
-    const uint32_t q = (uint8_t)en.data[i / 2] >> (4 * (i & 1));
-    float v[1] = {(float)((int32_t)(q << 28) >> 28) * (en.scales[i >> en.lgB] * c)};
-    store_elems<YT, 1>(en.out, i, v);
+  for (int u = 0; u < kClipSteps; ++u) {
+    const int64_t k0 = i + u * (4 * kNormThreads);
+    for (int64_t k = k0; k < en.n && k < k0 + 4; ++k) {
+      const float v[1] = {value((uint8_t)en.data[k / 2] >> (4 * (k & 1)), 0, en.scales[k >> en.lgB] * c)};
+      store_elems<YT, 1>(en.out, k, v);
+    }
   }
 }
 
 template <int YT>
-__device__ __forceinline__ void scale_to(const Entry& en, int64_t e0, int64_t e1, float c) {
+__device__ __forceinline__ void scale_to(const Entry& en, int64_t e0, float c) {
   switch (en.type) {
-    case ZQ_F32: scale_elems<ZQ_F32, YT>(en, e0, e1, c); break;
-    case ZQ_F16: scale_elems<ZQ_F16, YT>(en, e0, e1, c); break;
-    case ZQ_BF16: scale_elems<ZQ_BF16, YT>(en, e0, e1, c); break;
-    default: scale_int4<YT>(en, e0, e1, c); break;
+    case ZQ_F32: scale_elems<ZQ_F32, YT>(en, e0, c); break;
+    case ZQ_F16: scale_elems<ZQ_F16, YT>(en, e0, c); break;
+    case ZQ_BF16: scale_elems<ZQ_BF16, YT>(en, e0, c); break;
+    default: scale_int4<YT>(en, e0, c); break;
   }
 }
 
 __global__ void __launch_bounds__(kNormThreads)
-    k_grad_clip(const char* __restrict__ table, int norm_count, int count, int64_t chunks,
-                const float* __restrict__ norm, float max_norm, float scale) {
-  const Entry* entries = reinterpret_cast<const Entry*>(table + clip_at(norm_count));
+    k_grad_clip(const char* __restrict__ table, int count, const float* __restrict__ norm, float max_norm,
+                float scale) {
+  const int* entry_of = reinterpret_cast<const int*>(table + map_at(count));
+  const Entry en = reinterpret_cast<const Entry*>(table + clip_at(count))[entry_of[blockIdx.x]];
   const float ratio = max_norm / (*norm + 1e-6f);
   // a NaN ratio stays: min would drop it
   const float c = scale * (ratio > 1.0f ? 1.0f : ratio);
-  const int64_t W = gridDim.x, w = blockIdx.x;
-  int64_t k = w * chunks / W;
-  const int64_t k1 = (w + 1) * chunks / W;
-  if (k >= k1) return;
-  int i = find_entry(entries, count, k);
-  while (k < k1) {
-    const Entry en = entries[i];
-    const int64_t per = chunk_elems(en.type);
-    const int64_t e0 = (k - en.chunk0) * per;
-    const int64_t last = en.chunk0 + (en.n + per - 1) / per;
-    const int64_t to = k1 < last ? k1 : last;
-    int64_t e1 = (to - en.chunk0) * per;
-    if (e1 > en.n) e1 = en.n;
-    // in place and nothing to scale: the tensor stays as it is
-    if (!(en.out == en.data && c == 1.0f)) {
-      switch (en.out_type) {
-        case ZQ_F32: scale_to<ZQ_F32>(en, e0, e1, c); break;
-        case ZQ_F16: scale_to<ZQ_F16>(en, e0, e1, c); break;
-        default: scale_to<ZQ_BF16>(en, e0, e1, c); break;
-      }
-    }
-    k = to;
-    ++i;
+  // in place and nothing to scale: the tensor stays as it is
+  if (en.out == en.data && c == 1.0f) return;
+  const int64_t e0 = ((int64_t)blockIdx.x - en.chunk0) * kClipElems;
+  switch (en.out_type) {
+    case ZQ_F32: scale_to<ZQ_F32>(en, e0, c); break;
+    case ZQ_F16: scale_to<ZQ_F16>(en, e0, c); break;
+    default: scale_to<ZQ_BF16>(en, e0, c); break;
   }
 }
 
@@ -397,6 +372,7 @@ Entry clip_entry(const zq_grad& g) {
   return e;
 }
 int64_t chunks_of(const Entry& e) { return (e.n + chunk_elems(e.type) - 1) / chunk_elems(e.type); }
+int64_t pieces_of(const Entry& e) { return (e.n + kClipElems - 1) / kClipElems; }
 
 // Outputs must not overlap each other nor another tensor's data: the ranges in
 // the order of their addresses, each output against what starts before its end.
@@ -440,11 +416,12 @@ int plan_table(const zq_grad* grads, int32_t count, zq_grad_plan* plan) {
     const int rc = check(grads[i]);
     if (rc != ZQ_OK) return rc;
     p.norm_chunks += chunks_of(norm_entry(grads[i]));
-    p.clip_chunks += chunks_of(clip_entry(grads[i]));
+    p.clip_chunks += pieces_of(clip_entry(grads[i]));
+    if (p.clip_chunks > kMaxGrid) return ZQ_E_SIZE;
   }
   const int rc = check_overlaps(grads, count);
   if (rc != ZQ_OK) return rc;
-  p.bytes = clip_at(count) + (int64_t)count * (int64_t)sizeof(Entry);
+  p.bytes = map_at(count) + 4 * p.clip_chunks;
   *plan = p;
   return ZQ_OK;
 }
@@ -475,6 +452,7 @@ int zq_grad_plan_table(const zq_grad* grads, const zq_grad_plan* plan, void* hos
   std::fill(t, t + kEntriesAt, (char)0);
   Entry* norm = reinterpret_cast<Entry*>(t + kEntriesAt);
   Entry* clip = reinterpret_cast<Entry*>(t + clip_at(plan->count));
+  int* map = reinterpret_cast<int*>(t + map_at(plan->count));
   int64_t n = 0, c = 0;
   for (int32_t i = 0; i < plan->count; ++i) {
     norm[i] = norm_entry(grads[i]);
@@ -482,7 +460,9 @@ int zq_grad_plan_table(const zq_grad* grads, const zq_grad_plan* plan, void* hos
     norm[i].chunk0 = n;
     clip[i].chunk0 = c;
     n += chunks_of(norm[i]);
-    c += chunks_of(clip[i]);
+    const int64_t pieces = pieces_of(clip[i]);
+    std::fill(map + c, map + c + pieces, i);
+    c += pieces;
   }
   return ZQ_OK;
 }
@@ -507,8 +487,8 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
   if (!aligned(table, 16) || !aligned(norm, 4)) return ZQ_E_ALIGN;
   if (!(max_norm >= 0.0f)) return ZQ_E_SIZE;
   if (plan->clip_chunks == 0) return ZQ_OK;
-  return launch(&k_grad_clip, groups_for(plan->clip_chunks), kNormThreads, static_cast<hipStream_t>(stream),
-                static_cast<const char*>(table), plan->count, plan->count, plan->clip_chunks, norm, max_norm, scale);
+  return launch(&k_grad_clip, (unsigned)plan->clip_chunks, kNormThreads, static_cast<hipStream_t>(stream),
+                static_cast<const char*>(table), plan->count, norm, max_norm, scale);
 }
 
 }  // extern "C"
