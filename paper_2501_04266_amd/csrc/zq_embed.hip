@@ -50,9 +50,12 @@ __device__ __forceinline__ int64_t id_at(const void* ids, bool wide, int64_t t) 
   return wide ? static_cast<const int64_t*>(ids)[t] : (int64_t)static_cast<const int32_t*>(ids)[t];
 }
 
-// A thread moves E elements of one token's row.  The last piece of a row starts
-// E before its end (it repeats elements of the piece before it where E does not
-// divide D); E = 1 serves rows shorter than 8.
+// A thread moves E elements of one token's row, 16 or 32 bytes of y.  The last piece of a
+// row starts E before its end (it repeats elements of the piece before it where E does
+// not divide D); E = 1 serves rows shorter than 8.  y is written past the caches, which
+// are left to the table's rows: tokens repeat (16,384 tokens of 6,144 bf16 elements, ids
+// of frequency 1 / rank: 57 us, 64 with plain stores; from INT8 44 and 68).  Slices of
+// the columns by XCD, so that each XCD's L2 holds other columns, measured slower (65).
 template <int WT, int YT, int E>
 __global__ void __launch_bounds__(kEmbedThreads)
     k_embed(const void* __restrict__ ids, bool wide, const void* __restrict__ table, const float* __restrict__ scales,
@@ -88,7 +91,7 @@ __global__ void __launch_bounds__(kEmbedThreads)
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = scale * v[i];
   }
-  store_elems<YT, E>(y, p.row * D + d, v);
+  store_elems<YT, E, true>(y, p.row * D + d, v);
 }
 
 // ---------------------------------------------------------------- gradient
@@ -427,16 +430,28 @@ __global__ void __launch_bounds__(kEmbedThreads)
 
 using EmbedKernel = void (*)(const void*, bool, const void*, const float*, int64_t, int64_t, int64_t, int, double, int,
                              float, void*);
-template <int WT, int E>
-EmbedKernel embed_kernel_to(int yt) {
-  return yt == ZQ_F32 ? &k_embed<WT, ZQ_F32, E> : yt == ZQ_F16 ? &k_embed<WT, ZQ_F16, E> : &k_embed<WT, ZQ_BF16, E>;
+// columns of a piece: 16 bytes of the result (1 column where rows are shorter than 8)
+template <int YT>
+constexpr int piece_of() {
+  return 16 / dt_size<YT>();
 }
-template <int E>
-EmbedKernel embed_kernel(int wt, int yt) {
-  return wt == kInt8    ? embed_kernel_to<kInt8, E>(yt)
-         : wt == ZQ_F32 ? embed_kernel_to<ZQ_F32, E>(yt)
-         : wt == ZQ_F16 ? embed_kernel_to<ZQ_F16, E>(yt)
-                        : embed_kernel_to<ZQ_BF16, E>(yt);
+// of the lookup: 32 bytes where both sides are binary32 (16,384 x 6,144: 108 us, 126 with 16)
+constexpr int lookup_piece(int wt, int yt) { return wt == ZQ_F32 || yt != ZQ_F32 ? 8 : 4; }
+template <int WT, int YT>
+EmbedKernel embed_kernel_for(bool short_rows) {
+  return short_rows ? &k_embed<WT, YT, 1> : &k_embed<WT, YT, lookup_piece(WT, YT)>;
+}
+template <int WT>
+EmbedKernel embed_kernel_to(int yt, bool short_rows) {
+  return yt == ZQ_F32   ? embed_kernel_for<WT, ZQ_F32>(short_rows)
+         : yt == ZQ_F16 ? embed_kernel_for<WT, ZQ_F16>(short_rows)
+                        : embed_kernel_for<WT, ZQ_BF16>(short_rows);
+}
+EmbedKernel embed_kernel(int wt, int yt, bool short_rows) {
+  return wt == kInt8    ? embed_kernel_to<kInt8>(yt, short_rows)
+         : wt == ZQ_F32 ? embed_kernel_to<ZQ_F32>(yt, short_rows)
+         : wt == ZQ_F16 ? embed_kernel_to<ZQ_F16>(yt, short_rows)
+                        : embed_kernel_to<ZQ_BF16>(yt, short_rows);
 }
 
 using RowsKernel = void (*)(const void*, bool, const char*, const int*, const int*, int, unsigned, float*, int64_t,
@@ -450,11 +465,6 @@ RowsKernel rows_kernel_add(bool add) {
 template <int YT, int E>
 JoinKernel join_kernel_add(bool add) {
   return add ? &k_grad_join<YT, E, true> : &k_grad_join<YT, E, false>;
-}
-// columns of a piece: 16 bytes of the result (1 column where rows are shorter than 8)
-template <int YT>
-constexpr int piece_of() {
-  return 16 / dt_size<YT>();
 }
 template <int GT, int YT>
 RowsKernel rows_kernel_for(bool short_rows, bool add) {
@@ -498,11 +508,11 @@ int embed(const void* ids, int it, int64_t T, const void* table, const float* sc
   if (any_overlap({{y, T * D * elem_bytes(yt)}},
                   {{ids, T * ib}, {table, V * D * wb}, {scales, wt == kInt8 ? 4 * num_scales(V * D, block) : 0}}))
     return ZQ_E_ALIAS;
-  const int E = D < 8 ? 1 : 8;
-  const int64_t C = (D + E - 1) / E;
+  const bool short_rows = D < 8;
+  const int64_t E = short_rows ? 1 : lookup_piece(wt, yt), C = (D + E - 1) / E;
   const int64_t grid = grid_for(T * C, kEmbedThreads);
   if (grid == 0) return ZQ_E_SIZE;
-  return launch(E == 8 ? embed_kernel<8>(wt, yt) : embed_kernel<1>(wt, yt), (unsigned)grid, kEmbedThreads,
+  return launch(embed_kernel(wt, yt, short_rows), (unsigned)grid, kEmbedThreads,
                 static_cast<hipStream_t>(stream), ids, it == ZQ_I64, table, scales, T, V, D, (int)C, 1.0 / (double)C,
                 lgB, scale, y);
 }
