@@ -310,9 +310,13 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
  *   y       [M][N] float row-major (written)
  * K a multiple of 64, at most 2^22 (ZQ_E_SIZE); M, N >= 0 arbitrary; K = 0 writes
  * zeros.  x and packed 16-byte aligned, scales and y 4-byte aligned.  Meant for few
- * rows: the weight is read again for every 32 rows of x. */
+ * rows: the weight is read again for every 64 rows of x.
+ *   workspace: device memory of zq_int4_dequant_gemm_bytes(M, N, K) bytes or more, 4-byte
+ *   aligned, the call's own until it has run (sums over slices of a long K; may be NULL
+ *   where that is 0); one that is too small is ZQ_E_SIZE. */
 int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, const float* scales, int64_t M, int64_t N,
-                         int64_t K, int32_t block, float* y, void* stream);
+                         int64_t K, int32_t block, float* y, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t zq_int4_dequant_gemm_bytes(int64_t M, int64_t N, int64_t K); /* -1 for sizes outside the limits */
 
 /* Size helpers (host only): number of scales ceil(n/block) (-1 on a bad
  * block or n < 0), and INT4 bytes ceil(n/2) (-1 for n < 0). */

@@ -20,6 +20,7 @@ from ._lib import (  # noqa: F401
     grad_table,
     int4_bytes,
     int4_dequant_gemm,
+    int4_dequant_gemm_bytes,
     lib,
     num_scales,
     qgz_dequantize,

@@ -21,6 +21,7 @@ EXPORTS = ["qwz_quantize", "qwz_dequantize", "qgz_quantize", "qgz_reduce_level",
            "qgz_reduce_dequantize", "qgz_reduce_level_gather", "qgz_reduce_level_gather_noalloc",
            "qwz_dequant_gemm", "zq_embedding", "qwz_embedding", "zq_embedding_grad", "zq_embedding_grad_bytes",
            "zq_grad_plan_make", "zq_grad_plan_table", "zq_grad_norm", "zq_grad_clip", "zq_int4_dequant_gemm",
+           "zq_int4_dequant_gemm_bytes",
            "zq_num_scales", "zq_int4_bytes", "zq_status_string"]
 
 _TORCH_DT = {torch.float32: ZQ_F32, torch.float16: ZQ_F16, torch.bfloat16: ZQ_BF16}
@@ -72,7 +73,7 @@ def lib():
         "zq_grad_plan_table": [vp, vp, vp],
         "zq_grad_norm": [vp, vp, f32, vp, vp],
         "zq_grad_clip": [vp, vp, vp, f32, f32, vp],
-        "zq_int4_dequant_gemm": [vp, ci, vp, vp, i64, i64, i64, i32, vp, vp],
+        "zq_int4_dequant_gemm": [vp, ci, vp, vp, i64, i64, i64, i32, vp, vp, i64, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -80,6 +81,7 @@ def lib():
     L.zq_num_scales.argtypes, L.zq_num_scales.restype = [i64, i32], i64
     L.zq_int4_bytes.argtypes, L.zq_int4_bytes.restype = [i64], i64
     L.zq_embedding_grad_bytes.argtypes, L.zq_embedding_grad_bytes.restype = [i64, i64, i64], i64
+    L.zq_int4_dequant_gemm_bytes.argtypes, L.zq_int4_dequant_gemm_bytes.restype = [i64, i64, i64], i64
     L.zq_status_string.argtypes, L.zq_status_string.restype = [ci], ctypes.c_char_p
     _lib = L
     return L
@@ -137,6 +139,7 @@ _ELEM = (torch.float32, torch.float16, torch.bfloat16)
 _I8 = (torch.int8,)
 _U8 = (torch.uint8,)
 _F32 = (torch.float32,)
+_IDS = tuple(_ID_DT)
 
 
 def _check(status, what):
@@ -345,7 +348,7 @@ def embedding(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
         raise ValueError("table must be 2-D [V, D]")
     V, D = table.shape
     T = ids.numel()
-    _need(ids, "ids", T, tuple(_ID_DT))
+    _need(ids, "ids", T, _IDS)
     _need(table, "table", V * D, _ELEM)
     if out is None:
         out = torch.empty((*ids.shape, D), dtype=out_dtype or table.dtype, device=ids.device)
@@ -360,7 +363,7 @@ def qwz_embedding(ids, codes, scales, V, D, block=256, scale=1.0, out_dtype=torc
     [ceil(V*D/block)], as gathered): only the rows that occur are read and
     dequantised.  With scale 1 they are the rows qwz_dequantize writes."""
     T = ids.numel()
-    _need(ids, "ids", T, tuple(_ID_DT))
+    _need(ids, "ids", T, _IDS)
     _need(codes, "codes", V * D, _I8)
     _need(scales, "scales", _nsc(V * D, block), _F32)
     if out is None:
@@ -370,6 +373,16 @@ def qwz_embedding(ids, codes, scales, V, D, block=256, scale=1.0, out_dtype=torc
                                D, block, scale, _dev(out, "out"), _TORCH_DT[out.dtype], _stream(stream)),
            "qwz_embedding")
     return out
+
+
+def _workspace(nbytes, device, stream):
+    """Memory for one call on `stream`."""
+    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if stream is not None:
+        # allocated on the current stream, used on another: the allocator keeps it
+        # until that stream has passed the call
+        w.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+    return w
 
 
 def embedding_grad_bytes(T, V, D):
@@ -389,7 +402,7 @@ def embedding_grad(ids, dy, V, scale=1.0, out_dtype=torch.float32, out=None, acc
     are.  workspace: uint8, embedding_grad_bytes(T, V, D) or more; allocated if not
     given."""
     T = ids.numel()
-    _need(ids, "ids", T, tuple(_ID_DT))
+    _need(ids, "ids", T, _IDS)
     if dy.dim() < 1 or dy.numel() != T * dy.shape[-1]:
         raise ValueError(f"dy has shape {tuple(dy.shape)}; expected {(*ids.shape, 'D')}")
     D = dy.shape[-1]
@@ -401,11 +414,7 @@ def embedding_grad(ids, dy, V, scale=1.0, out_dtype=torch.float32, out=None, acc
         out = torch.empty((V, D), dtype=out_dtype, device=dy.device)
     _need(out, "out", V * D, _ELEM)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
-        if stream is not None:
-            # allocated on the current stream, used on another: the allocator
-            # keeps it until that stream has passed the call
-            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+        workspace = _workspace(need, dy.device, stream)
     _need(workspace, "workspace", need, _U8)
     _check(lib().zq_embedding_grad(_dev(ids, "ids"), _ID_DT[ids.dtype], T, _dev(dy, "dy"), _TORCH_DT[dy.dtype], V, D,
                                    scale, int(bool(accumulate)), _dev(out, "out"), _TORCH_DT[out.dtype],
@@ -499,11 +508,20 @@ def grad_clip(grads, norm, max_norm, scale=1.0, stream=None):
     return [o if o is not None else g[1] if isinstance(g, (tuple, list)) else g for g, o in zip(t.tensors, t.outs)]
 
 
-def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, stream=None):
+def int4_dequant_gemm_bytes(M, N, K):
+    """Bytes of workspace int4_dequant_gemm takes for M rows and an N x K weight."""
+    n = lib().zq_int4_dequant_gemm_bytes(M, N, K)
+    if n < 0:
+        raise ValueError(f"int4_dequant_gemm does not take M={M}, N={N}, K={K}")
+    return n
+
+
+def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, workspace=None, stream=None):
     """y[M, N] = x[M, K] @ W^T with W the N x K weight in the INT4 format (packed
     uint8 [N*K/2] row-major, scales [ceil(N*K/block)]: qgz_quantize of the weight),
     read as it is; meant for few rows.  x bf16 or fp16, y float32.  K must be a
-    multiple of 64."""
+    multiple of 64.  workspace: uint8, int4_dequant_gemm_bytes(M, N, K) or more;
+    allocated if not given."""
     if x.dim() != 2:
         raise ValueError("x must be 2-D [M, K]")
     M, K = x.shape
@@ -512,7 +530,14 @@ def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, stream=None):
     _need(scales, "scales", _nsc(N * K, block), _F32)
     if y is None:
         y = torch.empty((M, N), dtype=torch.float32, device=x.device)
-    _need(y, "y", M * N, _F32)
+    else:
+        _need(y, "y", M * N, _F32)
+    need = lib().zq_int4_dequant_gemm_bytes(M, N, K)
+    if workspace is None and need > 0:
+        workspace = _workspace(need, x.device, stream)
+    at, size = (0, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel())
+    if workspace is not None:
+        _need(workspace, "workspace", max(need, 0), _U8)
     _check(lib().zq_int4_dequant_gemm(_dev(x, "x"), _TORCH_DT[x.dtype], _dev(packed, "packed"), _dev(scales, "scales"),
-                                      M, N, K, block, _dev(y, "y"), _stream(stream)), "int4_dequant_gemm")
+                                      M, N, K, block, _dev(y, "y"), at, size, _stream(stream)), "int4_dequant_gemm")
     return y

@@ -9,9 +9,19 @@
 // codes stay apart from its scale, which multiplies them in binary32: no
 // weight is rounded.  The factor 16 goes into the finished sum.
 //
-// A workgroup of W waves takes 16 NT weight rows and all of K, the waves 256
-// codes a row in turn (whole 128-byte lines); their partial sums are added in
-// LDS in the order of the waves.  x passes through LDS, a range of K at a time.
+// A workgroup of 8 waves takes 16 weight rows at a time (or some times 16), its
+// waves 256 codes a row in turn (whole 128-byte lines) over a slice of K, which
+// is all of K unless x or the grid asks for less; the waves' sums are added in
+// LDS in the order of the waves, the slices' sums in a second launch.
+//
+// What bounds it: the weight's bytes where they are many and the rows of x few
+// (5 rows, 50,001 x 6,144: 35 us, 4.7 TB/s of the 6.4 of a plain copy; 16 rows,
+// 40,000 x 6,144: 38 us), close behind it the instructions that turn codes into
+// operands (about 330 cycles of a SIMD for 2,048 codes: 13 a word for 8 codes,
+// the moves between lanes, the addresses).  Up to about 8 MiB of weight a launch
+// and one round of loads take longer than its bytes: 6 to 8 us.  With more rows
+// x is read from the L2s by every workgroup, at 10 TB/s in all (64 rows, 24,576 x
+// 6,144: 57 us, 33 without these reads).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -67,6 +77,11 @@ __device__ __forceinline__ u32x4 operand(uint32_t w) {
                pack2<XT>(sixteenth<2>(w), sixteenth<2>(h)), pack2<XT>(sixteenth<3>(w), sixteenth<3>(h))};
 }
 
+// v of another lane
+__device__ __forceinline__ uint32_t from_lane(int lane, uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * lane, (int)v);
+}
+
 // Lane (c, g) (c = lane % 16, g = lane / 16) holds words 0 .. 3 of its 16 bytes:
 // word j of lane (c, g) becomes word g of lane (c, j).  A 4 x 4 transposition
 // between the quarters of the wave, so that MFMA j reads 32 codes in a row.
@@ -78,6 +93,16 @@ __device__ __forceinline__ u32x4 transposed(u32x4 w) {
   return u32x4{p[0], p[1], q[0], q[1]};
 }
 
+// The part of K that a workgroup sums over: slices of `each` (a multiple of kPiece)
+// codes by blockIdx.z, the sums of slice z in plane z of `y` (M x N each).
+struct Slice {
+  int from, count;
+  __device__ __forceinline__ Slice(int64_t K, int each) {
+    from = (int)blockIdx.z * each;
+    count = (int)K - from < each ? (int)K - from : each;
+  }
+};
+
 constexpr int kWaves = 8;
 constexpr int kPiece = 256;  // codes of a weight row that a wave takes at a time: a 128-byte line
 constexpr int kGemmThreads = 64 * kWaves;
@@ -88,10 +113,10 @@ __host__ __device__ inline int pieces_of(int64_t K) { return K == 0 ? 1 : (int)(
 // read 64 bytes in a row (with a row for each of 16 lanes in a row the same loads take
 // four times as long in the address unit), and the scale of those codes, which lie in
 // one block.  Slots of D pieces of NT x 16 rows are in flight.
-template <int NT, int D>
+template <int T, int S>
 struct Weight {
-  u32x4 codes[D][NT][2];
-  float scale[D][NT][2];
+  u32x4 codes[S][2];
+  float scale[S][2];
 
   const uint8_t* packed;
   const float* scales;
@@ -101,54 +126,48 @@ struct Weight {
   __amdgpu_buffer_rsrc_t wres, sres;
   uint32_t first;  // its first row's place in its block
   uint32_t row0;   // this lane's first code, in the group's flat order
-  int end;         // pieces that start before this have codes for the lane
+  int end;         // pieces of the slice that start before this have codes for the lane
 
-  __device__ __forceinline__ Weight(const uint8_t* p, const float* s, int64_t n, int64_t k, int lg, int gr)
+  __device__ __forceinline__ Weight(const uint8_t* p, const float* s, int64_t n, int64_t k, Slice sl, int lg, int gr)
       : packed(p), scales(s), N(n), K(k), lgB(lg), groups(gr) {
     const int lane = threadIdx.x & 63;
-    row0 = (uint32_t)(lane >> 2) * (uint32_t)k + 32u * (lane & 3);
-    end = (int)k - 32 * (lane & 3);
+    row0 = (uint32_t)(lane >> 2) * (uint32_t)k + (uint32_t)sl.from + 32u * (lane & 3);
+    end = sl.count - 32 * (lane & 3);
   }
   __device__ __forceinline__ void turn_to(int group) {
     // past the last group: empty resources; the same loads go out, so that the number
     // of loads in flight is known at every wait, and bring zeros
     const bool any = group < groups;
-    const int64_t n0 = any ? (int64_t)group * (16 * NT) : 0;
-    const int rows = any ? (int)(N - n0 < 16 * NT ? N - n0 : 16 * NT) : 0;
+    const int64_t n0 = any ? (int64_t)group * (16 * T) : 0;
+    const int rows = any ? (int)(N - n0 < 16 * T ? N - n0 : 16 * T) : 0;
     wres = __builtin_amdgcn_make_buffer_rsrc((void*)(packed + n0 * (K / 2)), (short)0, rows * (int)(K / 2), kRawBuffer);
     const int64_t f0 = n0 * K, s0 = f0 >> lgB, s1 = (f0 + (int64_t)rows * K + (1 << lgB) - 1) >> lgB;
     sres = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + s0), (short)0, (int)((s1 - s0) * 4), kRawBuffer);
     first = (uint32_t)(f0 & ((1ll << lgB) - 1));
   }
-  // the piece from code k0 of the group's rows on; rows past the last, and codes past K,
-  // are outside the resources: zeros
-  __device__ __forceinline__ void load(int d, uint32_t k0) {
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const uint32_t f = row0 + 16 * t * (uint32_t)K + k0;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bool in = (int)k0 < end - 128 * h;
-        const uint32_t off = in ? f / 2 + 64u * h : kOutside;
-        codes[d][t][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wres, (int)off, 0, 0));
-        const uint32_t soff = in ? ((f + first + 128u * h) >> lgB) * 4 : kOutside;
-        scale[d][t][h] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sres, (int)soff, 0, 0));
-      }
-    }
+  // half h of the piece from code k0 of the slice on of the group's tile t, into slot s; rows
+  // past the last, and codes past the slice, are outside the resources: zeros
+  __device__ __forceinline__ void load(int s, int h, int t, uint32_t k0) {
+    const uint32_t f = row0 + 16 * t * (uint32_t)K + k0;
+    const bool in = (int)k0 < end - 128 * h;
+    const uint32_t off = in ? f / 2 + 64u * h : kOutside;
+    codes[s][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wres, (int)off, 0, 0));
+    const uint32_t soff = in ? ((f + first + 128u * h) >> lgB) * 4 : kOutside;
+    scale[s][h] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sres, (int)soff, 0, 0));
   }
 };
 
-// x rows m0 .. m0 + mrows in LDS, whole; elements past K, which meet zero codes, are
+// A slice of x rows m0 .. m0 + mrows in LDS, whole; elements past it, which meet zero codes, are
 // zeros.  Rows are an odd number of 16-byte units long, so that lanes that read one
 // column of 8 rows meet distinct banks.  `between` runs once the first loads are out.
 // What there is no place for goes to the unit after the last row: a load whose result
 // is left in its registers makes the compiler wait for all loads wherever these are
 // used again, in each turn of the loops below.
-__device__ __forceinline__ int x_stride(int64_t K) { return pieces_of(K) * (kPiece / 8) + 1; }
+__host__ __device__ inline int x_stride(int64_t K) { return pieces_of(K) * (kPiece / 8) + 1; }
 template <typename F>
-__device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres, int mrows, int64_t K, F between) {
+__device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres, int mrows, int64_t K, Slice sl, F between) {
   constexpr int U = 4;
-  const int stride = x_stride(K), kk = (int)K;
+  const int stride = x_stride(sl.count);
   const unsigned row = (unsigned)stride - 1, units = (unsigned)mrows * row;  // 16-byte units: below 2^14
   // a unit's row: the quotient is a half over the row length or more away from the next
   // whole number, the product off by 2^-23 of it
@@ -159,7 +178,7 @@ __device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres,
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const unsigned i = at + u * kGemmThreads, m = row_of(i), k = 8 * (i - m * row);
-      const uint32_t off = i < units && k < (unsigned)kk ? (m * (unsigned)kk + k) * 2 : kOutside;
+      const uint32_t off = i < units && k < (unsigned)sl.count ? (m * (unsigned)K + (unsigned)sl.from + k) * 2 : kOutside;
       v[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xres, (int)off, 0, 0));
     }
   };
@@ -187,37 +206,36 @@ __device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres,
 // the product's 16 x 16 sums those with s = c % 4 count, a quarter: lane (c, g) has them,
 // elements m, where g = c % 4.  The matrix cores have room for that (16 cycles of about
 // 150 per operand), and no lane needs codes that another one loaded, beyond the
-// transposition.  Each column has one scale, whatever the block size.
-// MR: rows of x, 1, 2 or a multiple of 4.
+// transposition.  Each column has one scale, whatever the block size.  Two pieces in
+// flight (3 and 4 measured no faster).  One row, 18,432 x 6,144: 17 us; 24,576 x 6,144:
+// 21 us, 3.8 TB/s.
+// MR: rows of x, 1, 2 or 4.
 __host__ __device__ constexpr int few_sums(int MR) { return 4 * MR * 16; }  // a wave's: MR x 16 of each range
-__host__ __device__ constexpr int few_buffers(int MR) { return MR <= 4 ? 2 : 1; }
 template <int XT, int MR, int D>
 __global__ void __launch_bounds__(kGemmThreads)
     k_int4_few(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
-               int64_t M, int64_t N, int64_t K, int lgB, int groups, float* __restrict__ y) {
-  constexpr int MG = MR <= 4 ? 1 : MR / 4, MQ = MR < 4 ? MR : 4;
+               int64_t M, int64_t N, int64_t K, int each, int lgB, int groups, float* __restrict__ y) {
   extern __shared__ u32x4 lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15;
   const int g = lane >> 4;
-  const int kk = (int)K, mrows = (int)M, stride = x_stride(K);
-  const int rounds = (pieces_of(K) + kWaves - 1) / kWaves;
-  Weight<1, D> wt(packed, scales, N, K, lgB, groups);
+  const Slice sl(K, each);
+  const int mrows = (int)M, stride = x_stride(sl.count);
+  const int rounds = (pieces_of(sl.count) + kWaves - 1) / kWaves;
+  y += blockIdx.z * (M * N);
+  Weight<1, D> wt(packed, scales, N, K, sl, lgB, groups);
   int load_group = blockIdx.x, load_round = 0;
   wt.turn_to(load_group);
   auto load = [&](int d) {
-    wt.load(d, (uint32_t)((load_round * kWaves + wave) * kPiece));
+    const uint32_t k0 = (uint32_t)((load_round * kWaves + wave) * kPiece);
+    wt.load(d, 0, 0, k0), wt.load(d, 1, 0, k0);
     if (++load_round == rounds) load_round = 0, wt.turn_to(load_group += gridDim.x);
   };
-  stage_x(lds, __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * kk * 2, kRawBuffer), mrows, K, [&] {
+  stage_x(lds, __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * (int)K * 2, kRawBuffer), mrows, K, sl, [&] {
 #pragma unroll
     for (int d = 0; d < D; ++d) load(d);
   });
-  const u32x4* xat[MG];  // rows past M repeat the last one; their sums are not stored
-#pragma unroll
-  for (int q = 0; q < MG; ++q) {
-    const int m = 4 * q + (lane & 3);
-    xat[q] = lds + (m < mrows ? m : mrows - 1) * stride + 4 * (c >> 2) + g;
-  }
+  // rows past M repeat the last one; their sums are not stored
+  const u32x4* const xat = lds + ((lane & 3) < mrows ? lane & 3 : mrows - 1) * stride + 4 * (c >> 2) + g;
 
   float acc[4][MR];
   auto clear = [&] {
@@ -227,27 +245,19 @@ __global__ void __launch_bounds__(kGemmThreads)
       for (int m = 0; m < MR; ++m) acc[w][m] = 0.0f;
   };
   auto multiply = [&](int d, int h, int k0) {
-    u32x4 xf[MG];
-#pragma unroll
-    for (int q = 0; q < MG; ++q) xf[q] = xat[q][k0 / 8];
-    const u32x4 words = transposed(wt.codes[d][0][h]);
+    const u32x4 xf = xat[k0 / 8];
+    const u32x4 words = transposed(wt.codes[d][h]);
     float s[4];  // the scale of lane 16 w + c
 #pragma unroll
     for (int w = 0; w < 4; ++w)
-      s[w] = u2f((uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * w + c), (int)f2u(wt.scale[d][0][h])));
-    f32x4_t part[4][MG];
+      s[w] = u2f(from_lane(16 * w + c, f2u(wt.scale[d][h])));
+    f32x4_t part[4];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const u32x4 wf = operand<XT>(words[w]);
-#pragma unroll
-      for (int q = 0; q < MG; ++q) part[w][q] = mfma<XT>(xf[q], wf, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
-    }
+    for (int w = 0; w < 4; ++w) part[w] = mfma<XT>(xf, operand<XT>(words[w]), f32x4_t{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
     for (int w = 0; w < 4; ++w)
 #pragma unroll
-      for (int q = 0; q < MG; ++q)
-#pragma unroll
-        for (int m = 0; m < MQ; ++m) acc[w][4 * q + m] = __builtin_fmaf(part[w][q][m], s[w], acc[w][4 * q + m]);
+      for (int m = 0; m < MR; ++m) acc[w][m] = __builtin_fmaf(part[w][m], s[w], acc[w][m]);
   };
 
   float* const sums = reinterpret_cast<float*>(lds + mrows * stride);
@@ -255,7 +265,6 @@ __global__ void __launch_bounds__(kGemmThreads)
   int group = blockIdx.x, round = 0, turn = 0;
   auto finish = [&] {
     float* const part = sums + turn * (kWaves * kOne);
-    if (few_buffers(MR) == 1) __syncthreads();
     if (g == (c & 3)) {
 #pragma unroll
       for (int m = 0; m < MR; ++m)
@@ -273,7 +282,7 @@ __global__ void __launch_bounds__(kGemmThreads)
         for (int s = 0; s < 4; ++s) v += part[w * kOne + s * MR * 16 + threadIdx.x];
       y[m * N + n] = 16.0f * v;
     }
-    if (few_buffers(MR) == 2) turn ^= 1;  // the next group's sums go beside these, which may still be read
+    turn ^= 1;  // the next group's sums go beside these, which may still be read
     clear();
   };
 
@@ -285,7 +294,7 @@ __global__ void __launch_bounds__(kGemmThreads)
 #pragma unroll
     for (int d = 0; d < D; ++d) {
       const int k0 = (round * kWaves + wave) * kPiece;
-      if (k0 < kk) multiply(d, 0, k0), multiply(d, 1, k0 + 128);
+      if (k0 < sl.count) multiply(d, 0, k0), multiply(d, 1, k0 + 128);
       load(d);
       if (++round == rounds) {
         if (group < groups) finish();
@@ -296,104 +305,184 @@ __global__ void __launch_bounds__(kGemmThreads)
   } while (group < groups);
 }
 
-// ---------------------------------------------------------------- more rows
+// ---------------------------------------------------------------- 5 to 16 rows
 //
-// MT: 16-row tiles of x.  G: codes summed before their scale is applied (they lie in one
-// block).  The codes and scales go to the lanes that need them through LDS (one
-// permutation of the wave): lane (c, g) takes the 32 codes of row c from 32 g on.
-// XL: all of x is in LDS, from before the first group on.  Otherwise it is read from
-// the caches, half a piece ahead, permuted like the codes; a group then has several
-// tiles, which share it.
-template <int XT, int MT, int NT, int D, int G, bool XL>
+// All of x, or a slice, is in LDS from before the first group of 16 weight rows on, and
+// the workgroups that are resident at once share the groups.  The codes and scales go to
+// the lanes that need them through LDS (permutations of the wave): lane (c, g) takes the
+// 32 codes of row c from 32 g on.  (Loads that bring them there directly, a row to each
+// of 16 lanes in a row, take longer in the address unit: 76 us for 5 rows of 50,001 x
+// 6,144, 35 this way.)
+// G: codes summed before their scale is applied (they lie in one block).
+template <int XT, int D, int G>
 __global__ void __launch_bounds__(kGemmThreads)
-    k_int4_rows(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
-                int64_t M, int64_t N, int64_t K, int lgB, int groups, float* __restrict__ y) {
+    k_int4_lds(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
+               int64_t M, int64_t N, int64_t K, int each, int lgB, int groups, float* __restrict__ y) {
+  extern __shared__ u32x4 lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15;
+  const int g = lane >> 4;
+  const Slice sl(K, each);
+  const int mrows = (int)M, stride = x_stride(sl.count);
+  const int rounds = (pieces_of(sl.count) + kWaves - 1) / kWaves;
+  y += blockIdx.z * (M * N);
+  Weight<1, D> wt(packed, scales, N, K, sl, lgB, groups);
+  int load_group = blockIdx.x, load_round = 0;
+  wt.turn_to(load_group);
+  auto load = [&](int d) {
+    const uint32_t k0 = (uint32_t)((load_round * kWaves + wave) * kPiece);
+    wt.load(d, 0, 0, k0), wt.load(d, 1, 0, k0);
+    if (++load_round == rounds) load_round = 0, wt.turn_to(load_group += gridDim.x);
+  };
+  stage_x(lds, __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * (int)K * 2, kRawBuffer), mrows, K, sl, [&] {
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(d);
+  });
+  // Lane (c, g) multiplies in MFMA j of a half piece elements 32 g + 8 j on, where the
+  // codes may stay as they are loaded; else, with the words transposed, 32 j + 8 g on.
+  constexpr bool kAsLoaded = G == 128;
+  constexpr int XG = kAsLoaded ? 32 : 8, XJ = kAsLoaded ? 8 : 32;
+  // rows past M repeat the last one; their sums are not stored
+  const u32x4* const xat = lds + (c < mrows ? c : mrows - 1) * stride + XG * g / 8;
+
+  f32x4_t acc;
+  auto multiply = [&](int d, int h, int k0) {  // half h of the piece in slot d; k0: its first code
+    u32x4 xf[4], words;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) xf[j] = xat[(k0 + XJ * j) / 8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) words[q] = from_lane(4 * c + g, wt.codes[d][h][q]);
+    if constexpr (!kAsLoaded) words = transposed(words);
+    float s[128 / G];
+#pragma unroll
+    for (int q = 0; q < 128 / G; ++q) s[q] = u2f(from_lane(4 * c + q * (G / 32), f2u(wt.scale[d][h])));
+    f32x4_t part;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool first = (32 * j) % G == 0, done = (32 * j + 32) % G == 0;
+      part = mfma<XT>(xf[j], operand<XT>(words[j]), first ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part);
+      if (done) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(part[e], s[32 * j / G], acc[e]);
+      }
+    }
+  };
+
+  // the waves' sums, in the order of the waves; element e of lane (c, g): row 4 g + e of
+  // x, weight row c
+  float* const sums = reinterpret_cast<float*>(lds + mrows * stride);
+  int group = blockIdx.x, round = 0, turn = 0;
+  auto finish = [&] {
+    float* const part = sums + turn * (kWaves * 16 * mrows);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (4 * g + e < mrows) part[(wave * mrows + 4 * g + e) * 16 + c] = acc[e];
+    __syncthreads();
+    const int64_t n = (int64_t)group * 16 + (threadIdx.x & 15);
+    const int m = threadIdx.x >> 4;
+    if (m < mrows && n < N) {
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) v += part[w * mrows * 16 + threadIdx.x];
+      y[m * N + n] = 16.0f * v;
+    }
+    turn ^= 1;  // the next group's sums go beside these, which may still be read
+    acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  };
+
+  acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  __syncthreads();
+  // one way out, after the last of the D steps, as above
+  do {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      const int k0 = (round * kWaves + wave) * kPiece;
+      if (k0 < sl.count) multiply(d, 0, k0), multiply(d, 1, k0 + 128);
+      load(d);
+      if (++round == rounds) {
+        if (group < groups) finish();
+        round = 0;
+        group += gridDim.x;
+      }
+    }
+  } while (group < groups);
+}
+
+// ---------------------------------------------------------------- more rows, small weights
+//
+// A wave takes the half pieces of its part of K; x of a half piece (16 MT rows) comes from
+// the caches, moved between lanes like the codes, and is multiplied with the codes of GB
+// tiles of 16 weight rows, whose sums stay in registers over the slice.  Nothing waits for
+// a staged x, and no workgroup has more than its share of K to read: a 2,048 x 8,192
+// product of 16 rows takes 8 us, 11 with x passed through LDS.  What it costs is x, read
+// again by every workgroup: GB tiles of the weight share a read.  The codes of a whole
+// piece, GB tiles of it, are in flight, and one half piece of x (two where GB is 1).
+// G: codes summed before their scale is applied.
+template <int XT, int MT, int GB, int G>
+__global__ void __launch_bounds__(kGemmThreads, MT == 1 ? 4 : 2)
+    k_int4_regs(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
+                int64_t M, int64_t N, int64_t K, int each, int lgB, int groups, float* __restrict__ y) {
   extern __shared__ u32x4 lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15;
   const int g = lane >> 4;
   const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
   const int mrows = (int)(M - m0 < 16 * MT ? M - m0 : 16 * MT);
-  const int kk = (int)K, stride = x_stride(K);
+  const Slice sl(K, each);
+  y += blockIdx.z * (M * N);
   const __amdgpu_buffer_rsrc_t xres =
-      __builtin_amdgcn_make_buffer_rsrc((void*)(x + m0 * K), (short)0, mrows * kk * 2, kRawBuffer);
-  Weight<NT, D> wt(packed, scales, N, K, lgB, groups);
-  const int rounds = (pieces_of(K) + kWaves - 1) / kWaves;
-  int load_group = blockIdx.x, load_round = 0;
-  wt.turn_to(load_group);
-  auto load = [&](int d) {
-    wt.load(d, (uint32_t)((load_round * kWaves + wave) * kPiece));
-    if (++load_round == rounds) load_round = 0, wt.turn_to(load_group += gridDim.x);
-  };
-  auto from = [&](int source, uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_ds_bpermute(4 * source, (int)v);
-  };
+      __builtin_amdgcn_make_buffer_rsrc((void*)(x + m0 * K), (short)0, mrows * (int)K * 2, kRawBuffer);
+  Weight<GB, GB> wt(packed, scales, N, K, sl, lgB, groups);
+  const int rounds = (pieces_of(sl.count) + kWaves - 1) / kWaves;
 
-  // Lane (c, g) multiplies in MFMA j of a half piece: elements 32 g + 8 j on, where the
-  // codes may stay as they are loaded; else, with the words transposed, 32 j + 8 g on.
-  constexpr bool kAsLoaded = G == 128 && XL;
-  constexpr int XG = kAsLoaded ? 32 : 8, XJ = kAsLoaded ? 8 : 32;
-  int xrow[MT];  // rows past M repeat the last one; their sums are not stored
-#pragma unroll
-  for (int i = 0; i < MT; ++i) xrow[i] = 16 * i + c < mrows ? 16 * i + c : mrows - 1;
-  u32x4 xv[XL ? 1 : 2][MT][4];
-  auto read_x = [&](int buf, int k0) {  // the half piece from k0 on; lane l: row l / 4, 8 elements at 32 j + 8 (l % 4)
+  // In MFMA j of a half piece lane (c, g) multiplies elements 32 j + 8 g on.
+  constexpr int XB = GB == 1 ? 2 : 1;  // half pieces of x in flight
+  u32x4 xv[XB][MT][4];
+  auto read_x = [&](int buf, int k0) {  // the half piece from k0 on; lane l: row l / 4
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int k = k0 + 32 * j + 8 * (lane & 3);
-        const uint32_t off = k < kk ? ((uint32_t)(16 * i + (lane >> 2)) * (uint32_t)kk + (uint32_t)k) * 2 : kOutside;
+        const uint32_t off =
+            k < sl.count ? ((uint32_t)(16 * i + (lane >> 2)) * (uint32_t)K + (uint32_t)(sl.from + k)) * 2 : kOutside;
         xv[buf][i][j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xres, (int)off, 0, 0));
       }
   };
-  auto load_all = [&] {
-#pragma unroll
-    for (int d = 0; d < D; ++d) load(d);
-  };
-  if constexpr (XL) stage_x(lds, xres, mrows, K, load_all);
-  else load_all();
 
-  f32x4_t acc[MT][NT];
+  f32x4_t acc[MT][GB];
   auto clear = [&] {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) acc[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int t = 0; t < GB; ++t) acc[i][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   };
-  auto multiply = [&](int d, int h, int k0) {  // half h of the piece in slot d; k0: its first code
-    u32x4 xf[MT][4];
+  u32x4 xf[MT][4];
+  auto turn_x = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (XL) {
-          xf[i][j] = lds[xrow[i] * stride + (k0 + XG * g + XJ * j) / 8];
-        } else {
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) xf[i][j][q] = from(4 * c + g, xv[h][i][j][q]);
-        }
-      }
+        for (int q = 0; q < 4; ++q) xf[i][j][q] = from_lane(4 * c + g, xv[buf][i][j][q]);
+  };
+  auto multiply = [&](int t, int h) {  // half h of tile t's piece
+    u32x4 words;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      u32x4 words;
+    for (int q = 0; q < 4; ++q) words[q] = from_lane(4 * c + g, wt.codes[t][h][q]);
+    words = transposed(words);
+    float s[128 / G];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) words[q] = from(4 * c + g, wt.codes[d][t][h][q]);
-      if constexpr (!kAsLoaded) words = transposed(words);
-      float s[128 / G];
+    for (int q = 0; q < 128 / G; ++q) s[q] = u2f(from_lane(4 * c + q * (G / 32), f2u(wt.scale[t][h])));
+    f32x4_t part[MT];
 #pragma unroll
-      for (int q = 0; q < 128 / G; ++q) s[q] = u2f(from(4 * c + q * (G / 32), f2u(wt.scale[d][t][h])));
-      f32x4_t part[MT];
+    for (int j = 0; j < 4; ++j) {
+      const bool first = (32 * j) % G == 0, done = (32 * j + 32) % G == 0;
+      const u32x4 wf = operand<XT>(words[j]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool first = (32 * j) % G == 0, done = (32 * j + 32) % G == 0;
-        const u32x4 wf = operand<XT>(words[j]);
+      for (int i = 0; i < MT; ++i) {
+        part[i] = mfma<XT>(xf[i][j], wf, first ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part[i]);
+        if (done) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          part[i] = mfma<XT>(xf[i][j], wf, first ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part[i]);
-          if (done) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][t][e] = __builtin_fmaf(part[i][e], s[32 * j / G], acc[i][t][e]);
-          }
+          for (int e = 0; e < 4; ++e) acc[i][t][e] = __builtin_fmaf(part[i][e], s[32 * j / G], acc[i][t][e]);
         }
       }
     }
@@ -401,10 +490,8 @@ __global__ void __launch_bounds__(kGemmThreads)
 
   // ---- the waves' sums, in the order of the waves; D element e of lane (c, g): row
   // 4 g + e of x, weight row c
-  float* const sums = reinterpret_cast<float*>(lds + (XL ? mrows * stride : 0));
-  int group = blockIdx.x, round = 0, turn = 0;
-  auto finish = [&] {
-    float* const part = sums + turn * (kWaves * mrows * 16 * NT);
+  float* const sums = reinterpret_cast<float*>(lds);
+  auto finish = [&](int group) {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -412,109 +499,214 @@ __global__ void __launch_bounds__(kGemmThreads)
         const int m = 16 * i + 4 * g + e;
         if (m < mrows)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) part[(wave * mrows + m) * (16 * NT) + 16 * t + c] = acc[i][t][e];
+          for (int t = 0; t < GB; ++t) sums[(wave * mrows + m) * (16 * GB) + 16 * t + c] = acc[i][t][e];
       }
     __syncthreads();
-    const int64_t n0 = (int64_t)group * (16 * NT);
-    for (int o = threadIdx.x; o < mrows * 16 * NT; o += kGemmThreads) {
-      const int m = o / (16 * NT), n = o % (16 * NT);
+    const int64_t n0 = (int64_t)group * (16 * GB);
+    for (int o = threadIdx.x; o < mrows * 16 * GB; o += kGemmThreads) {
+      const int m = o / (16 * GB), n = o % (16 * GB);
       float v = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) v += part[w * mrows * (16 * NT) + o];
+      for (int w = 0; w < kWaves; ++w) v += sums[w * mrows * (16 * GB) + o];
       if (n0 + n < N) y[(m0 + m) * N + n0 + n] = 16.0f * v;
     }
-    turn ^= 1;  // the next group's sums go beside these, which may still be read
+    __syncthreads();  // the next group's sums go where these are
     clear();
   };
 
-  clear();
-  if constexpr (XL) __syncthreads();
-  else read_x(0, wave * kPiece);
-  // The D steps have one way out, after the last: with one after each the compiler
-  // waits for all loads in every turn.  Steps past the last group multiply zeros.
-  do {
+  int group = blockIdx.x, round = 0, k0 = wave * kPiece;
+  wt.turn_to(group);
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      const int k0 = (round * kWaves + wave) * kPiece;
-      if constexpr (XL) {
-        if (k0 < kk) multiply(d, 0, k0), multiply(d, 1, k0 + 128);
-      } else {
-        read_x(1, k0 + 128);
-        if (k0 < kk) multiply(d, 0, k0);
-        read_x(0, round + 1 == rounds ? wave * kPiece : k0 + kWaves * kPiece);
-        if (k0 < kk) multiply(d, 1, k0 + 128);
+  for (int b = 0; b < XB; ++b) read_x(b, k0 + 128 * b);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int t = 0; t < GB; ++t) wt.load(t, h, t, (uint32_t)k0);
+  clear();
+  do {
+    const bool last = round + 1 == rounds;
+    const int next = last ? wave * kPiece : k0 + kWaves * kPiece;
+    if (last) wt.turn_to(group + gridDim.x);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      turn_x(h % XB);
+      read_x(h % XB, XB == 2 ? next + 128 * h : h == 0 ? k0 + 128 : next);
+#pragma unroll
+      for (int t = 0; t < GB; ++t) {
+        if (k0 + 128 * h < sl.count) multiply(t, h);
+        wt.load(t, h, t, (uint32_t)next);
       }
-      load(d);
-      if (++round == rounds) {
-        if (group < groups) finish();
-        round = 0;
-        group += gridDim.x;
-      }
+    }
+    k0 = next;
+    ++round;
+    if (last) {
+      finish(group);
+      round = 0;
+      group += gridDim.x;
     }
   } while (group < groups);
 }
 
-using Int4Kernel = void (*)(const uint16_t*, const uint8_t*, const float*, int64_t, int64_t, int64_t, int, int, float*);
-
-template <int XT, int MT, int NT, int D, bool XL>
-Int4Kernel int4_kernel_for(int G) {
-  return G == 128  ? &k_int4_rows<XT, MT, NT, D, 128, XL>
-         : G == 64 ? &k_int4_rows<XT, MT, NT, D, 64, XL>
-                   : &k_int4_rows<XT, MT, NT, D, 32, XL>;
-}
-template <int XT>
-Int4Kernel int4_few_kernel(int few) {
-  return few == 1   ? &k_int4_few<XT, 1, 2>
-         : few == 2 ? &k_int4_few<XT, 2, 2>
-                    : &k_int4_few<XT, 4, 2>;
-}
-template <int XT>
-Int4Kernel int4_kernel(bool xl, int MT, int NT, int G) {
-  if (xl) return MT == 1 ? int4_kernel_for<XT, 1, 1, 2, true>(G) : int4_kernel_for<XT, 2, 1, 2, true>(G);
-  if (MT == 1) return NT == 1 ? int4_kernel_for<XT, 1, 1, 3, false>(G) : int4_kernel_for<XT, 1, 2, 2, false>(G);
-  return NT == 1 ? int4_kernel_for<XT, 2, 1, 3, false>(G) : int4_kernel_for<XT, 2, 2, 2, false>(G);
+// The slices' sums, in the order of the slices.  16 rows of 6,144 columns, 2 slices: 2 us.
+constexpr int kJoinThreads = 256;
+__global__ void __launch_bounds__(kJoinThreads)
+    k_int4_join(const float* __restrict__ planes, int64_t n, int count, float* __restrict__ y) {
+  const int64_t i = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
+  if (i >= n) return;
+  float v = 0.0f;
+  for (int z = 0; z < count; ++z) v += planes[z * n + i];
+  y[i] = v;
 }
 
-constexpr int64_t kInt4MaxK = 1 << 22;  // 32 rows of x and 16 of codes stay below 2^31 bytes
+using Int4Kernel = void (*)(const uint16_t*, const uint8_t*, const float*, int64_t, int64_t, int64_t, int, int, int,
+                            float*);
+
+template <int XT>
+Int4Kernel int4_few_kernel(int MR) {
+  return MR == 1 ? &k_int4_few<XT, 1, 2> : MR == 2 ? &k_int4_few<XT, 2, 2> : &k_int4_few<XT, 4, 2>;
+}
+template <int XT>
+Int4Kernel int4_lds_kernel(int G) {
+  return G == 128 ? &k_int4_lds<XT, 2, 128> : G == 64 ? &k_int4_lds<XT, 2, 64> : &k_int4_lds<XT, 2, 32>;
+}
+template <int XT, int MT, int GB>
+Int4Kernel int4_regs_kernel_for(int G) {
+  return G == 128  ? &k_int4_regs<XT, MT, GB, 128>
+         : G == 64 ? &k_int4_regs<XT, MT, GB, 64>
+                   : &k_int4_regs<XT, MT, GB, 32>;
+}
+template <int XT, int GB>
+Int4Kernel int4_regs_kernel_of(int MT, int G) {
+  return MT == 1   ? int4_regs_kernel_for<XT, 1, GB>(G)
+         : MT == 2 ? int4_regs_kernel_for<XT, 2, GB>(G)
+                   : int4_regs_kernel_for<XT, 4, GB>(G);
+}
+template <int XT>
+Int4Kernel int4_regs_kernel(int MT, int GB, int G) {
+  return GB == 1   ? int4_regs_kernel_of<XT, 1>(MT, G)
+         : GB == 2 ? int4_regs_kernel_of<XT, 2>(MT, G)
+                   : int4_regs_kernel_of<XT, 3>(MT, G);
+}
+
+constexpr int64_t kInt4MaxK = 1 << 22;  // 64 rows of x and 48 of codes stay below 2^31 bytes
 constexpr int64_t kLds = 160 * 1024, kCus = 256;
+
+// How a product is cut.
+enum class Int4Way { few, lds, regs };
+struct Int4Plan {
+  Int4Way way;
+  int MR, MT, GB;        // few: rows of sums; regs: 16-row tiles of x, tiles of the weight
+  int64_t each, slices;  // of K
+  int64_t groups, grid, mgroups, lds;
+};
+
+// codes of a slice where there are `slices` at most
+inline int64_t slice_of(int64_t K, int64_t slices) {
+  const int64_t each = ((K + slices - 1) / slices + kPiece - 1) / kPiece * kPiece;
+  return each < kPiece ? kPiece : each;
+}
+
+// Up to 4 rows k_int4_few; up to 16 and more than two tiles a CU k_int4_lds, whose
+// reads of x cost least once its LDS is filled (5 rows, 50,001 x 6,144: 35 us, k_int4_regs
+// 52; 16 rows, 24,576 x 4,096: 16 and 19; but 16 rows, 6,144 x 6,144: 14 and 9).  Both
+// take x in slices where it is too long for LDS.  Else k_int4_regs.
+inline Int4Plan int4_plan(int64_t M, int64_t N, int64_t K) {
+  Int4Plan p{};
+  const int64_t tiles = (N + 15) / 16;
+  p.MR = M <= 2 ? (int)M : 4;
+  p.MT = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  p.GB = 1, p.mgroups = 1, p.slices = 1;
+  p.way = M <= 4 ? Int4Way::few : M <= 16 && tiles > 2 * kCus ? Int4Way::lds : Int4Way::regs;
+  if (p.way != Int4Way::regs) {
+    const int64_t sums = 2 * kWaves * 4 * (p.way == Int4Way::few ? few_sums(p.MR) : 16 * M);
+    auto lds_of = [&](int64_t k) { return M * x_stride(k) * 16 + sums; };
+    // slices: the largest that fit; with up to 4 rows two workgroups a CU (3 rows, 4,096 x
+    // 49,152: 34 us, 44 with one; 16 rows, 24,576 x 6,144: 31, with one 27)
+    const int64_t most = p.way == Int4Way::few && lds_of(K) > kLds ? kLds / 2 : kLds;
+    while (lds_of(slice_of(K, p.slices)) > most) ++p.slices;
+    p.each = slice_of(K, p.slices);
+    p.lds = lds_of(p.each);
+    p.groups = tiles;
+    // as many workgroups as are resident at once, each with all slices' share
+    const int64_t room = (p.lds <= kLds / 2 ? 2 : 1) * kCus;
+    p.grid = room / p.slices > 1 ? room / p.slices : 1;
+  } else {
+    p.mgroups = (M + 16 * p.MT - 1) / (16 * p.MT);
+    // The least load of the busiest CU, in quarters of a tile's code: a workgroup's tiles
+    // and its reads of x (3/4 of a tile's time for 16 rows), for its codes and 1,024 more
+    // to begin and end; slices cost the second launch, and their sums' bytes.  Of the
+    // choices tried at 96 sizes (8 to 64 rows, 1,000 to 40,000 x 2,048 to 24,576) it takes
+    // the fastest or one within 10% of it at 89, within 26% at all.  16 rows, 6,144 x
+    // 24,576: 30 us by two slices of 3 tiles, 47 by single tiles.
+    double least = 0;
+    for (int GB = 3; GB >= 1; --GB)
+      for (int64_t S = 1; S == 1 || (S <= 16 && S <= K / 2048); ++S) {
+        const double wgs = (double)((tiles + GB - 1) / GB) * (double)(p.mgroups * S);
+        const double load = __builtin_ceil(wgs / kCus) * (double)(slice_of(K, S) + 1024) * (4 * GB + 3 * p.MT) +
+                            (S > 1 ? 49152.0 + (double)M * (double)N * (double)S / 64 : 0.0);
+        if (least == 0 || load < least) least = load, p.GB = GB, p.slices = S;
+      }
+    p.each = slice_of(K, p.slices);
+    p.groups = (tiles + p.GB - 1) / p.GB;
+    p.grid = (p.MT == 1 ? 2 : 1) * kCus;
+    p.lds = kWaves * 16 * 4 * (M < 16 * p.MT ? M : 16 * p.MT) * p.GB;
+  }
+  if (p.grid > p.groups) p.grid = p.groups;
+  p.slices = K ? (K + p.each - 1) / p.each : 1;
+  return p;
+}
+
+inline bool int4_sizes_ok(int64_t M, int64_t N, int64_t K) {
+  return M >= 0 && N >= 0 && K >= 0 && K % 64 == 0 && K <= kInt4MaxK && M <= 64 * 65535 && N <= INT64_MAX / 16 / (K + 1) &&
+         (N + 15) / 16 <= kMaxGrid / 2 && (M == 0 || N <= INT64_MAX / 1024 / M);
+}
 
 }  // namespace
 }  // namespace zq
 
-extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, const float* scales, int64_t M,
-                                    int64_t N, int64_t K, int32_t block, float* y, void* stream) {
+extern "C" int64_t zq_int4_dequant_gemm_bytes(int64_t M, int64_t N, int64_t K) {
   using namespace zq;
-  if (M < 0 || N < 0 || K < 0 || K % 64 != 0 || K > kInt4MaxK) return ZQ_E_SIZE;
+  if (!int4_sizes_ok(M, N, K)) return -1;
+  if (M == 0 || N == 0) return 0;
+  const Int4Plan p = int4_plan(M, N, K);
+  return p.slices == 1 ? 0 : 4 * M * N * p.slices;
+}
+
+extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, const float* scales, int64_t M,
+                                    int64_t N, int64_t K, int32_t block, float* y, void* workspace,
+                                    int64_t workspace_bytes, void* stream) {
+  using namespace zq;
+  if (!int4_sizes_ok(M, N, K)) return ZQ_E_SIZE;
   const int lgB = log2_block(block);
   if (lgB < 0) return ZQ_E_BLOCK;
   if (xt != ZQ_BF16 && xt != ZQ_F16) return ZQ_E_DTYPE;
   if (M == 0 || N == 0) return ZQ_OK;
-  if (!y || (K > 0 && (!x || !packed || !scales))) return ZQ_E_NULL;
-  if (!aligned(x, 16) || !aligned(packed, 16) || !aligned(scales, 4) || !aligned(y, 4)) return ZQ_E_ALIGN;
-  if (N > INT64_MAX / 8 / (K + 1) || M > INT64_MAX / 8 / (K + 1) || M > INT64_MAX / 8 / N) return ZQ_E_SIZE;
-  if (any_overlap({{y, 4 * M * N}}, {{x, 2 * M * K}, {packed, N * K / 2}, {scales, 4 * num_scales(N * K, block)}}))
+  const int64_t need = zq_int4_dequant_gemm_bytes(M, N, K);
+  if (workspace_bytes < need) return ZQ_E_SIZE;
+  if (!y || (need > 0 && !workspace) || (K > 0 && (!x || !packed || !scales))) return ZQ_E_NULL;
+  if (!aligned(x, 16) || !aligned(packed, 16) || !aligned(scales, 4) || !aligned(y, 4) ||
+      (need > 0 && !aligned(workspace, 4)))
+    return ZQ_E_ALIGN;
+  if (any_overlap({{y, 4 * M * N}, {workspace, need}},
+                  {{x, 2 * M * K}, {packed, N * K / 2}, {scales, 4 * num_scales(N * K, block)}}))
     return ZQ_E_ALIAS;
 
-  const int MT = M <= 16 ? 1 : 2;
-  const int64_t mrows = M < 16 * MT ? M : 16 * MT, mgroups = (M + 16 * MT - 1) / (16 * MT);
+  const Int4Plan p = int4_plan(M, N, K);
   // codes under one scale: 128 from a multiple of 128 on lie in one block only where
   // rows start at multiples of 128
   const int G = block >= 128 && K % 128 == 0 ? 128 : block >= 64 ? 64 : 32;
-  // x in LDS where it leaves room for the waves' sums
-  const int few = M <= 2 ? (int)M : M <= 4 ? 4 : 0;
-  const int64_t xbytes = mrows * (pieces_of(K) * (kPiece / 8) + 1) * 16;
-  const int64_t sbytes = few ? few_buffers(few) * kWaves * few_sums(few) * 4 : 2 * kWaves * 16 * mrows * 4;
-  const bool xl = xbytes + sbytes <= kLds;
-  const int64_t tiles = (N + 15) / 16;
-  const int NT = xl || tiles <= 512 ? 1 : 2;
-  const int64_t groups = (tiles + NT - 1) / NT;
-  if (groups > kMaxGrid / 2 || mgroups > 65535) return ZQ_E_SIZE;
-  const int64_t lds = xl ? xbytes + sbytes : 2 * kWaves * 16 * 4 * mrows * NT;
-  // x in LDS: as many workgroups as are resident at once
-  const int64_t room = (lds <= kLds / 2 ? 2 : 1) * kCus, grid = xl && groups > room ? room : groups;
-  const Int4Kernel k = xl && few ? (xt == ZQ_BF16 ? int4_few_kernel<ZQ_BF16>(few) : int4_few_kernel<ZQ_F16>(few))
-                                 : (xt == ZQ_BF16 ? int4_kernel<ZQ_BF16>(xl, MT, NT, G) : int4_kernel<ZQ_F16>(xl, MT, NT, G));
-  return launch_grid(k, dim3((unsigned)grid, (unsigned)mgroups), (unsigned)kGemmThreads, (unsigned)lds,
-                     static_cast<hipStream_t>(stream), static_cast<const uint16_t*>(x), packed, scales, M, N, K, lgB,
-                     (int)groups, y);
+  const bool bf = xt == ZQ_BF16;
+  const Int4Kernel k = p.way == Int4Way::few   ? (bf ? int4_few_kernel<ZQ_BF16>(p.MR) : int4_few_kernel<ZQ_F16>(p.MR))
+                       : p.way == Int4Way::lds ? (bf ? int4_lds_kernel<ZQ_BF16>(G) : int4_lds_kernel<ZQ_F16>(G))
+                                               : (bf ? int4_regs_kernel<ZQ_BF16>(p.MT, p.GB, G)
+                                                     : int4_regs_kernel<ZQ_F16>(p.MT, p.GB, G));
+  const int64_t joins = grid_for(M * N, kJoinThreads);
+  if (p.slices > 1 && joins == 0) return ZQ_E_SIZE;
+  const auto st = static_cast<hipStream_t>(stream);
+  float* const out = p.slices > 1 ? static_cast<float*>(workspace) : y;
+  const int rc = launch_grid(k, dim3((unsigned)p.grid, (unsigned)p.mgroups, (unsigned)p.slices), (unsigned)kGemmThreads,
+                             (unsigned)p.lds, st, static_cast<const uint16_t*>(x), packed, scales, M, N, K, (int)p.each,
+                             lgB, (int)p.groups, out);
+  if (rc != ZQ_OK || p.slices == 1) return rc;
+  return launch(&k_int4_join, (unsigned)joins, (unsigned)kJoinThreads, st, out, M * N, (int)p.slices, y);
 }

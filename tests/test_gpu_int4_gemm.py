@@ -46,6 +46,11 @@ CASES = [(1, 1, 64, 32), (1, 15, 64, 1024), (2, 17, 128, 64), (3, 33, 192, 128),
          (15, 65, 4160, 128), (16, 100, 6208, 256), (16, 64, 2048, 32), (16, 31, 12352, 512), (17, 100, 704, 128),
          (31, 77, 2240, 64), (32, 128, 4096, 128), (33, 50, 960, 32), (48, 96, 6144, 256), (63, 40, 1600, 128),
          (64, 200, 2048, 64), (65, 33, 1024, 128), (130, 90, 576, 256), (2, 6145, 512, 128), (9, 50001, 128, 128)]
+# weight rows that share x in groups of one, two and three tiles, and more groups than run at
+# once; a K summed in slices, the last one shorter
+CASES += [(1, 16400, 192, 64), (5, 8320, 448, 128), (16, 8208, 5440, 64), (12, 8210, 576, 32), (4, 40, 24576, 128),
+          (2, 24, 49152, 32), (9, 4500, 64, 32), (20, 4300, 320, 128), (40, 4300, 192, 64), (24, 8300, 320, 128),
+          (50, 8300, 256, 256), (64, 12400, 128, 32), (10, 40, 24576, 128), (33, 70, 16448, 64), (20, 100, 14400, 32)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
@@ -109,6 +114,63 @@ def test_special_values():
     assert got[rows][:, 7].eq(0).all() and got[rows][:, 9].eq(0).all()
     assert got[rows][:, 11].eq(float("inf")).all() and got[rows][:, 13].isnan().all()
     assert got[rows][:, 15].eq(512 * 2.0**100).all() and got[rows][:, 17].eq(7 * 512 * 2.0**-126).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 24576), (12, 8320, 512), (12, 8320, 8192), (12, 40, 24576), (40, 4300, 512)])
+def test_special_rows(M, N, K):
+    """NaN and infinities of x stay in their rows, those of scales in their columns,
+    whichever way the product is cut."""
+    packed, scales, _ = weight(N, K, 128, 4, True)
+    packed.view(N, K // 2)[17] = 0x11
+    s = scales.view(N, K // 128)
+    s[17] = 1.0
+    s[19, 1], s[N - 1] = float("nan"), 0.0
+    x = torch.ones(M, K, dtype=torch.bfloat16)
+    x[1, K - 1], x[2, 200] = float("nan"), float("inf")
+    got = zq.int4_dequant_gemm(x.to(DEV), packed, scales, N, 128).cpu()
+    rows = [m for m in range(M) if m not in (1, 2)]
+    assert bool(got[1].isnan().all()) and math_nan(got[2, N - 1])
+    assert bool(got[:, 19].isnan().all())
+    assert bool(got[rows][:, [n for n in range(N) if n != 19]].isfinite().all())
+    assert bool(got[rows][:, 17].eq(K).all()) and bool(got[rows][:, N - 1].eq(0).all()) and got[2, 17] == float("inf")
+
+
+@pytest.mark.parametrize("M", [16, 31])
+def test_slices_of_three_tiles(M):
+    """A weight of many rows and a long K, against 64-bit products on the GPU."""
+    N, K, block = 5003, 20544, 64
+    assert zq.int4_dequant_gemm_bytes(M, N, K) > 0
+    g = torch.Generator(device=DEV).manual_seed(M)
+    packed = torch.randint(0, 256, (N * K // 2,), dtype=torch.uint8, device=DEV, generator=g)
+    scales = torch.rand(N * K // block, device=DEV, generator=g) * 1e-2
+    x = torch.randn(M, K, device=DEV, generator=g).bfloat16()
+    got = zq.int4_dequant_gemm(x, packed, scales, N, block).double()
+    for n in range(0, N, 500):
+        b = packed.view(N, K // 2)[n:n + 500]
+        q = (torch.stack((b & 15, b >> 4), -1).view(len(b), K).to(torch.int8) ^ 8) - 8
+        w = (q.double().view(len(b), -1, block) * scales.view(N, -1)[n:n + 500, :, None].double()).view(len(b), K)
+        far = (got[:, n:n + 500] - x.double() @ w.t()).abs()
+        assert bool((far <= (K + 64) * 2.0**-23 * (x.double().abs() @ w.abs().t())).all())
+
+
+def test_workspace():
+    """Given, it is used; too small, it is refused; what it held does not count."""
+    M, N, K, block = 7, 33, 24576, 128
+    need = zq.int4_dequant_gemm_bytes(M, N, K)
+    assert need > 0 and zq.int4_dequant_gemm_bytes(M, N, 64) == 0
+    packed, scales, _ = weight(N, K, block, 3, False)
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(1)).half().to(DEV)
+    want = zq.int4_dequant_gemm(x, packed, scales, N, block)
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    assert torch.equal(zq.int4_dequant_gemm(x, packed, scales, N, block, workspace=ws), want)
+    assert bool((ws[need:] == 0xFF).all())
+    with pytest.raises(ValueError):
+        zq.int4_dequant_gemm(x, packed, scales, N, block, workspace=ws[:need - 1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = zq.int4_dequant_gemm(x, packed, scales, N, block, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
 
 
 def math_nan(v):

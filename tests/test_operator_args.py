@@ -12,6 +12,7 @@ import paper_2501_04266_amd as zq
 from paper_2501_04266_amd import _lib
 
 A, B, C, W = 0x7F0000000000, 0x7F0010000000, 0x7F0020000000, 0x7F0030000000
+V = 0x7F0040000000
 NULL, ALIGN, SIZE, BLOCK, DTYPE, ALIAS = -1, -4, -5, -2, -3, -8
 
 
@@ -161,8 +162,8 @@ def test_grad_plan_and_call_errors(L):
 
 
 def test_int4_gemm_argument_errors(L):
-    f = L.zq_int4_dequant_gemm
-    # (x, xt, packed, scales, M, N, K, block, y, stream)
+    def f(*a):  # (x, xt, packed, scales, M, N, K, block, y, stream)
+        return L.zq_int4_dequant_gemm(*a[:-1], None, 0, a[-1])
     assert f(A, 0, B, C, 4, 4, 64, 128, W, None) == DTYPE
     assert f(A, 2, B, C, 4, 4, 96, 128, W, None) == SIZE
     assert f(A, 2, B, C, 4, 4, (1 << 22) + 64, 128, W, None) == SIZE
@@ -176,6 +177,17 @@ def test_int4_gemm_argument_errors(L):
     assert f(A, 2, B, C, 4, 4, 64, 128, A + 508, None) == ALIAS and f(A, 2, B, C, 4, 4, 64, 128, B + 124, None) == ALIAS
     assert f(A, 2, B, C, 4, 4, 64, 128, C + 4, None) == ALIAS
     assert f(None, 2, None, None, 0, 4, 64, 128, None, None) == 0 and f(None, 2, None, None, 4, 0, 64, 128, None, None) == 0
+
+
+def test_int4_gemm_workspace(L):
+    f, need = L.zq_int4_dequant_gemm, L.zq_int4_dequant_gemm_bytes(8, 32, 24576)
+    assert need > 0 and need % (4 * 8 * 32) == 0 and L.zq_int4_dequant_gemm_bytes(8, 32, 64) == 0
+    args = (A, 2, B, C, 8, 32, 24576, 128, W)
+    assert f(*args, None, 0, None) == SIZE and f(*args, V, need - 1, None) == SIZE and f(*args, None, need, None) == NULL
+    assert f(*args, V + 2, need, None) == ALIGN and f(*args, A, need, None) == ALIAS and f(*args, W, need, None) == ALIAS
+    for bad in ((-1, 4, 64), (4, -1, 64), (4, 4, 65), (4, 4, -64), (1 << 40, 4, 64), (4, 1 << 60, 64)):
+        assert L.zq_int4_dequant_gemm_bytes(*bad) == -1
+    assert L.zq_int4_dequant_gemm_bytes(0, 4, 64) == 0 and L.zq_int4_dequant_gemm_bytes(4, 0, 64) == 0
 
 
 def test_binding_refusals():
