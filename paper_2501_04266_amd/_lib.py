@@ -122,6 +122,15 @@ def _need(t, name, count, dtypes):
         raise ValueError(f"{name} holds {t.numel()} elements; {count} needed")
 
 
+def _ptr(t, name, count, dtypes):
+    """The address of a buffer that passes _need and _dev, checked in one go (0.3 us a
+    buffer, 0.5 by the two); else what _need raises, or None: left to _dev, once the
+    other buffers' sizes are checked."""
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.numel() >= count and t.is_contiguous()):
+        return t.data_ptr()
+    _need(t, name, count, dtypes)
+
+
 def _nsc(n, block):
     """Scales needed for n elements; 0 for a block the library will reject
     itself (ZQ_E_BLOCK), so that error is reported as the library's."""
@@ -140,6 +149,7 @@ _I8 = (torch.int8,)
 _U8 = (torch.uint8,)
 _F32 = (torch.float32,)
 _IDS = tuple(_ID_DT)
+_HALF = (torch.bfloat16, torch.float16)
 
 
 def _check(status, what):
@@ -348,13 +358,14 @@ def embedding(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
         raise ValueError("table must be 2-D [V, D]")
     V, D = table.shape
     T = ids.numel()
-    _need(ids, "ids", T, _IDS)
-    _need(table, "table", V * D, _ELEM)
+    ids_at = _ptr(ids, "ids", T, _IDS)
+    table_at = _ptr(table, "table", V * D, _ELEM)
     if out is None:
         out = torch.empty((*ids.shape, D), dtype=out_dtype or table.dtype, device=ids.device)
-    _need(out, "out", T * D, _ELEM)
-    _check(lib().zq_embedding(_dev(ids, "ids"), _ID_DT[ids.dtype], T, _dev(table, "table"), _TORCH_DT[table.dtype], V,
-                              D, scale, _dev(out, "out"), _TORCH_DT[out.dtype], _stream(stream)), "embedding")
+    out_at = _ptr(out, "out", T * D, _ELEM)
+    _check(lib().zq_embedding(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, table_at or _dev(table, "table"),
+                              _TORCH_DT[table.dtype], V, D, scale, out_at or _dev(out, "out"), _TORCH_DT[out.dtype],
+                              _stream(stream)), "embedding")
     return out
 
 
@@ -363,15 +374,15 @@ def qwz_embedding(ids, codes, scales, V, D, block=256, scale=1.0, out_dtype=torc
     [ceil(V*D/block)], as gathered): only the rows that occur are read and
     dequantised.  With scale 1 they are the rows qwz_dequantize writes."""
     T = ids.numel()
-    _need(ids, "ids", T, _IDS)
-    _need(codes, "codes", V * D, _I8)
-    _need(scales, "scales", _nsc(V * D, block), _F32)
+    ids_at = _ptr(ids, "ids", T, _IDS)
+    codes_at = _ptr(codes, "codes", V * D, _I8)
+    scales_at = _ptr(scales, "scales", _nsc(V * D, block), _F32)
     if out is None:
         out = torch.empty((*ids.shape, D), dtype=out_dtype, device=ids.device)
-    _need(out, "out", T * D, _ELEM)
-    _check(lib().qwz_embedding(_dev(ids, "ids"), _ID_DT[ids.dtype], T, _dev(codes, "codes"), _dev(scales, "scales"), V,
-                               D, block, scale, _dev(out, "out"), _TORCH_DT[out.dtype], _stream(stream)),
-           "qwz_embedding")
+    out_at = _ptr(out, "out", T * D, _ELEM)
+    _check(lib().qwz_embedding(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, codes_at or _dev(codes, "codes"),
+                               scales_at or _dev(scales, "scales"), V, D, block, scale, out_at or _dev(out, "out"),
+                               _TORCH_DT[out.dtype], _stream(stream)), "qwz_embedding")
     return out
 
 
@@ -525,19 +536,19 @@ def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, workspace=None, s
     if x.dim() != 2:
         raise ValueError("x must be 2-D [M, K]")
     M, K = x.shape
-    _need(x, "x", M * K, (torch.bfloat16, torch.float16))
-    _need(packed, "packed", int4_bytes(N * K), _U8)
-    _need(scales, "scales", _nsc(N * K, block), _F32)
+    x_at = _ptr(x, "x", M * K, _HALF)
+    packed_at = _ptr(packed, "packed", int4_bytes(N * K), _U8)
+    scales_at = _ptr(scales, "scales", _nsc(N * K, block), _F32)
     if y is None:
         y = torch.empty((M, N), dtype=torch.float32, device=x.device)
-    else:
-        _need(y, "y", M * N, _F32)
+    y_at = _ptr(y, "y", M * N, _F32)
     need = lib().zq_int4_dequant_gemm_bytes(M, N, K)
     if workspace is None and need > 0:
         workspace = _workspace(need, x.device, stream)
     at, size = (0, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel())
     if workspace is not None:
         _need(workspace, "workspace", max(need, 0), _U8)
-    _check(lib().zq_int4_dequant_gemm(_dev(x, "x"), _TORCH_DT[x.dtype], _dev(packed, "packed"), _dev(scales, "scales"),
-                                      M, N, K, block, _dev(y, "y"), at, size, _stream(stream)), "int4_dequant_gemm")
+    _check(lib().zq_int4_dequant_gemm(x_at or _dev(x, "x"), _TORCH_DT[x.dtype], packed_at or _dev(packed, "packed"),
+                                      scales_at or _dev(scales, "scales"), M, N, K, block, y_at or _dev(y, "y"), at,
+                                      size, _stream(stream)), "int4_dequant_gemm")
     return y
