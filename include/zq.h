@@ -77,8 +77,7 @@ enum {
   ZQ_E_SIZE = -5,   /* negative element count, or a size the call does not take */
   ZQ_E_P = -6,      /* slice count outside [1, 1024] */
   ZQ_E_HIP = -7,    /* HIP kernel launch failed */
-  ZQ_E_ALIAS = -8,  /* an output overlaps an input or another output */
-  ZQ_E_MEMORY = -9  /* no host memory (zq_grad_plan_make) */
+  ZQ_E_ALIAS = -8   /* an output overlaps an input or another output */
 };
 
 /* qwZ quantiser (Background, ZeRO++: quantise the weight shard to INT8 blocks

@@ -16,7 +16,7 @@ LIB_PATH = os.environ.get("ZQ_LIBRARY") or os.path.join(_PKG, "libzq.so")
 ZQ_F32, ZQ_F16, ZQ_BF16 = 0, 1, 2
 ZQ_I32, ZQ_I64, ZQ_INT4 = 3, 4, 5
 STATUS = {0: "ZQ_OK", -1: "ZQ_E_NULL", -2: "ZQ_E_BLOCK", -3: "ZQ_E_DTYPE", -4: "ZQ_E_ALIGN",
-          -5: "ZQ_E_SIZE", -6: "ZQ_E_P", -7: "ZQ_E_HIP", -8: "ZQ_E_ALIAS", -9: "ZQ_E_MEMORY"}
+          -5: "ZQ_E_SIZE", -6: "ZQ_E_P", -7: "ZQ_E_HIP", -8: "ZQ_E_ALIAS"}
 EXPORTS = ["qwz_quantize", "qwz_dequantize", "qgz_quantize", "qgz_reduce_level", "qgz_dequantize",
            "qgz_reduce_dequantize", "qgz_reduce_level_gather", "qgz_reduce_level_gather_noalloc",
            "qwz_dequant_gemm", "zq_embedding", "qwz_embedding", "zq_embedding_grad", "zq_embedding_grad_bytes",

@@ -278,11 +278,10 @@ const char* zq_status_string(int status) {
     case ZQ_E_BLOCK: return "block must be a power of two in [32, 1024]";
     case ZQ_E_DTYPE: return "unknown dtype";
     case ZQ_E_ALIGN: return "misaligned pointer (elements/codes 16 B, scales 4 B)";
-    case ZQ_E_SIZE: return "negative size, or a size the call does not take";
+    case ZQ_E_SIZE: return "negative size";
     case ZQ_E_P: return "slice count outside [1, 1024]";
     case ZQ_E_HIP: return "HIP launch failed";
     case ZQ_E_ALIAS: return "an output overlaps an input";
-    case ZQ_E_MEMORY: return "no host memory";
     default: return "unknown status";
   }
 }

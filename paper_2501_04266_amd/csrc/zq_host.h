@@ -24,23 +24,18 @@ inline int64_t grid_for(int64_t units, int64_t units_per_wg) {
   return g > kMaxGrid ? 0 : g;
 }
 
-// Launch with the kernel's exact parameter types and `lds` bytes of dynamic LDS;
-// returns ZQ_E_HIP when the runtime rejects the launch.
+// Launch with the kernel's exact parameter types; returns ZQ_E_HIP when the
+// runtime rejects the launch.
 template <typename... KArgs, typename... Args>
-inline int launch_grid(void (*kern)(KArgs...), dim3 grid, unsigned block, unsigned lds, hipStream_t st,
-                       Args&&... args) {
+inline int launch(void (*kern)(KArgs...), unsigned grid, unsigned block, hipStream_t st, Args&&... args) {
   std::tuple<KArgs...> tup(std::forward<Args>(args)...);
   void* argv[sizeof...(KArgs)];
   std::apply([&](auto&... a) {
     int i = 0;
     ((argv[i++] = static_cast<void*>(&a)), ...);
   }, tup);
-  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kern), grid, dim3(block), argv, lds, st);
+  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3(grid), dim3(block), argv, 0, st);
   return e == hipSuccess ? ZQ_OK : ZQ_E_HIP;
-}
-template <typename... KArgs, typename... Args>
-inline int launch(void (*kern)(KArgs...), unsigned grid, unsigned block, hipStream_t st, Args&&... args) {
-  return launch_grid(kern, dim3(grid), block, 0u, st, std::forward<Args>(args)...);
 }
 
 inline int log2_block(int32_t block) {

@@ -703,10 +703,14 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
   const int64_t joins = grid_for(M * N, kJoinThreads);
   if (p.slices > 1 && joins == 0) return ZQ_E_SIZE;
   const auto st = static_cast<hipStream_t>(stream);
-  float* const out = p.slices > 1 ? static_cast<float*>(workspace) : y;
-  const int rc = launch_grid(k, dim3((unsigned)p.grid, (unsigned)p.mgroups, (unsigned)p.slices), (unsigned)kGemmThreads,
-                             (unsigned)p.lds, st, static_cast<const uint16_t*>(x), packed, scales, M, N, K, (int)p.each,
-                             lgB, (int)p.groups, out);
-  if (rc != ZQ_OK || p.slices == 1) return rc;
+  float* out = p.slices > 1 ? static_cast<float*>(workspace) : y;
+  const uint16_t* xs = static_cast<const uint16_t*>(x);
+  int each = (int)p.each, lg = lgB, groups = (int)p.groups;
+  void* args[] = {&xs, &packed, &scales, &M, &N, &K, &each, &lg, &groups, &out};
+  const hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(k),
+                                       dim3((unsigned)p.grid, (unsigned)p.mgroups, (unsigned)p.slices),
+                                       dim3(kGemmThreads), args, (size_t)p.lds, st);
+  if (e != hipSuccess) return ZQ_E_HIP;
+  if (p.slices == 1) return ZQ_OK;
   return launch(&k_int4_join, (unsigned)joins, (unsigned)kJoinThreads, st, out, M * N, (int)p.slices, y);
 }

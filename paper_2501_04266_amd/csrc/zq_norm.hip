@@ -9,7 +9,9 @@
 // sum is sum_b s_b^2 sum_{i in b} q_i^2, the inner sum in whole numbers (one
 // v_dot8_i32_i4 for 8 codes), and clipping it means scaling its scales.
 //
-// Bound by memory: each byte is read once (and, clipping, written once).  The
+// Bound by memory: each byte is read once (and, clipping, written once).  The norm
+// of 1.2 billion bf16 elements takes 360 us (6.7 TB/s), of 906 million INT4 codes 75
+// (6.4 TB/s); a second launch of 2 to 4 us adds the workgroups' sums.  The
 // squares are summed in binary64, exactly squared binary32 values, so neither
 // overflow nor underflow of a square is met and the order of the sums does not
 // show in the binary32 result except by one rounding; the order is fixed all
@@ -223,8 +225,8 @@ __global__ void __launch_bounds__(kNormThreads)
 
 // ---- clipping: a workgroup per piece of kClipElems elements.  Pieces are small and
 // workgroups start in their order, so that the result is written nearly in address
-// order (50 million bf16 elements into binary32: 51 us;
-// in 2,048 streams far apart, as the norm reads, 60).
+// order (50 million bf16 elements into binary32: 51 us, 5.9 TB/s; in 2,048 streams far
+// apart, as the norm reads, 60).
 constexpr int kClipElems = 4096;
 constexpr int kClipSteps = kClipElems / kNormThreads / 4;
 
@@ -441,8 +443,8 @@ using namespace zq;
 int zq_grad_plan_make(const zq_grad* grads, int32_t count, zq_grad_plan* plan) {
   try {
     return plan_table(grads, count, plan);
-  } catch (...) {  // no memory for the overlap check
-    return ZQ_E_MEMORY;
+  } catch (...) {  // more tensors than the host has memory to check for overlaps
+    return ZQ_E_SIZE;
   }
 }
 
