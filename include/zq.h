@@ -229,8 +229,8 @@ int qwz_embedding(const void* ids, zq_dtype it, int64_t T, const int8_t* codes, 
  *   dw[v][d] = cvt(fl(scale * sum_{t: ids[t] = v} dy[t][d]))   zeros where v does not occur
  * with accumulate != 0 added to what dw holds: dw[v][d] = cvt(fl(dw[v][d] + fl(scale *
  * sum))), rows that do not occur untouched.  Sums are taken in binary32 in an order that
- * follows from the ids alone (tokens ascending, 64s of them summed apart where a row has many), so
- * results are the same in every run.
+ * follows from the ids alone (tokens ascending; where a row has many, 64 at a time, and
+ * then these sums ascending), so results are the same in every run.
  *   dy [T][D] of dtype gt (read), dw [V][D] of dtype wt (written)
  *   workspace: device memory of zq_embedding_grad_bytes(T, V, D) bytes or more, 16-byte
  *   aligned, the call's own until it has run.  T, V <= 2^30 (ZQ_E_SIZE); a workspace
@@ -302,7 +302,8 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
  * The weight is not narrowed: the codes' products are exact and summed in binary32 by
  * the matrix cores, each scale multiplies its block's sum (or a part of it), and these
  * are added in binary32, in a fixed order: within (K + 64) * 2^-23 * sum_k |x w| of
- * the exact value, the same bits in every run.
+ * the exact value (where the scales are 2^-122 or more, or 0: the products with smaller
+ * ones can fall below the normal numbers), the same bits in every run.
  *   x       [M][K] row-major, xt = ZQ_BF16 or ZQ_F16 (read)
  *   packed  [ceil(N*K/2)] INT4 codes of the N x K weight, row-major, scales
  *           [ceil(N*K/block)] floats (read)
