@@ -396,6 +396,16 @@ def _workspace(nbytes, device, stream):
     return w
 
 
+def _given_workspace(workspace, need, device, stream):
+    """(address, bytes) of the caller's workspace, or of one for this call."""
+    if workspace is None:
+        if need <= 0:
+            return 0, 0
+        workspace = _workspace(need, device, stream)
+    _need(workspace, "workspace", max(need, 0), _U8)
+    return _dev(workspace, "workspace"), workspace.numel()
+
+
 def embedding_grad_bytes(T, V, D):
     """Bytes of workspace embedding_grad takes for T tokens and a V x D table."""
     n = lib().zq_embedding_grad_bytes(T, V, D)
@@ -413,23 +423,21 @@ def embedding_grad(ids, dy, V, scale=1.0, out_dtype=torch.float32, out=None, acc
     are.  workspace: uint8, embedding_grad_bytes(T, V, D) or more; allocated if not
     given."""
     T = ids.numel()
-    _need(ids, "ids", T, _IDS)
+    ids_at = _ptr(ids, "ids", T, _IDS)
     if dy.dim() < 1 or dy.numel() != T * dy.shape[-1]:
         raise ValueError(f"dy has shape {tuple(dy.shape)}; expected {(*ids.shape, 'D')}")
     D = dy.shape[-1]
-    _need(dy, "dy", T * D, _ELEM)
+    dy_at = _ptr(dy, "dy", T * D, _ELEM)
     need = embedding_grad_bytes(T, V, D)
     if out is None:
         if accumulate:
             raise ValueError("accumulate adds to out: give it")
         out = torch.empty((V, D), dtype=out_dtype, device=dy.device)
-    _need(out, "out", V * D, _ELEM)
-    if workspace is None:
-        workspace = _workspace(need, dy.device, stream)
-    _need(workspace, "workspace", need, _U8)
-    _check(lib().zq_embedding_grad(_dev(ids, "ids"), _ID_DT[ids.dtype], T, _dev(dy, "dy"), _TORCH_DT[dy.dtype], V, D,
-                                   scale, int(bool(accumulate)), _dev(out, "out"), _TORCH_DT[out.dtype],
-                                   _dev(workspace, "workspace"), workspace.numel(), _stream(stream)), "embedding_grad")
+    out_at = _ptr(out, "out", V * D, _ELEM)
+    ws_at, ws_size = _given_workspace(workspace, need, dy.device, stream)
+    _check(lib().zq_embedding_grad(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, dy_at or _dev(dy, "dy"),
+                                   _TORCH_DT[dy.dtype], V, D, scale, int(bool(accumulate)), out_at or _dev(out, "out"),
+                                   _TORCH_DT[out.dtype], ws_at, ws_size, _stream(stream)), "embedding_grad")
     return out
 
 
@@ -542,12 +550,7 @@ def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, workspace=None, s
     if y is None:
         y = torch.empty((M, N), dtype=torch.float32, device=x.device)
     y_at = _ptr(y, "y", M * N, _F32)
-    need = lib().zq_int4_dequant_gemm_bytes(M, N, K)
-    if workspace is None and need > 0:
-        workspace = _workspace(need, x.device, stream)
-    at, size = (0, 0) if workspace is None else (_dev(workspace, "workspace"), workspace.numel())
-    if workspace is not None:
-        _need(workspace, "workspace", max(need, 0), _U8)
+    at, size = _given_workspace(workspace, lib().zq_int4_dequant_gemm_bytes(M, N, K), x.device, stream)
     _check(lib().zq_int4_dequant_gemm(x_at or _dev(x, "x"), _TORCH_DT[x.dtype], packed_at or _dev(packed, "packed"),
                                       scales_at or _dev(scales, "scales"), M, N, K, block, y_at or _dev(y, "y"), at,
                                       size, _stream(stream)), "int4_dequant_gemm")

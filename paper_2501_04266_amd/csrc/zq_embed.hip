@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kEmbedThreads)
 
 // ---------------------------------------------------------------- gradient
 //
-// 1. k_sort_ids (7 us for 512 tokens, 14 for 16,384 of 50,000 rows, 18 for 40,001 of
+// 1. k_sort_ids (14 us for 16,384 of 50,000 rows, 18 for 40,001 of
 //    16,411: latency of the loads and the LDS counts): the tokens in the order of their ids, ties in the order of the
 //    tokens, and each row's first position in that order.  A workgroup owns a
 //    range of rows and a part of the tokens, and reads all ids: first it counts its
@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(kEmbedThreads)
 //    segments, beside the other rows.
 // 3. k_grad_join: the long rows from their segments' sums.
 // The order of every sum follows from the ids alone: no atomics on sums.
+// Up to 512 tokens take k_grad_few instead, one launch.
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kRangeBits = 9, kMaxRange = 1 << kRangeBits;  // rows of a workgroup's range at most (36 KiB of LDS)
@@ -429,6 +430,92 @@ __global__ void __launch_bounds__(kEmbedThreads)
   put_row<YT, E, ADD>(dw, row, D, c, C, d, scale, acc);
 }
 
+// ---- few tokens: one launch
+//
+// A workgroup has up to kFewRows rows and the columns of 4 waves' pieces, 8 KiB or a little
+// more of the result: it is written fastest in the order of its addresses, and workgroups
+// are few enough to look through all ids each (512 tokens, 8,000 x 1,024 in binary32: 9 us,
+// in 16 KiB 13.7, in 32 KiB 20; in three launches 15.5).  It marks its rows' tokens, a bit
+// each, in LDS: the bits of a row in their order are its tokens in theirs.
+constexpr int kFewTokens = 512, kFewWords = kFewTokens / 32;
+constexpr int kFewRows = 64;
+constexpr int64_t kFewBytes = 8192;
+constexpr int kEmbedWaves = kEmbedThreads / 64;
+template <int GT, int YT, int E, bool ADD>
+__global__ void __launch_bounds__(kEmbedThreads)
+    k_grad_few(const void* __restrict__ ids, bool wide, int T, const char* __restrict__ dy, int64_t V, int64_t D, int C,
+               int per, unsigned cols, int rb, float scale, void* __restrict__ dw) {
+  __shared__ uint32_t marks[kFewRows * kFewWords];
+  __shared__ int counts[kFewRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned block = blockIdx.x / cols, col = blockIdx.x - block * cols;
+  const int64_t row0 = (int64_t)block * rb;
+  const int n = (int)(V - row0 < rb ? V - row0 : rb);
+  int64_t id[kFewTokens / kEmbedThreads];
+#pragma unroll
+  for (int u = 0; u < kFewTokens / kEmbedThreads; ++u) {
+    const int t = u * kEmbedThreads + (int)threadIdx.x;
+    id[u] = t < T ? id_at(ids, wide, t) : -1;
+  }
+  for (int i = threadIdx.x; i < n * kFewWords; i += kEmbedThreads) marks[i] = 0;
+  if (threadIdx.x < kFewRows) counts[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < kFewTokens / kEmbedThreads; ++u) {
+    const uint64_t rel = (uint64_t)(id[u] - row0);
+    if (id[u] >= 0 && rel < (uint64_t)n) {
+      const int t = u * kEmbedThreads + (int)threadIdx.x;
+      atomicOr(&marks[(int)rel * kFewWords + t / 32], 1u << (t & 31));
+      atomicAdd(&counts[(int)rel], 1);
+    }
+  }
+  __syncthreads();
+  const int tokens_of = counts[lane];
+
+  // the 4 waves take the (row, piece) pairs in turn
+  const int first = (int)col * kEmbedWaves, subs = per - first < kEmbedWaves ? per - first : kEmbedWaves;
+  const unsigned inv = 65536u / (unsigned)subs + 1u;  // exact for the 256 pairs
+  for (int i = wave; i < n * subs; i += kEmbedWaves) {
+    const int row = (int)((unsigned)i * inv >> 16), sub = i - row * subs;
+    const int c = (first + sub) * 64 + lane;
+    const unsigned d = (unsigned)piece_column<E>(c, C, D);
+    int left = __builtin_amdgcn_readlane(tokens_of, row);
+    if (ADD && left == 0) continue;
+    float acc[E] = {};
+    if (left > 0) {
+      const uint32_t word = lane < kFewWords ? marks[row * kFewWords + lane] : 0u;
+      uint64_t words = __ballot(word != 0);
+      uint32_t bits = 0;
+      int at = 0;
+      auto next = [&] {  // the next token of the row
+        if (bits == 0) {
+          at = __builtin_ctzll(words);
+          words &= words - 1;
+          bits = (uint32_t)__builtin_amdgcn_readlane((int)word, at);
+        }
+        const int t = at * 32 + __builtin_ctz(bits);
+        bits &= bits - 1;
+        return t;
+      };
+      auto batch = [&](auto size) {
+        constexpr int N = decltype(size)::value;
+        const char* rows[N];
+#pragma unroll
+        for (int u = 0; u < N; ++u) rows[u] = dy + (int64_t)next() * (D * dt_size<GT>());
+        add_rows<GT, E, N>(rows, d, acc);
+        left -= N;
+      };
+      if constexpr (E < 8)
+        while (left >= 16) batch(std::integral_constant<int, 16>{});
+      while (left >= 8) batch(std::integral_constant<int, 8>{});
+      if (left >= 4) batch(std::integral_constant<int, 4>{});
+      if (left >= 2) batch(std::integral_constant<int, 2>{});
+      if (left >= 1) batch(std::integral_constant<int, 1>{});
+    }
+    put_row<YT, E, ADD>(dw, row0 + row, D, c, C, d, scale, acc);
+  }
+}
+
 // ---------------------------------------------------------------- dispatch
 
 using EmbedKernel = void (*)(const void*, bool, const void*, const float*, int64_t, int64_t, int64_t, int, double, int,
@@ -485,6 +572,27 @@ RowsKernel rows_kernel(int gt, int yt, bool short_rows, bool add) {
                         : rows_kernel_to<ZQ_BF16>(yt, short_rows, add);
 }
 
+using FewKernel = void (*)(const void*, bool, int, const char*, int64_t, int64_t, int, int, unsigned, int, float, void*);
+template <int GT, int YT, int E>
+FewKernel few_kernel_add(bool add) {
+  return add ? &k_grad_few<GT, YT, E, true> : &k_grad_few<GT, YT, E, false>;
+}
+template <int GT, int YT>
+FewKernel few_kernel_for(bool short_rows, bool add) {
+  return short_rows ? few_kernel_add<GT, YT, 1>(add) : few_kernel_add<GT, YT, piece_of<YT>()>(add);
+}
+template <int GT>
+FewKernel few_kernel_to(int yt, bool short_rows, bool add) {
+  return yt == ZQ_F32   ? few_kernel_for<GT, ZQ_F32>(short_rows, add)
+         : yt == ZQ_F16 ? few_kernel_for<GT, ZQ_F16>(short_rows, add)
+                        : few_kernel_for<GT, ZQ_BF16>(short_rows, add);
+}
+FewKernel few_kernel(int gt, int yt, bool short_rows, bool add) {
+  return gt == ZQ_F32   ? few_kernel_to<ZQ_F32>(yt, short_rows, add)
+         : gt == ZQ_F16 ? few_kernel_to<ZQ_F16>(yt, short_rows, add)
+                        : few_kernel_to<ZQ_BF16>(yt, short_rows, add);
+}
+
 template <int YT>
 JoinKernel join_kernel_for(bool short_rows, bool add) {
   return short_rows ? join_kernel_add<YT, 1>(add) : join_kernel_add<YT, piece_of<YT>()>(add);
@@ -520,6 +628,13 @@ int embed(const void* ids, int it, int64_t T, const void* table, const float* sc
                 lgB, scale, y);
 }
 
+// One launch for few tokens, unless the result is so large that the order it is written
+// in outweighs two launches (512 tokens, three launches and one: 400 MB in binary32 67 and
+// 64 us, 524 MB 112 and 103; 1.2 GB 179 and 208, 614 MB in bf16 94 and 107).  A row's
+// tokens are added by the same lanes one after the other: 512 tokens of one row of 6,144
+// columns 45 us, 38 in three launches; 1,024 tokens took 100.
+bool in_one_launch(int64_t T, int64_t V, int64_t D) { return T <= kFewTokens && (D == 0 || V <= (1 << 27) / D); }
+
 // Workspace of the gradient: first positions (V + 1), the order (T), the segments'
 // sums (2 rows of D each), each from a 16-byte boundary on.
 int64_t up16(int64_t b) { return (b + 15) & ~(int64_t)15; }
@@ -546,6 +661,7 @@ int qwz_embedding(const void* ids, zq_dtype it, int64_t T, const int8_t* codes, 
 
 int64_t zq_embedding_grad_bytes(int64_t T, int64_t V, int64_t D) {
   if (T < 0 || T > kMaxTokens || V < 0 || V > kMaxTokens || D < 0 || D > kMaxRow) return -1;
+  if (in_one_launch(T, V, D)) return 0;
   return start_bytes(V) + order_bytes(T) + (T < kPart ? 0 : 8 * ((T + kPart - 1) / kPart) * D);
 }
 
@@ -556,9 +672,10 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
   if (need < 0) return ZQ_E_SIZE;
   if ((it != ZQ_I32 && it != ZQ_I64) || !dtype_ok(gt) || !dtype_ok(wt)) return ZQ_E_DTYPE;
   if (V == 0 || D == 0 || (accumulate && T == 0)) return ZQ_OK;
-  if (!dw || !workspace || (T > 0 && (!ids || !dy))) return ZQ_E_NULL;
+  if (!dw || (need > 0 && !workspace) || (T > 0 && (!ids || !dy))) return ZQ_E_NULL;
   const int64_t ib = it == ZQ_I64 ? 8 : 4;
-  if (!aligned(ids, ib) || !aligned(dy, elem_bytes(gt)) || !aligned(dw, elem_bytes(wt)) || !aligned(workspace, 16))
+  if (!aligned(ids, ib) || !aligned(dy, elem_bytes(gt)) || !aligned(dw, elem_bytes(wt)) ||
+      (need > 0 && !aligned(workspace, 16)))
     return ZQ_E_ALIGN;
   if (workspace_bytes < need) return ZQ_E_SIZE;
   if (any_overlap({{dw, V * D * elem_bytes(wt)}, {workspace, need}}, {{ids, T * ib}, {dy, T * D * elem_bytes(gt)}}))
@@ -571,6 +688,17 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
   // waves of a row: 64 pieces each
   const bool short_rows = D < 8, add = accumulate != 0;
   const int64_t E = short_rows ? 1 : wt == ZQ_F32 ? 4 : 8, C = (D + E - 1) / E, per = (C + 63) / 64;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (in_one_launch(T, V, D)) {
+    const int64_t cols = (per + kEmbedWaves - 1) / kEmbedWaves;
+    const int64_t bytes = (D < 64 * kEmbedWaves * E ? D : 64 * kEmbedWaves * E) * elem_bytes(wt);  // of a row
+    int64_t rb = kFewBytes / bytes;
+    if (rb < 1) rb = 1;
+    if (rb > kFewRows) rb = kFewRows;
+    const int64_t grid = (V + rb - 1) / rb * cols;
+    return launch(few_kernel(gt, wt, short_rows, add), (unsigned)grid, kEmbedThreads, st, ids, it == ZQ_I64, (int)T,
+                  static_cast<const char*>(dy), V, D, (int)C, (int)per, (unsigned)cols, (int)rb, scale, dw);
+  }
   // no row is long with fewer tokens than a segment
   const int64_t segs = T < kPart ? 0 : (T + kPart - 1) / kPart;
   const int64_t seg_groups = segs ? grid_for(segs * per, kEmbedThreads / 64) : 0;
@@ -585,8 +713,6 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
   while (parts < 16 && (int64_t)(parts + 1) * 1024 <= T && (2 * parts + 1) * (2 * parts + 1) * ranges < 4 * 1700) ++parts;
   const int64_t sorts = ranges * parts;
   if (sorts > kMaxGrid) return ZQ_E_SIZE;
-
-  hipStream_t st = static_cast<hipStream_t>(stream);
   int rc = it == ZQ_I64 ? launch(&k_sort_ids<int64_t>, (unsigned)sorts, kSortThreads, st,
                                  static_cast<const int64_t*>(ids), (int)T, V, parts, start, order)
                         : launch(&k_sort_ids<int32_t>, (unsigned)sorts, kSortThreads, st,

@@ -136,7 +136,8 @@ def grad64(ids, dy, V, scale):
 
 GRADS = [(0, 5, 8), (1, 1, 1), (1, 40, 7), (2, 3, 8), (63, 4, 9), (64, 1, 16), (65, 1, 16), (129, 2, 24), (300, 257, 40),
          (1000, 7, 130), (1025, 600, 33), (5000, 3, 3), (4097, 1000, 72), (700, 140001, 8), (20000, 300, 64),
-         (200, 50, 2051)]
+         (200, 50, 2051), (513, 1, 16), (600, 4, 9), (700, 5, 24), (900, 50, 2051), (512, 70, 1030), (511, 1000, 2600),
+         (17, 300, 8200), (512, 1, 64)]
 
 
 @pytest.mark.parametrize("gt,yt", [("f32", "f32"), ("bf16", "f32"), ("f16", "f32"), ("bf16", "bf16"), ("f32", "f16")])
@@ -169,7 +170,7 @@ def test_gradient(T, V, D, gt, yt):
     assert torch.equal(w.view(V, D).cpu()[none], old.view(V, D).cpu()[none]) and guards_whole(buf, off, V * D)
 
 
-@pytest.mark.parametrize("T", [1, 63, 64, 65, 127, 128, 129, 4096, 10007])
+@pytest.mark.parametrize("T", [1, 63, 64, 65, 127, 128, 129, 511, 512, 513, 575, 576, 577, 640, 4096, 10007])
 @pytest.mark.parametrize("V,v", [(1, 0), (9, 8), (70000, 65535)])
 def test_gradient_of_one_row(T, V, v):
     """All tokens the same: whole 64s, and what is left before and after them; exact,

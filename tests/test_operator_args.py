@@ -69,26 +69,29 @@ def test_int8_embedding_argument_errors(L, args, status):
 
 def test_embedding_grad_argument_errors(L):
     f = L.zq_embedding_grad
-    need = L.zq_embedding_grad_bytes(100, 50, 64)
-    assert need >= 4 * 51 + 4 * 100   # first positions, the order, and partial sums
-    assert 0 < L.zq_embedding_grad_bytes(0, 0, 0) <= 16
+    need = L.zq_embedding_grad_bytes(1000, 50, 64)
+    assert need >= 4 * 51 + 4 * 1000   # first positions, the order, and partial sums
+    assert L.zq_embedding_grad_bytes(0, 0, 0) == 0 and L.zq_embedding_grad_bytes(100, 50, 64) == 0  # one launch
     for bad in ((-1, 50, 64), (100, -1, 64), (100, 50, -1), ((1 << 30) + 1, 50, 64), (100, (1 << 30) + 1, 64),
                 (100, 50, (1 << 24) + 1)):
         assert L.zq_embedding_grad_bytes(*bad) == -1
         T, V, D = bad
         assert f(A, 4, T, B, 2, V, D, 1.0, 0, C, 0, W, 1 << 40, None) == SIZE
 
-    def call(ids=A, it=4, T=100, dy=B, gt=2, V=50, D=64, acc=0, dw=C, wt=0, ws=W, size=need):
+    def call(ids=A, it=4, T=1000, dy=B, gt=2, V=50, D=64, acc=0, dw=C, wt=0, ws=W, size=need):
         return f(ids, it, T, dy, gt, V, D, 1.0, acc, dw, wt, ws, size, None)
 
     assert call(it=2) == DTYPE and call(gt=4) == DTYPE and call(wt=-2) == DTYPE
     assert call(ids=None) == NULL and call(dy=None) == NULL and call(dw=None) == NULL and call(ws=None) == NULL
     assert call(ids=A + 4) == ALIGN and call(dy=B + 1) == ALIGN and call(dw=C + 2) == ALIGN and call(ws=W + 8) == ALIGN
     assert call(size=need - 1) == SIZE
-    assert call(dw=B) == ALIAS and call(dw=A + 796) == ALIAS and call(ws=B) == ALIAS and call(ws=A) == ALIAS
+    assert call(dw=B) == ALIAS and call(dw=A + 7996) == ALIAS and call(ws=B) == ALIAS and call(ws=A) == ALIAS
     assert call(ws=C + 64) == ALIAS
     assert call(V=0, dw=None, ws=None) == 0 and call(D=0, dw=None, ws=None) == 0
     assert call(T=0, acc=1, ids=None, dy=None, dw=None, ws=None) == 0
+    # few tokens, without a workspace
+    assert call(T=100, ws=None, size=0, ids=None) == NULL and call(T=100, ws=None, size=0, dw=B) == ALIAS
+    assert call(T=100, ws=None, size=-1) == SIZE
 
 
 def grad(data=A, n=100, dtype=0, scales=None, out=None, out_dtype=0, block=0):
@@ -219,7 +222,7 @@ def test_binding_refusals():
     with pytest.raises(ValueError):
         zq.embedding_grad(ids, dy, -1)
     with pytest.raises(ValueError):
-        zq.embedding_grad(ids, dy, 10, out=table, workspace=torch.zeros(10, dtype=torch.uint8))
+        zq.embedding_grad(ids.repeat(200), dy.repeat(200, 1), 10, out=table, workspace=torch.zeros(10, dtype=torch.uint8))
     with pytest.raises(TypeError):
         zq.embedding_grad(ids, dy, 10, out=table, workspace=torch.zeros(1000))
     with pytest.raises(TypeError):
