@@ -361,7 +361,7 @@ def embedding(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
     ids_at = _ptr(ids, "ids", T, _IDS)
     table_at = _ptr(table, "table", V * D, _ELEM)
     if out is None:
-        out = torch.empty((*ids.shape, D), dtype=out_dtype or table.dtype, device=ids.device)
+        out = torch.empty(*ids.shape, D, dtype=out_dtype or table.dtype, device=ids.device)
     out_at = _ptr(out, "out", T * D, _ELEM)
     _check(lib().zq_embedding(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, table_at or _dev(table, "table"),
                               _TORCH_DT[table.dtype], V, D, scale, out_at or _dev(out, "out"), _TORCH_DT[out.dtype],
@@ -378,7 +378,7 @@ def qwz_embedding(ids, codes, scales, V, D, block=256, scale=1.0, out_dtype=torc
     codes_at = _ptr(codes, "codes", V * D, _I8)
     scales_at = _ptr(scales, "scales", _nsc(V * D, block), _F32)
     if out is None:
-        out = torch.empty((*ids.shape, D), dtype=out_dtype, device=ids.device)
+        out = torch.empty(*ids.shape, D, dtype=out_dtype, device=ids.device)
     out_at = _ptr(out, "out", T * D, _ELEM)
     _check(lib().qwz_embedding(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, codes_at or _dev(codes, "codes"),
                                scales_at or _dev(scales, "scales"), V, D, block, scale, out_at or _dev(out, "out"),
@@ -432,7 +432,7 @@ def embedding_grad(ids, dy, V, scale=1.0, out_dtype=torch.float32, out=None, acc
     if out is None:
         if accumulate:
             raise ValueError("accumulate adds to out: give it")
-        out = torch.empty((V, D), dtype=out_dtype, device=dy.device)
+        out = torch.empty(V, D, dtype=out_dtype, device=dy.device)
     out_at = _ptr(out, "out", V * D, _ELEM)
     ws_at, ws_size = _given_workspace(workspace, need, dy.device, stream)
     _check(lib().zq_embedding_grad(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, dy_at or _dev(dy, "dy"),
@@ -548,7 +548,7 @@ def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, workspace=None, s
     packed_at = _ptr(packed, "packed", int4_bytes(N * K), _U8)
     scales_at = _ptr(scales, "scales", _nsc(N * K, block), _F32)
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float32, device=x.device)
+        y = torch.empty(M, N, dtype=torch.float32, device=x.device)
     y_at = _ptr(y, "y", M * N, _F32)
     at, size = _given_workspace(workspace, lib().zq_int4_dequant_gemm_bytes(M, N, K), x.device, stream)
     _check(lib().zq_int4_dequant_gemm(x_at or _dev(x, "x"), _TORCH_DT[x.dtype], packed_at or _dev(packed, "packed"),
