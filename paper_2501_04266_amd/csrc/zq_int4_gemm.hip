@@ -19,9 +19,9 @@
 // 40,000 x 6,144: 38 us), close behind it the instructions that turn codes into
 // operands (about 330 cycles of a SIMD for 2,048 codes: 13 a word for 8 codes,
 // the moves between lanes, the addresses).  Up to about 8 MiB of weight a launch
-// and one round of loads take longer than its bytes: 6 to 8 us.  With more rows
-// x is read from the L2s by every workgroup, at 10 TB/s in all (64 rows, 24,576 x
-// 6,144: 57 us, 33 without these reads).
+// and one round of loads take longer than its bytes: 6 to 8 us.  With more than
+// 16 rows the conversion and x bind, which k_int4_wide shares in LDS (64 rows,
+// 24,576 x 6,144: 50 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -414,7 +414,8 @@ __global__ void __launch_bounds__(kGemmThreads)
 // tiles of 16 weight rows, whose sums stay in registers over the slice.  Nothing waits for
 // a staged x, and no workgroup has more than its share of K to read: a 2,048 x 8,192
 // product of 16 rows takes 8 us, 11 with x passed through LDS.  What it costs is x, read
-// again by every workgroup: GB tiles of the weight share a read.  The codes of a whole
+// again by every workgroup, at 10 TB/s from the L2s in all: GB tiles of the weight share a
+// read.  The codes of a whole
 // piece, GB tiles of it, are in flight, and one half piece of x (two where GB is 1).
 // G: codes summed before their scale is applied.
 template <int XT, int MT, int GB, int G>
@@ -547,6 +548,112 @@ __global__ void __launch_bounds__(kGemmThreads, MT == 1 ? 4 : 2)
   } while (group < groups);
 }
 
+// ---------------------------------------------------------------- more than 16 rows
+//
+// Each wave has a tile of 16 weight rows to itself over the slice of K, and the 8 waves
+// share x: a piece of 16 MT rows is in LDS while the next one is on its way there through
+// registers, so that x is read once for 128 weight rows.  Bound by LDS and the codes'
+// conversion in turn: 64 rows, 65,536 x 2,048 34 us (k_int4_regs 69, most of it reads of x);
+// 24,576 x 6,144 51 (57).
+// MT: 16-row tiles of x.  G: codes summed before their scale is applied.
+template <int XT, int MT, int G>
+__global__ void __launch_bounds__(kGemmThreads, 4)
+    k_int4_wide(const uint16_t* __restrict__ x, const uint8_t* __restrict__ packed, const float* __restrict__ scales,
+                int64_t M, int64_t N, int64_t K, int each, int lgB, int tiles, float* __restrict__ y) {
+  constexpr int D = 2;                                  // pieces of the weight in flight, and of x in LDS
+  constexpr int kRow = kPiece / 8 + 1;                  // 16-byte units of a row: odd, as above
+  constexpr int kBuffer = 16 * MT * kRow;
+  static_assert(kGemmThreads * MT * 8 == 16 * MT * kPiece, "a piece of x is MT units a thread");
+  __shared__ u32x4 lds[D * kBuffer];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15;
+  const int g = lane >> 4;
+  const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
+  const int mrows = (int)(M - m0 < 16 * MT ? M - m0 : 16 * MT);
+  const Slice sl(K, each);
+  const int pieces = pieces_of(sl.count);
+  const __amdgpu_buffer_rsrc_t xres =
+      __builtin_amdgcn_make_buffer_rsrc((void*)(x + m0 * K), (short)0, mrows * (int)K * 2, kRawBuffer);
+  const int tile = (int)blockIdx.x * kWaves + wave;
+  Weight<1, D> wt(packed, scales, N, K, sl, lgB, tiles);
+  wt.turn_to(tile);
+
+  const int xrow = threadIdx.x / (kPiece / 8), xcol = threadIdx.x % (kPiece / 8);  // of the first unit; the next: 16 rows on
+  u32x4 xv[MT];
+  auto read_x = [&](int p) {  // rows past M are outside the resource: zeros
+    const int k = p * kPiece + 8 * xcol;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const uint32_t off =
+          k < sl.count ? ((uint32_t)(16 * i + xrow) * (uint32_t)K + (uint32_t)(sl.from + k)) * 2 : kOutside;
+      xv[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xres, (int)off, 0, 0));
+    }
+  };
+  auto write_x = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) lds[buf * kBuffer + (16 * i + xrow) * kRow + xcol] = xv[i];
+  };
+
+  constexpr bool kAsLoaded = G == 128;
+  constexpr int XG = kAsLoaded ? 32 : 8, XJ = kAsLoaded ? 8 : 32;
+  const u32x4* const xat = lds + c * kRow + XG * g / 8;
+  f32x4_t acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  auto multiply = [&](int d, int h) {  // half h of the piece in slot d and buffer d
+    u32x4 words;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) words[q] = from_lane(4 * c + g, wt.codes[d][h][q]);
+    if constexpr (!kAsLoaded) words = transposed(words);
+    float s[128 / G];
+#pragma unroll
+    for (int q = 0; q < 128 / G; ++q) s[q] = u2f(from_lane(4 * c + q * (G / 32), f2u(wt.scale[d][h])));
+    f32x4_t part[MT];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool first = (32 * j) % G == 0, done = (32 * j + 32) % G == 0;
+      const u32x4 wf = operand<XT>(words[j]);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const u32x4 xf = xat[d * kBuffer + 16 * i * kRow + (128 * h + XJ * j) / 8];
+        part[i] = mfma<XT>(xf, wf, first ? f32x4_t{0.0f, 0.0f, 0.0f, 0.0f} : part[i]);
+        if (done) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][e] = __builtin_fmaf(part[i][e], s[32 * j / G], acc[i][e]);
+        }
+      }
+    }
+  };
+
+  read_x(0);
+#pragma unroll
+  for (int d = 0; d < D; ++d) wt.load(d, 0, 0, (uint32_t)(d * kPiece)), wt.load(d, 1, 0, (uint32_t)(d * kPiece));
+  write_x(0);
+  read_x(1);
+  for (int p = 0; p < pieces; p += D) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+      __syncthreads();  // x of this piece is there, and no wave reads the last one any more
+      if (p + d < pieces) multiply(d, 0), multiply(d, 1);
+      const uint32_t next = (uint32_t)((p + d + D) * kPiece);
+      wt.load(d, 0, 0, next), wt.load(d, 1, 0, next);
+      write_x(d ^ 1);
+      read_x(p + d + 2);
+    }
+  }
+
+  // element e of lane (c, g): row 4 g + e of x, weight row c
+  y += blockIdx.z * (M * N);
+  const int64_t n = (int64_t)tile * 16 + c;
+  if (n >= N) return;
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int m = 16 * i + 4 * g + e;
+      if (m < mrows) y[(m0 + m) * N + n] = 16.0f * acc[i][e];
+    }
+}
+
 // The slices' sums, in the order of the slices.  16 rows of 6,144 columns, 2 slices: 2 us.
 constexpr int kJoinThreads = 256;
 __global__ void __launch_bounds__(kJoinThreads)
@@ -568,6 +675,16 @@ Int4Kernel int4_few_kernel(int MR) {
 template <int XT>
 Int4Kernel int4_lds_kernel(int G) {
   return G == 128 ? &k_int4_lds<XT, 2, 128> : G == 64 ? &k_int4_lds<XT, 2, 64> : &k_int4_lds<XT, 2, 32>;
+}
+template <int XT, int MT>
+Int4Kernel int4_wide_kernel_of(int G) {
+  return G == 128 ? &k_int4_wide<XT, MT, 128> : G == 64 ? &k_int4_wide<XT, MT, 64> : &k_int4_wide<XT, MT, 32>;
+}
+template <int XT>
+Int4Kernel int4_wide_kernel(int MT, int G) {
+  return MT == 2   ? int4_wide_kernel_of<XT, 2>(G)
+         : MT == 3 ? int4_wide_kernel_of<XT, 3>(G)
+                   : int4_wide_kernel_of<XT, 4>(G);
 }
 template <int XT, int MT, int GB>
 Int4Kernel int4_regs_kernel_for(int G) {
@@ -592,7 +709,7 @@ constexpr int64_t kInt4MaxK = 1 << 22;  // 64 rows of x and 48 of codes stay bel
 constexpr int64_t kLds = 160 * 1024, kCus = 256;
 
 // How a product is cut.
-enum class Int4Way { few, lds, regs };
+enum class Int4Way { few, lds, regs, wide };
 struct Int4Plan {
   Int4Way way;
   int MR, MT, GB;        // few: rows of sums; regs: 16-row tiles of x, tiles of the weight
@@ -609,7 +726,7 @@ inline int64_t slice_of(int64_t K, int64_t slices) {
 // Up to 4 rows k_int4_few; up to 16 and more than two tiles a CU k_int4_lds, whose
 // reads of x cost least once its LDS is filled (5 rows, 50,001 x 6,144: 35 us, k_int4_regs
 // 52; 16 rows, 24,576 x 4,096: 16 and 19; but 16 rows, 6,144 x 6,144: 14 and 9).  Both
-// take x in slices where it is too long for LDS.  Else k_int4_regs.
+// take x in slices where it is too long for LDS.  Else k_int4_regs or k_int4_wide.
 inline Int4Plan int4_plan(int64_t M, int64_t N, int64_t K) {
   Int4Plan p{};
   const int64_t tiles = (N + 15) / 16;
@@ -632,26 +749,46 @@ inline Int4Plan int4_plan(int64_t M, int64_t N, int64_t K) {
     p.grid = room / p.slices > 1 ? room / p.slices : 1;
   } else {
     p.mgroups = (M + 16 * p.MT - 1) / (16 * p.MT);
-    // The least load of the busiest CU, in quarters of a tile's code: a workgroup's tiles
-    // and its reads of x (3/4 of a tile's time for 16 rows), for its codes and 1,024 more
-    // to begin and end; slices cost the second launch, and their sums' bytes.  Of the
-    // choices tried at 96 sizes (8 to 64 rows, 1,000 to 40,000 x 2,048 to 24,576) it takes
-    // the fastest or one within 10% of it at 89, within 26% at all.  16 rows, 6,144 x
-    // 24,576: 30 us by two slices of 3 tiles, 47 by single tiles.
+    // The least load of the busiest CU, in quarters of a tile's code (about 7,000 a us): a
+    // workgroup's tiles and its reads of x (3/4 of a tile's time for 16 rows), for its
+    // codes and 1,024 more to begin and end; slices cost the second launch, and their sums'
+    // bytes.  Of the choices tried at 96 sizes (8 to 64 rows, 1,000 to 40,000 x 2,048 to
+    // 24,576) it takes the fastest or one within 10% of it at 89, within 26% at all.  16
+    // rows, 6,144 x 24,576: 30 us by two slices of 3 tiles, 47 by single tiles.
     double least = 0;
+    auto load_of = [](double wgs) { return __builtin_ceil(wgs / kCus); };
     for (int GB = 3; GB >= 1; --GB)
       for (int64_t S = 1; S == 1 || (S <= 16 && S <= K / 2048); ++S) {
-        const double wgs = (double)((tiles + GB - 1) / GB) * (double)(p.mgroups * S);
-        const double load = __builtin_ceil(wgs / kCus) * (double)(slice_of(K, S) + 1024) * (4 * GB + 3 * p.MT) +
+        const double load = load_of((double)((tiles + GB - 1) / GB) * (double)(p.mgroups * S)) *
+                                (double)(slice_of(K, S) + 1024) * (4 * GB + 3 * p.MT) +
                             (S > 1 ? 49152.0 + (double)M * (double)N * (double)S / 64 : 0.0);
         if (least == 0 || load < least) least = load, p.GB = GB, p.slices = S;
       }
+    // k_int4_wide for more than 16 rows: a workgroup's 8 tiles take 1.1, 1.4 or 1.9 us a
+    // piece (2, 3 and 4 tiles of x; two workgroups on a CU twice that), and one and a half
+    // pieces to begin and end.  32 rows: 65,536 x 2,048 23 us, k_int4_regs 37; 20,000 x
+    // 12,288 in three slices 45 and 64; but 4,096 x 4,096 12 and 8.
+    if (p.MT > 1) {
+      const int MT = M <= 32 ? 2 : M <= 48 ? 3 : 4;
+      const double piece = 7000 * (MT == 2 ? 1.15 : MT == 3 ? 1.44 : 1.87);
+      const int64_t grid = (tiles + kWaves - 1) / kWaves, mgroups = (M + 16 * MT - 1) / (16 * MT);
+      for (int64_t S = 1; S == 1 || (S <= 16 && S <= K / 512); ++S) {
+        const double load = load_of((double)grid * (double)(mgroups * S)) * (slice_of(K, S) / kPiece + 1.5) * piece +
+                            (S > 1 ? 35000.0 + (double)M * (double)N * (double)S / 375 : 0.0);
+        if (load < least) {
+          least = load, p.way = Int4Way::wide, p.slices = S;
+          p.MT = MT, p.mgroups = mgroups, p.grid = grid, p.groups = tiles, p.lds = 0;
+        }
+      }
+    }
     p.each = slice_of(K, p.slices);
-    p.groups = (tiles + p.GB - 1) / p.GB;
-    p.grid = (p.MT == 1 ? 2 : 1) * kCus;
-    p.lds = kWaves * 16 * 4 * (M < 16 * p.MT ? M : 16 * p.MT) * p.GB;
+    if (p.way == Int4Way::regs) {
+      p.groups = (tiles + p.GB - 1) / p.GB;
+      p.grid = (p.MT == 1 ? 2 : 1) * kCus;
+      p.lds = kWaves * 16 * 4 * (M < 16 * p.MT ? M : 16 * p.MT) * p.GB;
+    }
   }
-  if (p.grid > p.groups) p.grid = p.groups;
+  if (p.way != Int4Way::wide && p.grid > p.groups) p.grid = p.groups;
   p.slices = K ? (K + p.each - 1) / p.each : 1;
   return p;
 }
@@ -697,6 +834,7 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
   const int G = block >= 128 && K % 128 == 0 ? 128 : block >= 64 ? 64 : 32;
   const bool bf = xt == ZQ_BF16;
   const Int4Kernel k = p.way == Int4Way::few   ? (bf ? int4_few_kernel<ZQ_BF16>(p.MR) : int4_few_kernel<ZQ_F16>(p.MR))
+                       : p.way == Int4Way::wide ? (bf ? int4_wide_kernel<ZQ_BF16>(p.MT, G) : int4_wide_kernel<ZQ_F16>(p.MT, G))
                        : p.way == Int4Way::lds ? (bf ? int4_lds_kernel<ZQ_BF16>(G) : int4_lds_kernel<ZQ_F16>(G))
                                                : (bf ? int4_regs_kernel<ZQ_BF16>(p.MT, p.GB, G)
                                                      : int4_regs_kernel<ZQ_F16>(p.MT, p.GB, G));

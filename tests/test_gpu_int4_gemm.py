@@ -51,6 +51,9 @@ CASES = [(1, 1, 64, 32), (1, 15, 64, 1024), (2, 17, 128, 64), (3, 33, 192, 128),
 CASES += [(1, 16400, 192, 64), (5, 8320, 448, 128), (16, 8208, 5440, 64), (12, 8210, 576, 32), (4, 40, 24576, 128),
           (2, 24, 49152, 32), (9, 4500, 64, 32), (20, 4300, 320, 128), (40, 4300, 192, 64), (24, 8300, 320, 128),
           (50, 8300, 256, 256), (64, 12400, 128, 32), (10, 40, 24576, 128), (33, 70, 16448, 64), (20, 100, 14400, 32)]
+# more than 16 rows and many weight rows: a tile a wave, x through LDS
+CASES += [(24, 16400, 320, 128), (32, 16390, 1088, 64), (17, 16500, 64, 32), (40, 16400, 576, 64), (48, 16385, 512, 256),
+          (35, 16400, 192, 32), (64, 16390, 832, 32), (49, 16400, 1280, 128), (60, 16400, 320, 64), (70, 16400, 192, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
@@ -116,7 +119,8 @@ def test_special_values():
     assert got[rows][:, 15].eq(512 * 2.0**100).all() and got[rows][:, 17].eq(7 * 512 * 2.0**-126).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(3, 40, 24576), (12, 8320, 512), (12, 8320, 8192), (12, 40, 24576), (40, 4300, 512)])
+@pytest.mark.parametrize("M,N,K", [(3, 40, 24576), (12, 8320, 512), (12, 8320, 8192), (12, 40, 24576), (40, 4300, 512),
+                                   (20, 16400, 640)])
 def test_special_rows(M, N, K):
     """NaN and infinities of x stay in their rows, those of scales in their columns,
     whichever way the product is cut."""
@@ -135,21 +139,26 @@ def test_special_rows(M, N, K):
     assert bool(got[rows][:, 17].eq(K).all()) and bool(got[rows][:, N - 1].eq(0).all()) and got[2, 17] == float("inf")
 
 
-@pytest.mark.parametrize("M", [16, 31])
-def test_slices_of_three_tiles(M):
-    """A weight of many rows and a long K, against 64-bit products on the GPU."""
-    N, K, block = 5003, 20544, 64
-    assert zq.int4_dequant_gemm_bytes(M, N, K) > 0
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K,block", [
+    (16, 5003, 20544, 64), (31, 5003, 20544, 64), (13, 5003, 20480, 128), (16, 5003, 20480, 32),  # slices of K
+    (9, 4500, 384, 128), (9, 4500, 320, 64), (20, 4300, 384, 128), (20, 4300, 384, 32), (20, 300, 320, 32), (24, 8300, 384, 256),
+    (24, 8300, 320, 32), (40, 4300, 512, 32), (40, 4300, 512, 64), (40, 4300, 512, 128), (50, 8300, 512, 32),
+    (50, 8300, 576, 64), (30, 16400, 768, 128), (64, 20011, 2176, 128), (12, 20011, 10560, 256), (3, 6001, 24576, 64)])
+def test_against_the_gpu(M, N, K, block, dtype):
+    """Weights of many rows, against 64-bit products on the GPU."""
     g = torch.Generator(device=DEV).manual_seed(M)
     packed = torch.randint(0, 256, (N * K // 2,), dtype=torch.uint8, device=DEV, generator=g)
-    scales = torch.rand(N * K // block, device=DEV, generator=g) * 1e-2
-    x = torch.randn(M, K, device=DEV, generator=g).bfloat16()
+    scales = torch.rand(-(-N * K // block), device=DEV, generator=g) * 1e-2
+    x = torch.randn(M, K, device=DEV, generator=g).to(DT[dtype])
     got = zq.int4_dequant_gemm(x, packed, scales, N, block).double()
-    for n in range(0, N, 500):
-        b = packed.view(N, K // 2)[n:n + 500]
+    step = max(1, (1 << 23) // K)
+    for n in range(0, N, step):
+        b = packed.view(N, K // 2)[n:n + step]
         q = (torch.stack((b & 15, b >> 4), -1).view(len(b), K).to(torch.int8) ^ 8) - 8
-        w = (q.double().view(len(b), -1, block) * scales.view(N, -1)[n:n + 500, :, None].double()).view(len(b), K)
-        far = (got[:, n:n + 500] - x.double() @ w.t()).abs()
+        at = torch.arange(n * K, n * K + q.numel(), device=DEV) // block
+        w = q.double() * scales[at].double().view_as(q)
+        far = (got[:, n:n + step] - x.double() @ w.t()).abs()
         assert bool((far <= (K + 64) * 2.0**-23 * (x.double().abs() @ w.abs().t())).all())
 
 
