@@ -793,6 +793,9 @@ inline Int4Plan int4_plan(int64_t M, int64_t N, int64_t K) {
   return p;
 }
 
+// bytes: the slices' sums
+inline int64_t workspace_of(const Int4Plan& p, int64_t M, int64_t N) { return p.slices == 1 ? 0 : 4 * M * N * p.slices; }
+
 inline bool int4_sizes_ok(int64_t M, int64_t N, int64_t K) {
   return M >= 0 && N >= 0 && K >= 0 && K % 64 == 0 && K <= kInt4MaxK && M <= 64 * 65535 && N <= INT64_MAX / 16 / (K + 1) &&
          (N + 15) / 16 <= kMaxGrid / 2 && (M == 0 || N <= INT64_MAX / 1024 / M);
@@ -805,8 +808,7 @@ extern "C" int64_t zq_int4_dequant_gemm_bytes(int64_t M, int64_t N, int64_t K) {
   using namespace zq;
   if (!int4_sizes_ok(M, N, K)) return -1;
   if (M == 0 || N == 0) return 0;
-  const Int4Plan p = int4_plan(M, N, K);
-  return p.slices == 1 ? 0 : 4 * M * N * p.slices;
+  return workspace_of(int4_plan(M, N, K), M, N);
 }
 
 extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, const float* scales, int64_t M,
@@ -818,7 +820,8 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
   if (lgB < 0) return ZQ_E_BLOCK;
   if (xt != ZQ_BF16 && xt != ZQ_F16) return ZQ_E_DTYPE;
   if (M == 0 || N == 0) return ZQ_OK;
-  const int64_t need = zq_int4_dequant_gemm_bytes(M, N, K);
+  const Int4Plan p = int4_plan(M, N, K);
+  const int64_t need = workspace_of(p, M, N);
   if (workspace_bytes < need) return ZQ_E_SIZE;
   if (!y || (need > 0 && !workspace) || (K > 0 && (!x || !packed || !scales))) return ZQ_E_NULL;
   if (!aligned(x, 16) || !aligned(packed, 16) || !aligned(scales, 4) || !aligned(y, 4) ||
@@ -828,7 +831,6 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
                   {{x, 2 * M * K}, {packed, N * K / 2}, {scales, 4 * num_scales(N * K, block)}}))
     return ZQ_E_ALIAS;
 
-  const Int4Plan p = int4_plan(M, N, K);
   // codes under one scale: 128 from a multiple of 128 on lie in one block only where
   // rows start at multiples of 128
   const int G = block >= 128 && K % 128 == 0 ? 128 : block >= 64 ? 64 : 32;
