@@ -756,24 +756,26 @@ inline Int4Plan int4_plan(int64_t M, int64_t N, int64_t K) {
     // 24,576) it takes the fastest or one within 10% of it at 89, within 26% at all.  16
     // rows, 6,144 x 24,576: 30 us by two slices of 3 tiles, 47 by single tiles.
     double least = 0;
-    auto load_of = [](double wgs) { return __builtin_ceil(wgs / kCus); };
     for (int GB = 3; GB >= 1; --GB)
       for (int64_t S = 1; S == 1 || (S <= 16 && S <= K / 2048); ++S) {
-        const double load = load_of((double)((tiles + GB - 1) / GB) * (double)(p.mgroups * S)) *
-                                (double)(slice_of(K, S) + 1024) * (4 * GB + 3 * p.MT) +
+        const double wgs = (double)((tiles + GB - 1) / GB) * (double)(p.mgroups * S);
+        const double load = __builtin_ceil(wgs / kCus) * (double)(slice_of(K, S) + 1024) * (4 * GB + 3 * p.MT) +
                             (S > 1 ? 49152.0 + (double)M * (double)N * (double)S / 64 : 0.0);
         if (least == 0 || load < least) least = load, p.GB = GB, p.slices = S;
       }
-    // k_int4_wide for more than 16 rows: a workgroup's 8 tiles take 1.1, 1.4 or 1.9 us a
-    // piece (2, 3 and 4 tiles of x; two workgroups on a CU twice that), and one and a half
-    // pieces to begin and end.  32 rows: 65,536 x 2,048 23 us, k_int4_regs 37; 20,000 x
+    // k_int4_wide for more than 16 rows: a workgroup's 8 tiles take 1.2, 1.4 or 1.9 us a
+    // piece (2, 3 and 4 tiles of x), and one and a half pieces to begin and end; two
+    // workgroups on a CU take nearly twice that, and a few more than the CUs hold one of
+    // take half as long again, not twice as long.  32 rows: 65,536 x 2,048 23 us, k_int4_regs 37; 20,000 x
     // 12,288 in three slices 45 and 64; but 4,096 x 4,096 12 and 8.
     if (p.MT > 1) {
       const int MT = M <= 32 ? 2 : M <= 48 ? 3 : 4;
       const double piece = 7000 * (MT == 2 ? 1.15 : MT == 3 ? 1.44 : 1.87);
       const int64_t grid = (tiles + kWaves - 1) / kWaves, mgroups = (M + 16 * MT - 1) / (16 * MT);
       for (int64_t S = 1; S == 1 || (S <= 16 && S <= K / 512); ++S) {
-        const double load = load_of((double)grid * (double)(mgroups * S)) * (slice_of(K, S) / kPiece + 1.5) * piece +
+        const double w = (double)grid * (double)(mgroups * S) / kCus, even = 0.45 + 0.9 * w;
+        const double turns = even < 1.0 ? 1.0 : even < __builtin_ceil(w) ? even : __builtin_ceil(w);
+        const double load = turns * (double)(slice_of(K, S) / kPiece + 1.5) * piece +
                             (S > 1 ? 35000.0 + (double)M * (double)N * (double)S / 375 : 0.0);
         if (load < least) {
           least = load, p.way = Int4Way::wide, p.slices = S;
