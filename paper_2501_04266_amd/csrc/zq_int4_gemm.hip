@@ -165,7 +165,8 @@ struct Weight {
 // used again, in each turn of the loops below.
 __host__ __device__ inline int x_stride(int64_t K) { return pieces_of(K) * (kPiece / 8) + 1; }
 template <typename F>
-__device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres, int mrows, int64_t K, Slice sl, F between) {
+__device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres, int mrows, int64_t K, Slice sl,
+                                        F between) {
   constexpr int U = 4;
   const int stride = x_stride(sl.count);
   const unsigned row = (unsigned)stride - 1, units = (unsigned)mrows * row;  // 16-byte units: below 2^14
@@ -178,7 +179,8 @@ __device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres,
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const unsigned i = at + u * kGemmThreads, m = row_of(i), k = 8 * (i - m * row);
-      const uint32_t off = i < units && k < (unsigned)sl.count ? (m * (unsigned)K + (unsigned)sl.from + k) * 2 : kOutside;
+      const uint32_t off =
+          i < units && k < (unsigned)sl.count ? (m * (unsigned)K + (unsigned)sl.from + k) * 2 : kOutside;
       v[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xres, (int)off, 0, 0));
     }
   };
@@ -230,7 +232,9 @@ __global__ void __launch_bounds__(kGemmThreads)
     wt.load(d, 0, 0, k0), wt.load(d, 1, 0, k0);
     if (++load_round == rounds) load_round = 0, wt.turn_to(load_group += gridDim.x);
   };
-  stage_x(lds, __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * (int)K * 2, kRawBuffer), mrows, K, sl, [&] {
+  const __amdgpu_buffer_rsrc_t xres =
+      __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * (int)K * 2, kRawBuffer);
+  stage_x(lds, xres, mrows, K, sl, [&] {
 #pragma unroll
     for (int d = 0; d < D; ++d) load(d);
   });
@@ -333,7 +337,9 @@ __global__ void __launch_bounds__(kGemmThreads)
     wt.load(d, 0, 0, k0), wt.load(d, 1, 0, k0);
     if (++load_round == rounds) load_round = 0, wt.turn_to(load_group += gridDim.x);
   };
-  stage_x(lds, __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * (int)K * 2, kRawBuffer), mrows, K, sl, [&] {
+  const __amdgpu_buffer_rsrc_t xres =
+      __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, mrows * (int)K * 2, kRawBuffer);
+  stage_x(lds, xres, mrows, K, sl, [&] {
 #pragma unroll
     for (int d = 0; d < D; ++d) load(d);
   });
@@ -577,7 +583,8 @@ __global__ void __launch_bounds__(kGemmThreads, 4)
   Weight<1, D> wt(packed, scales, N, K, sl, lgB, tiles);
   wt.turn_to(tile);
 
-  const int xrow = threadIdx.x / (kPiece / 8), xcol = threadIdx.x % (kPiece / 8);  // of the first unit; the next: 16 rows on
+  // of the thread's first unit; the next ones are 16 rows on each
+  const int xrow = threadIdx.x / (kPiece / 8), xcol = threadIdx.x % (kPiece / 8);
   u32x4 xv[MT];
   auto read_x = [&](int p) {  // rows past M are outside the resource: zeros
     const int k = p * kPiece + 8 * xcol;
@@ -796,11 +803,13 @@ inline Int4Plan int4_plan(int64_t M, int64_t N, int64_t K) {
 }
 
 // bytes: the slices' sums
-inline int64_t workspace_of(const Int4Plan& p, int64_t M, int64_t N) { return p.slices == 1 ? 0 : 4 * M * N * p.slices; }
+inline int64_t workspace_of(const Int4Plan& p, int64_t M, int64_t N) {
+  return p.slices == 1 ? 0 : 4 * M * N * p.slices;
+}
 
 inline bool int4_sizes_ok(int64_t M, int64_t N, int64_t K) {
-  return M >= 0 && N >= 0 && K >= 0 && K % 64 == 0 && K <= kInt4MaxK && M <= 64 * 65535 && N <= INT64_MAX / 16 / (K + 1) &&
-         (N + 15) / 16 <= kMaxGrid / 2 && (M == 0 || N <= INT64_MAX / 1024 / M);
+  return M >= 0 && N >= 0 && K >= 0 && K % 64 == 0 && K <= kInt4MaxK && M <= 64 * 65535 &&
+         N <= INT64_MAX / 16 / (K + 1) && (N + 15) / 16 <= kMaxGrid / 2 && (M == 0 || N <= INT64_MAX / 1024 / M);
 }
 
 }  // namespace
@@ -838,7 +847,8 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
   const int G = block >= 128 && K % 128 == 0 ? 128 : block >= 64 ? 64 : 32;
   const bool bf = xt == ZQ_BF16;
   const Int4Kernel k = p.way == Int4Way::few   ? (bf ? int4_few_kernel<ZQ_BF16>(p.MR) : int4_few_kernel<ZQ_F16>(p.MR))
-                       : p.way == Int4Way::wide ? (bf ? int4_wide_kernel<ZQ_BF16>(p.MT, G) : int4_wide_kernel<ZQ_F16>(p.MT, G))
+                       : p.way == Int4Way::wide ? (bf ? int4_wide_kernel<ZQ_BF16>(p.MT, G)
+                                                      : int4_wide_kernel<ZQ_F16>(p.MT, G))
                        : p.way == Int4Way::lds ? (bf ? int4_lds_kernel<ZQ_BF16>(G) : int4_lds_kernel<ZQ_F16>(G))
                                                : (bf ? int4_regs_kernel<ZQ_BF16>(p.MT, p.GB, G)
                                                      : int4_regs_kernel<ZQ_F16>(p.MT, p.GB, G));
