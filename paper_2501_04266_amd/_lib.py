@@ -103,6 +103,27 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_object(stream, device):
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+
+
+def _output(shape, dtype, device, stream):
+    """A tensor for a call on `stream` to write and return, allocated on the current
+    stream, where its user expects it.  Another `stream` waits for the work that is
+    pending on the current one (the memory's last user may be part of it), and, given as
+    an object, the allocator keeps the tensor until that stream has passed the call.  (A
+    raw handle may be gone by the time the tensor is freed: its owner keeps the tensor
+    until the call has run.)"""
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        st, current = _stream_object(stream, device), torch.cuda.current_stream(device)
+        if st.cuda_stream != current.cuda_stream:
+            st.wait_stream(current)
+            if st is stream:
+                t.record_stream(st)
+    return t
+
+
 def _dev(t, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU tensor")
@@ -361,7 +382,7 @@ def embedding(ids, table, scale=1.0, out_dtype=None, out=None, stream=None):
     ids_at = _ptr(ids, "ids", T, _IDS)
     table_at = _ptr(table, "table", V * D, _ELEM)
     if out is None:
-        out = torch.empty(*ids.shape, D, dtype=out_dtype or table.dtype, device=ids.device)
+        out = _output((*ids.shape, D), out_dtype or table.dtype, ids.device, stream)
     out_at = _ptr(out, "out", T * D, _ELEM)
     _check(lib().zq_embedding(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, table_at or _dev(table, "table"),
                               _TORCH_DT[table.dtype], V, D, scale, out_at or _dev(out, "out"), _TORCH_DT[out.dtype],
@@ -378,7 +399,7 @@ def qwz_embedding(ids, codes, scales, V, D, block=256, scale=1.0, out_dtype=torc
     codes_at = _ptr(codes, "codes", V * D, _I8)
     scales_at = _ptr(scales, "scales", _nsc(V * D, block), _F32)
     if out is None:
-        out = torch.empty(*ids.shape, D, dtype=out_dtype, device=ids.device)
+        out = _output((*ids.shape, D), out_dtype, ids.device, stream)
     out_at = _ptr(out, "out", T * D, _ELEM)
     _check(lib().qwz_embedding(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, codes_at or _dev(codes, "codes"),
                                scales_at or _dev(scales, "scales"), V, D, block, scale, out_at or _dev(out, "out"),
@@ -387,13 +408,12 @@ def qwz_embedding(ids, codes, scales, V, D, block=256, scale=1.0, out_dtype=torc
 
 
 def _workspace(nbytes, device, stream):
-    """Memory for one call on `stream`."""
-    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if stream is not None:
-        # allocated on the current stream, used on another: the allocator keeps it
-        # until that stream has passed the call
-        w.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
-    return w
+    """Memory for one call on `stream`, from that stream's own pool: its last user and
+    its next one are ordered with the call."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(_stream_object(stream, device)):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def _given_workspace(workspace, need, device, stream):
@@ -432,7 +452,7 @@ def embedding_grad(ids, dy, V, scale=1.0, out_dtype=torch.float32, out=None, acc
     if out is None:
         if accumulate:
             raise ValueError("accumulate adds to out: give it")
-        out = torch.empty(V, D, dtype=out_dtype, device=dy.device)
+        out = _output((V, D), out_dtype, dy.device, stream)
     out_at = _ptr(out, "out", V * D, _ELEM)
     ws_at, ws_size = _given_workspace(workspace, need, dy.device, stream)
     _check(lib().zq_embedding_grad(ids_at or _dev(ids, "ids"), _ID_DT[ids.dtype], T, dy_at or _dev(dy, "dy"),
@@ -497,7 +517,7 @@ def _table(grads, stream):
         return grads
     t = grad_table(grads)
     if stream is not None:
-        t.table.record_stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+        t.table.record_stream(_stream_object(stream, t.table.device))
     return t
 
 
@@ -508,7 +528,7 @@ def grad_norm(grads, scale=1.0, out=None, stream=None):
     order."""
     t = _table(grads, stream)
     if out is None:
-        out = torch.empty(1, dtype=torch.float32, device=t.table.device).view(())
+        out = _output(1, torch.float32, t.table.device, stream).view(())
     _need(out, "out", 1, _F32)
     _check(lib().zq_grad_norm(ctypes.byref(t.plan), t.table.data_ptr(), scale, _dev(out, "out"), _stream(stream)),
            "grad_norm")
@@ -548,7 +568,7 @@ def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, workspace=None, s
     packed_at = _ptr(packed, "packed", int4_bytes(N * K), _U8)
     scales_at = _ptr(scales, "scales", _nsc(N * K, block), _F32)
     if y is None:
-        y = torch.empty(M, N, dtype=torch.float32, device=x.device)
+        y = _output((M, N), torch.float32, x.device, stream)
     y_at = _ptr(y, "y", M * N, _F32)
     at, size = _given_workspace(workspace, lib().zq_int4_dequant_gemm_bytes(M, N, K), x.device, stream)
     _check(lib().zq_int4_dequant_gemm(x_at or _dev(x, "x"), _TORCH_DT[x.dtype], packed_at or _dev(packed, "packed"),
