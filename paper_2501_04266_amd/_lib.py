@@ -104,7 +104,10 @@ def _stream(stream):
 
 
 def _stream_object(stream, device):
-    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    # a tensor on the CPU is refused, as such, once the call looks at its address
+    return torch.cuda.ExternalStream(int(stream), device=device if device.type == "cuda" else None)
 
 
 def _output(shape, dtype, device, stream):
@@ -115,7 +118,7 @@ def _output(shape, dtype, device, stream):
     raw handle may be gone by the time the tensor is freed: its owner keeps the tensor
     until the call has run.)"""
     t = torch.empty(shape, dtype=dtype, device=device)
-    if stream is not None:
+    if stream is not None and t.is_cuda:
         st, current = _stream_object(stream, device), torch.cuda.current_stream(device)
         if st.cuda_stream != current.cuda_stream:
             st.wait_stream(current)
@@ -183,9 +186,9 @@ def qwz_quantize(x, block=256, codes=None, scales=None, stream=None):
     n = x.numel()
     _need(x, "x", n, _ELEM)
     if codes is None:
-        codes = torch.empty(n, dtype=torch.int8, device=x.device)
+        codes = _output(n, torch.int8, x.device, stream)
     if scales is None:
-        scales = torch.empty(_alloc_nsc(n, block), dtype=torch.float32, device=x.device)
+        scales = _output(_alloc_nsc(n, block), torch.float32, x.device, stream)
     _need(codes, "codes", n, _I8)
     _need(scales, "scales", _nsc(n, block), _F32)
     _check(lib().qwz_quantize(_dev(x, "x"), _TORCH_DT[x.dtype], n, block, _dev(codes, "codes"),
@@ -196,7 +199,7 @@ def qwz_quantize(x, block=256, codes=None, scales=None, stream=None):
 def qwz_dequantize(codes, scales, block=256, out_dtype=torch.bfloat16, y=None, n=None, stream=None):
     n = codes.numel() if n is None else n
     if y is None:
-        y = torch.empty(n, dtype=out_dtype, device=codes.device)
+        y = _output(n, out_dtype, codes.device, stream)
     _need(codes, "codes", n, _I8)
     _need(scales, "scales", _nsc(n, block), _F32)
     _need(y, "y", n, _ELEM)
@@ -210,9 +213,9 @@ def qgz_quantize(g, block=128, packed=None, scales=None, stream=None):
     n = g.numel()
     _need(g, "g", n, _ELEM)
     if packed is None:
-        packed = torch.empty(int4_bytes(n), dtype=torch.uint8, device=g.device)
+        packed = _output(int4_bytes(n), torch.uint8, g.device, stream)
     if scales is None:
-        scales = torch.empty(_alloc_nsc(n, block), dtype=torch.float32, device=g.device)
+        scales = _output(_alloc_nsc(n, block), torch.float32, g.device, stream)
     _need(packed, "packed", int4_bytes(n), _U8)
     _need(scales, "scales", _nsc(n, block), _F32)
     _check(lib().qgz_quantize(_dev(g, "g"), _TORCH_DT[g.dtype], n, block, _dev(packed, "packed"),
@@ -222,7 +225,7 @@ def qgz_quantize(g, block=128, packed=None, scales=None, stream=None):
 
 def qgz_dequantize(packed, scales, n, block=128, out_dtype=torch.float32, y=None, stream=None):
     if y is None:
-        y = torch.empty(n, dtype=out_dtype, device=packed.device)
+        y = _output(n, out_dtype, packed.device, stream)
     _need(packed, "packed", int4_bytes(n), _U8)
     _need(scales, "scales", _nsc(n, block), _F32)
     _need(y, "y", n, _ELEM)
@@ -236,9 +239,9 @@ def qgz_reduce_level(packed_in, scales_in, P, m, block=128, packed_out=None, sca
     P slices of ceil(m/2) bytes back to back, scales_in P x ceil(m/B)."""
     dev = packed_in.device
     if packed_out is None:
-        packed_out = torch.empty(int4_bytes(m), dtype=torch.uint8, device=dev)
+        packed_out = _output(int4_bytes(m), torch.uint8, dev, stream)
     if scales_out is None:
-        scales_out = torch.empty(_alloc_nsc(m, block), dtype=torch.float32, device=dev)
+        scales_out = _output(_alloc_nsc(m, block), torch.float32, dev, stream)
     _need(packed_in, "packed_in", P * int4_bytes(m), _U8)
     _need(scales_in, "scales_in", P * _nsc(m, block), _F32)
     _need(packed_out, "packed_out", int4_bytes(m), _U8)
@@ -255,7 +258,7 @@ def qgz_reduce_dequantize(packed_in, scales_in, P, m, block=128, out_dtype=torch
     out_dtype) bit-identical to qgz_dequantize(qgz_reduce_level(...)).  Pass
     packed_out and scales_out to also receive the INT4 result."""
     if y is None:
-        y = torch.empty(m, dtype=out_dtype, device=packed_in.device)
+        y = _output(m, out_dtype, packed_in.device, stream)
     if (packed_out is None) != (scales_out is None):
         raise ValueError("give both packed_out and scales_out, or neither")
     _need(packed_in, "packed_in", P * int4_bytes(m), _U8)
@@ -303,9 +306,9 @@ def qgz_reduce_level_gather(packed_slices, scale_slices, m, block=128, packed_ou
             raise ValueError(f"scale_slices[{p}] must be 4-byte aligned")
     dev = packed_slices[0].device
     if packed_out is None:
-        packed_out = torch.empty(int4_bytes(m), dtype=torch.uint8, device=dev)
+        packed_out = _output(int4_bytes(m), torch.uint8, dev, stream)
     if scales_out is None:
-        scales_out = torch.empty(_alloc_nsc(m, block), dtype=torch.float32, device=dev)
+        scales_out = _output(_alloc_nsc(m, block), torch.float32, dev, stream)
     _need(packed_out, "packed_out", int4_bytes(m), _U8)
     _need(scales_out, "scales_out", _nsc(m, block), _F32)
     # the pointer tables live in device memory (the kernel reads them); built
@@ -315,7 +318,7 @@ def qgz_reduce_level_gather(packed_slices, scale_slices, m, block=128, packed_ou
     if tables is None:
         tab, stab = gather_tables(packed_slices, scale_slices)
         if stream is not None:
-            st = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+            st = _stream_object(stream, dev)
             tab.record_stream(st)
             stab.record_stream(st)
     else:
@@ -363,7 +366,7 @@ def qwz_dequant_gemm(x, codes, scales, N, block=256, y=None, stream=None):
     _need(codes, "codes", N * K, _I8)
     _need(scales, "scales", _nsc(N * K, block), _F32)
     if y is None:
-        y = torch.empty((M, N), dtype=torch.float32, device=x.device)
+        y = _output((M, N), torch.float32, x.device, stream)
     _need(y, "y", M * N, _F32)
     _check(lib().qwz_dequant_gemm(_dev(x, "x"), _TORCH_DT[x.dtype], _dev(codes, "codes"), _dev(scales, "scales"),
                                   M, N, K, block, _dev(y, "y"), _stream(stream)), "qwz_dequant_gemm")

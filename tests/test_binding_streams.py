@@ -6,6 +6,7 @@ the allocator hears of a stream object's use.  Without that, memory freed with w
 pending is written by that work while the call uses it."""
 import contextlib
 import ctypes
+import sys
 
 import pytest
 import torch
@@ -25,6 +26,7 @@ class Stream:
 class Memory(torch.Tensor):
     """A tensor that says on which streams it is recorded."""
     log = None
+    is_cuda = True
 
     def record_stream(self, stream):
         self.log.append(("record", self.kind, stream.cuda_stream))
@@ -54,7 +56,7 @@ class Torch:
 
     def empty(self, *size, dtype=None, device=None):
         t = torch.empty(*size, dtype=dtype).as_subclass(Memory)
-        t.log, t.kind = self.log, "workspace" if dtype == torch.uint8 else "output"
+        t.log, t.kind = self.log, "workspace" if sys._getframe(1).f_code.co_name == "_workspace" else "output"
         self.log.append(("empty", t.kind, self.now.cuda_stream))
         return t
 
@@ -86,7 +88,17 @@ def log(monkeypatch):
 IDS, DY, TABLE = torch.zeros(6, dtype=torch.int64), torch.zeros(6, 8), torch.zeros(10, 8)
 X, CODES = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(64, dtype=torch.uint8)
 GRADS = zq.GradTable([DY], [None], _lib._GradPlan(), torch.zeros(64, dtype=torch.uint8))
+U8, F32 = torch.zeros(128, dtype=torch.uint8), torch.zeros(128)
 CALLS = {
+    "qwz_quantize": lambda s: zq.qwz_quantize(DY, 32, stream=s),
+    "qwz_dequantize": lambda s: zq.qwz_dequantize(torch.zeros(64, dtype=torch.int8), F32, 32, stream=s),
+    "qgz_quantize": lambda s: zq.qgz_quantize(DY, 32, stream=s),
+    "qgz_dequantize": lambda s: zq.qgz_dequantize(U8, F32, 64, 32, stream=s),
+    "qgz_reduce_level": lambda s: zq.qgz_reduce_level(U8, F32, 2, 64, 32, stream=s),
+    "qgz_reduce_dequantize": lambda s: zq.qgz_reduce_dequantize(U8, F32, 2, 64, 32, stream=s),
+    "qgz_reduce_level_gather": lambda s: zq.qgz_reduce_level_gather([U8, U8], [F32, F32], 64, 32, stream=s,
+                                                                    tables=(IDS, IDS)),
+    "qwz_dequant_gemm": lambda s: zq.qwz_dequant_gemm(X, torch.zeros(128, dtype=torch.int8), F32, 2, 32, stream=s),
     "embedding": lambda s: zq.embedding(IDS, TABLE, stream=s),
     "qwz_embedding": lambda s: zq.qwz_embedding(IDS, torch.zeros(80, dtype=torch.int8), torch.zeros(1), 10, 8, stream=s),
     "embedding_grad": lambda s: zq.embedding_grad(IDS, DY, 10, stream=s),
@@ -102,8 +114,9 @@ def test_memory_of_a_call_on_another_stream(log, name, kind):
     call = [i for i, e in enumerate(log) if e[0] == "call"]
     assert len(call) == 1 and log[call[0]][2] == 7
     assert ("empty", "workspace", 1) not in log, "a workspace from the current stream's pool"
-    out = log.index(("empty", "output", 1))
-    assert out < log.index(("wait", 7, 1)) < call[0], "the output's memory may have pending work"
+    outs = [i for i, e in enumerate(log) if e == ("empty", "output", 1)]
+    waits = [i for i, e in enumerate(log) if e == ("wait", 7, 1)]
+    assert outs and waits and outs[-1] < waits[-1] < call[0], "the output's memory may have pending work"
     # a handle's stream may be gone when the output is freed
     assert (("record", "output", 7) in log) == (kind == "stream")
 

@@ -66,3 +66,38 @@ def test_pending_work_on_freed_memory(make, kind, given):
     got = call(stream=side if kind == "stream" else side.cuda_stream, **({name: out} if given else {}))
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def path_calls():
+    n, block = 40_000, 64
+    x = torch.randn(n, generator=torch.Generator().manual_seed(6)).to(DEV)
+    codes, cs = zq.qwz_quantize(x, block)
+    packed, ps = zq.qgz_quantize(x, block)
+    pair, pair_s = torch.cat([packed, packed]), torch.cat([ps, ps])
+    xb = x[:6400].view(10, 640).bfloat16()
+    return {
+        "qwz_quantize": (lambda **k: zq.qwz_quantize(x, block, **k), [n, 4 * len(ps)]),
+        "qwz_dequantize": (lambda **k: zq.qwz_dequantize(codes, cs, block, **k), [2 * n]),
+        "qgz_quantize": (lambda **k: zq.qgz_quantize(x, block, **k), [n // 2, 4 * len(ps)]),
+        "qgz_dequantize": (lambda **k: zq.qgz_dequantize(packed, ps, n, block, **k), [4 * n]),
+        "qgz_reduce_level": (lambda **k: zq.qgz_reduce_level(pair, pair_s, 2, n, block, **k), [n // 2, 4 * len(ps)]),
+        "qgz_reduce_dequantize": (lambda **k: zq.qgz_reduce_dequantize(pair, pair_s, 2, n, block, **k), [4 * n]),
+        "qgz_reduce_level_gather": (lambda **k: zq.qgz_reduce_level_gather([packed, packed], [ps, ps], n, block, **k),
+                                    [n // 2, 4 * len(ps)]),
+        "qwz_dequant_gemm": (lambda **k: zq.qwz_dequant_gemm(xb, codes[:62 * 640], cs, 62, block, **k), [10 * 62 * 4]),
+    }
+
+
+@pytest.mark.parametrize("name", ["qwz_quantize", "qwz_dequantize", "qgz_quantize", "qgz_dequantize",
+                                  "qgz_reduce_level", "qgz_reduce_dequantize", "qgz_reduce_level_gather",
+                                  "qwz_dequant_gemm"])
+def test_pending_work_on_a_path_calls_output(name):
+    call, sizes = path_calls()[name]
+    want = call()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    pending(sizes)
+    got = call(stream=side)
+    torch.cuda.synchronize()
+    for g, w in zip(*((v if isinstance(v, tuple) else (v,)) for v in (got, want))):
+        assert torch.equal(g, w)
