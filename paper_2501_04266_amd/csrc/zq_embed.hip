@@ -60,9 +60,10 @@ __device__ __forceinline__ int64_t id_at(const void* ids, bool wide, int64_t t) 
 // the columns by XCD, so that each XCD's L2 holds other columns, measured slower (65).
 template <int WT, int YT, int E>
 __global__ void __launch_bounds__(kEmbedThreads)
-    k_embed(const void* __restrict__ ids, bool wide, const void* __restrict__ table, const float* __restrict__ scales,
-            int64_t T, int64_t V, int64_t D, int C, double inv_c, int lgB, float scale, void* __restrict__ y) {
-  const Piece p = locate(blockIdx.x, C, inv_c);
+    k_embed(unsigned first, const void* __restrict__ ids, bool wide, const void* __restrict__ table,
+            const float* __restrict__ scales, int64_t T, int64_t V, int64_t D, int C, double inv_c, int lgB, float scale,
+            void* __restrict__ y) {
+  const Piece p = locate(first + blockIdx.x, C, inv_c);
   if (p.row >= T) return;
   const int64_t id = id_at(ids, wide, p.row);
   const int64_t d0 = (int64_t)p.piece * E;
@@ -365,11 +366,13 @@ __device__ __forceinline__ bool is_long(int s, int e) { return (s + kPart - 1) /
 // write the rows that are not long.
 template <int GT, int YT, int E, bool ADD>
 __global__ void __launch_bounds__(kEmbedThreads)
-    k_grad_rows(const void* __restrict__ ids, bool wide, const char* __restrict__ dy, const int* __restrict__ start,
-                const int* __restrict__ order, int segs, unsigned seg_groups, float* __restrict__ parts, int64_t V,
-                int64_t D, int C, int per, double inv_per, float scale, void* __restrict__ dw) {
-  const bool seg = blockIdx.x < seg_groups;
-  const WaveRow w = wave_row(seg ? blockIdx.x : blockIdx.x - seg_groups, per, inv_per);
+    k_grad_rows(unsigned first, const void* __restrict__ ids, bool wide, const char* __restrict__ dy,
+                const int* __restrict__ start, const int* __restrict__ order, int segs, unsigned seg_groups,
+                float* __restrict__ parts, int64_t V, int64_t D, int C, int per, double inv_per, float scale,
+                void* __restrict__ dw) {
+  const unsigned group = first + blockIdx.x;
+  const bool seg = group < seg_groups;
+  const WaveRow w = wave_row(seg ? group : group - seg_groups, per, inv_per);
   const int c = w.sub * 64 + (threadIdx.x & 63);
   const unsigned d = (unsigned)piece_column<E>(c, C, D);
   if (seg) {
@@ -402,10 +405,10 @@ __global__ void __launch_bounds__(kEmbedThreads)
 // The long rows' sums, each by the waves of its first whole segment.
 template <int YT, int E, bool ADD>
 __global__ void __launch_bounds__(kEmbedThreads)
-    k_grad_join(const void* __restrict__ ids, bool wide, const int* __restrict__ start, const int* __restrict__ order,
-                int segs, const float* __restrict__ parts, int64_t V, int64_t D, int C, int per, double inv_per,
-                float scale, void* __restrict__ dw) {
-  const WaveRow w = wave_row(blockIdx.x, per, inv_per);
+    k_grad_join(unsigned first, const void* __restrict__ ids, bool wide, const int* __restrict__ start,
+                const int* __restrict__ order, int segs, const float* __restrict__ parts, int64_t V, int64_t D, int C,
+                int per, double inv_per, float scale, void* __restrict__ dw) {
+  const WaveRow w = wave_row(first + blockIdx.x, per, inv_per);
   const int j = (int)w.row, p0 = j * kPart;
   if (j >= segs || p0 + kPart > start[V]) return;
   const int64_t row = id_at(ids, wide, order[p0]);
@@ -518,8 +521,8 @@ __global__ void __launch_bounds__(kEmbedThreads)
 
 // ---------------------------------------------------------------- dispatch
 
-using EmbedKernel = void (*)(const void*, bool, const void*, const float*, int64_t, int64_t, int64_t, int, double, int,
-                             float, void*);
+using EmbedKernel = void (*)(unsigned, const void*, bool, const void*, const float*, int64_t, int64_t, int64_t, int,
+                             double, int, float, void*);
 // columns of a piece: 16 bytes of the result (1 column where rows are shorter than 8)
 template <int YT>
 constexpr int piece_of() {
@@ -544,10 +547,10 @@ EmbedKernel embed_kernel(int wt, int yt, bool short_rows) {
                         : embed_kernel_to<ZQ_BF16>(yt, short_rows);
 }
 
-using RowsKernel = void (*)(const void*, bool, const char*, const int*, const int*, int, unsigned, float*, int64_t,
-                            int64_t, int, int, double, float, void*);
-using JoinKernel = void (*)(const void*, bool, const int*, const int*, int, const float*, int64_t, int64_t, int, int,
-                            double, float, void*);
+using RowsKernel = void (*)(unsigned, const void*, bool, const char*, const int*, const int*, int, unsigned, float*,
+                            int64_t, int64_t, int, int, double, float, void*);
+using JoinKernel = void (*)(unsigned, const void*, bool, const int*, const int*, int, const float*, int64_t, int64_t,
+                            int, int, double, float, void*);
 template <int GT, int YT, int E>
 RowsKernel rows_kernel_add(bool add) {
   return add ? &k_grad_rows<GT, YT, E, true> : &k_grad_rows<GT, YT, E, false>;
@@ -623,9 +626,8 @@ int embed(const void* ids, int it, int64_t T, const void* table, const float* sc
   const int64_t E = short_rows ? 1 : lookup_piece(wt, yt), C = (D + E - 1) / E;
   const int64_t grid = grid_for(T * C, kEmbedThreads);
   if (grid == 0) return ZQ_E_SIZE;
-  return launch(embed_kernel(wt, yt, short_rows), (unsigned)grid, kEmbedThreads,
-                static_cast<hipStream_t>(stream), ids, it == ZQ_I64, table, scales, T, V, D, (int)C, 1.0 / (double)C,
-                lgB, scale, y);
+  return launch_parts(embed_kernel(wt, yt, short_rows), grid, kEmbedThreads, static_cast<hipStream_t>(stream), ids,
+                      it == ZQ_I64, table, scales, T, V, D, (int)C, 1.0 / (double)C, lgB, scale, y);
 }
 
 // One launch for few tokens, unless the result is so large that the order it is written
@@ -718,12 +720,12 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
                         : launch(&k_sort_ids<int32_t>, (unsigned)sorts, kSortThreads, st,
                                  static_cast<const int32_t*>(ids), (int)T, V, parts, start, order);
   if (rc != ZQ_OK) return rc;
-  rc = launch(rows_kernel(gt, wt, short_rows, add), (unsigned)(row_groups + seg_groups), kEmbedThreads, st, ids,
-              it == ZQ_I64, static_cast<const char*>(dy), start, order, (int)segs, (unsigned)seg_groups, sums, V, D,
-              (int)C, (int)per, 1.0 / (double)per, scale, dw);
+  rc = launch_parts(rows_kernel(gt, wt, short_rows, add), row_groups + seg_groups, kEmbedThreads, st, ids, it == ZQ_I64,
+                    static_cast<const char*>(dy), start, order, (int)segs, (unsigned)seg_groups, sums, V, D, (int)C,
+                    (int)per, 1.0 / (double)per, scale, dw);
   if (rc != ZQ_OK || segs == 0) return rc;
-  return launch(join_kernel(wt, short_rows, add), (unsigned)seg_groups, kEmbedThreads, st, ids, it == ZQ_I64, start,
-                order, (int)segs, sums, V, D, (int)C, (int)per, 1.0 / (double)per, scale, dw);
+  return launch_parts(join_kernel(wt, short_rows, add), seg_groups, kEmbedThreads, st, ids, it == ZQ_I64, start, order,
+                      (int)segs, sums, V, D, (int)C, (int)per, 1.0 / (double)per, scale, dw);
 }
 
 }  // extern "C"

@@ -14,7 +14,11 @@
 
 namespace zq {
 
-constexpr int64_t kMaxGrid = 0x7fffffff;  // workgroups per launch
+constexpr int64_t kMaxGrid = 0x7fffffff;  // workgroups of a call
+// A launch has fewer than 2^32 work items a dimension.  The runtime does not refuse
+// more: it launches their number modulo 2^32.
+constexpr uint64_t kMaxItems = 0xffffffffu;
+inline unsigned most_groups(unsigned block) { return (unsigned)(kMaxItems / block); }
 
 // Workgroups to cover `units` at `units_per_wg` each (0 if it exceeds the
 // launch limit; callers turn that into ZQ_E_SIZE before anything is enqueued).
@@ -25,9 +29,10 @@ inline int64_t grid_for(int64_t units, int64_t units_per_wg) {
 }
 
 // Launch with the kernel's exact parameter types; returns ZQ_E_HIP when the
-// runtime rejects the launch.
+// runtime rejects the launch, ZQ_E_SIZE for more work items than one can have.
 template <typename... KArgs, typename... Args>
 inline int launch(void (*kern)(KArgs...), unsigned grid, unsigned block, hipStream_t st, Args&&... args) {
+  if (grid > most_groups(block)) return ZQ_E_SIZE;
   std::tuple<KArgs...> tup(std::forward<Args>(args)...);
   void* argv[sizeof...(KArgs)];
   std::apply([&](auto&... a) {
@@ -36,6 +41,20 @@ inline int launch(void (*kern)(KArgs...), unsigned grid, unsigned block, hipStre
   }, tup);
   hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kern), dim3(grid), dim3(block), argv, 0, st);
   return e == hipSuccess ? ZQ_OK : ZQ_E_HIP;
+}
+
+// Any number of workgroups up to kMaxGrid, in as many launches as they take: the
+// kernel's first argument is the launch's first workgroup.
+template <typename... KArgs, typename... Args>
+inline int launch_parts(void (*kern)(unsigned, KArgs...), int64_t groups, unsigned block, hipStream_t st,
+                        const Args&... args) {
+  const int64_t most = most_groups(block);
+  for (int64_t first = 0; first < groups; first += most) {
+    const int rc = launch(kern, (unsigned)(groups - first < most ? groups - first : most), block, st, (unsigned)first,
+                          args...);
+    if (rc != ZQ_OK) return rc;
+  }
+  return ZQ_OK;
 }
 
 inline int log2_block(int32_t block) {

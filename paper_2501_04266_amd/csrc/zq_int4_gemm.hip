@@ -664,8 +664,8 @@ __global__ void __launch_bounds__(kGemmThreads, 4)
 // The slices' sums, in the order of the slices.  16 rows of 6,144 columns, 2 slices: 2 us.
 constexpr int kJoinThreads = 256;
 __global__ void __launch_bounds__(kJoinThreads)
-    k_int4_join(const float* __restrict__ planes, int64_t n, int count, float* __restrict__ y) {
-  const int64_t i = (int64_t)blockIdx.x * kJoinThreads + threadIdx.x;
+    k_int4_join(unsigned first, const float* __restrict__ planes, int64_t n, int count, float* __restrict__ y) {
+  const int64_t i = (int64_t)(first + blockIdx.x) * kJoinThreads + threadIdx.x;
   if (i >= n) return;
   float v = 0.0f;
   for (int z = 0; z < count; ++z) v += planes[z * n + i];
@@ -779,7 +779,8 @@ inline Int4Plan int4_plan(int64_t M, int64_t N, int64_t K) {
       const int MT = M <= 32 ? 2 : M <= 48 ? 3 : 4;
       const double piece = 7000 * (MT == 2 ? 1.15 : MT == 3 ? 1.44 : 1.87);
       const int64_t grid = (tiles + kWaves - 1) / kWaves, mgroups = (M + 16 * MT - 1) / (16 * MT);
-      for (int64_t S = 1; S == 1 || (S <= 16 && S <= K / 512); ++S) {
+      // k_int4_regs, whose workgroups share the tiles out, where one launch has no room for a tile a wave
+      for (int64_t S = 1; grid <= most_groups(kGemmThreads) && (S == 1 || (S <= 16 && S <= K / 512)); ++S) {
         const double w = (double)grid * (double)(mgroups * S) / kCus, even = 0.45 + 0.9 * w;
         const double turns = even < 1.0 ? 1.0 : even < __builtin_ceil(w) ? even : __builtin_ceil(w);
         const double load = turns * (double)(slice_of(K, S) / kPiece + 1.5) * piece +
@@ -864,5 +865,5 @@ extern "C" int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* p
                                        dim3(kGemmThreads), args, (size_t)p.lds, st);
   if (e != hipSuccess) return ZQ_E_HIP;
   if (p.slices == 1) return ZQ_OK;
-  return launch(&k_int4_join, (unsigned)joins, (unsigned)kJoinThreads, st, out, M * N, (int)p.slices, y);
+  return launch_parts(&k_int4_join, joins, (unsigned)kJoinThreads, st, out, M * N, (int)p.slices, y);
 }

@@ -310,16 +310,17 @@ __device__ __forceinline__ void scale_to(const Entry& en, int64_t e0, float c) {
 }
 
 __global__ void __launch_bounds__(kNormThreads)
-    k_grad_clip(const char* __restrict__ table, int count, const float* __restrict__ norm, float max_norm,
-                float scale) {
+    k_grad_clip(unsigned first, const char* __restrict__ table, int count, const float* __restrict__ norm,
+                float max_norm, float scale) {
   const int* entry_of = reinterpret_cast<const int*>(table + map_at(count));
-  const Entry en = reinterpret_cast<const Entry*>(table + clip_at(count))[entry_of[blockIdx.x]];
+  const unsigned piece = first + blockIdx.x;
+  const Entry en = reinterpret_cast<const Entry*>(table + clip_at(count))[entry_of[piece]];
   const float ratio = max_norm / (*norm + 1e-6f);
   // a NaN ratio stays: min would drop it
   const float c = scale * (ratio > 1.0f ? 1.0f : ratio);
   // in place and nothing to scale: the tensor stays as it is
   if (en.out == en.data && c == 1.0f) return;
-  const int64_t e0 = ((int64_t)blockIdx.x - en.chunk0) * kClipElems;
+  const int64_t e0 = ((int64_t)piece - en.chunk0) * kClipElems;
   switch (en.out_type) {
     case ZQ_F32: scale_to<ZQ_F32>(en, e0, c); break;
     case ZQ_F16: scale_to<ZQ_F16>(en, e0, c); break;
@@ -489,8 +490,8 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
   if (!aligned(table, 16) || !aligned(norm, 4)) return ZQ_E_ALIGN;
   if (!(max_norm >= 0.0f)) return ZQ_E_SIZE;
   if (plan->clip_chunks == 0) return ZQ_OK;
-  return launch(&k_grad_clip, (unsigned)plan->clip_chunks, kNormThreads, static_cast<hipStream_t>(stream),
-                static_cast<const char*>(table), plan->count, norm, max_norm, scale);
+  return launch_parts(&k_grad_clip, plan->clip_chunks, kNormThreads, static_cast<hipStream_t>(stream),
+                      static_cast<const char*>(table), plan->count, norm, max_norm, scale);
 }
 
 }  // extern "C"
