@@ -119,9 +119,16 @@ constexpr int kRangeBits = 9, kMaxRange = 1 << kRangeBits;  // rows of a workgro
 constexpr int kPart = 64;        // positions of a segment
 constexpr int64_t kMaxTokens = 1 << 30;
 
+// What this wave's lanes wrote and read in LDS before comes before what they do after.
+__device__ __forceinline__ void order_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // This lane's place among the tokens of its row: the row's count so far (in the
 // wave's `counts`) and the lanes of the same row before it; the counts move on.
-// The lanes of one row are found by comparing the rows bit by bit.
+// The lanes of one row are found by comparing the rows bit by bit.  Lanes that are not
+// `in` give row 0 and get a place of no meaning.
 __device__ __forceinline__ int take_place(int* counts, bool in, int row) {
   const uint64_t all = __ballot(in);
   uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
@@ -132,16 +139,14 @@ __device__ __forceinline__ int take_place(int* counts, bool in, int row) {
     lo &= ~((uint32_t)set ^ mine);
     hi &= ~((uint32_t)(set >> 32) ^ mine);
   }
-  int place = 0;
-  if (in) {
-    const int before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
-    const int base = counts[row];
-    place = base + before;
-    if (before == 0) counts[row] = base + __popc(lo) + __popc(hi);
-  }
-  // the next group's reads come after this group's writes
-  __builtin_amdgcn_wave_barrier();
-  return place;
+  const int before = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+  // All lanes of a row read its count before the first of them moves it on, and the next
+  // group's lanes read it after that: lanes of one wave, so the fence costs no wait of its own.
+  const int base = counts[row];
+  order_lds();
+  if (in && before == 0) counts[row] = base + __popc(lo) + __popc(hi);
+  order_lds();
+  return base + before;
 }
 
 constexpr int kSortSteps = 8;   // groups of 64 ids that a wave loads at a time
