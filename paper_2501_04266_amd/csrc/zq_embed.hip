@@ -318,8 +318,6 @@ __device__ __forceinline__ void add_tokens(const char* dy, const int* order, int
     };
     int b = 0;
     for (; b + kMost <= n; b += kMost) batch(b, std::integral_constant<int, kMost>{});
-    if constexpr (kMost > 8)
-      if (n - b >= 8) batch(b, std::integral_constant<int, 8>{}), b += 8;
     if constexpr (kMost > 4)
       if (n - b >= 4) batch(b, std::integral_constant<int, 4>{}), b += 4;
     if (n - b >= 2) batch(b, std::integral_constant<int, 2>{}), b += 2;
