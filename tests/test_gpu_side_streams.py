@@ -103,3 +103,18 @@ def test_pending_work_on_a_path_calls_output(name):
     torch.cuda.synchronize()
     for g, w in zip(*((v if isinstance(v, tuple) else (v,)) for v in (got, want))):
         assert torch.equal(g, w)
+
+
+def test_one_table_on_two_streams():
+    """Calls that share a table's partial sums write the same ones."""
+    grads = [torch.randn(n, generator=torch.Generator().manual_seed(n)).to(DEV) for n in (20_000_000, 3, 5_000_001)]
+    table = zq.grad_table(grads)
+    want = zq.grad_norm(table)
+    outs = [torch.zeros(20, device=DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(20):
+        for out, st in zip(outs, streams):
+            zq.grad_norm(table, out=out[i], stream=st)
+    torch.cuda.synchronize()
+    assert all(bool((out == want).all()) for out in outs)
