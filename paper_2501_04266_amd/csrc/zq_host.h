@@ -11,14 +11,9 @@
 #include <utility>
 
 #include "zq.h"
+#include "zq_limits.h"
 
 namespace zq {
-
-constexpr int64_t kMaxGrid = 0x7fffffff;  // workgroups of a call
-// A launch has fewer than 2^32 work items a dimension.  The runtime does not refuse
-// more: it launches their number modulo 2^32.
-constexpr uint64_t kMaxItems = 0xffffffffu;
-inline unsigned most_groups(unsigned block) { return (unsigned)(kMaxItems / block); }
 
 // Workgroups to cover `units` at `units_per_wg` each (0 if it exceeds the
 // launch limit; callers turn that into ZQ_E_SIZE before anything is enqueued).
