@@ -302,8 +302,11 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
  * The weight is not narrowed: the codes' products are exact and summed in binary32 by
  * the matrix cores, each scale multiplies its block's sum (or a part of it), and these
  * are added in binary32, in a fixed order: within (K + 64) * 2^-23 * sum_k |x w| of
- * the exact value (where the scales are 2^-122 or more, or 0: the products with smaller
- * ones can fall below the normal numbers), the same bits in every run.
+ * the exact value, the same bits in every run.  The bound holds where sum_k |x w| is 0
+ * or from 2^-122 to the largest binary32 number and every x is 0 or of a magnitude from
+ * 2^-110 to below 2^122 (fp16 always is): up to 128 products x * q / 16 are summed before
+ * their scale is applied, which overflows beyond, and falls below the normal numbers
+ * under it, whatever the scale.
  *   x       [M][K] row-major, xt = ZQ_BF16 or ZQ_F16 (read)
  *   packed  [ceil(N*K/2)] INT4 codes of the N x K weight, row-major, scales
  *           [ceil(N*K/block)] floats (read)

@@ -562,7 +562,8 @@ def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, workspace=None, s
     """y[M, N] = x[M, K] @ W^T with W the N x K weight in the INT4 format (packed
     uint8 [N*K/2] row-major, scales [ceil(N*K/block)]: qgz_quantize of the weight),
     read as it is; meant for few rows.  x bf16 or fp16, y float32.  K must be a
-    multiple of 64.  workspace: uint8, int4_dequant_gemm_bytes(M, N, K) or more;
+    multiple of 64.  Codes are summed before they are scaled: bf16 x of 2^122 and more
+    may overflow, of less than 2^-110 lose bits.  workspace: uint8, int4_dequant_gemm_bytes(M, N, K) or more;
     allocated if not given."""
     if x.dim() != 2:
         raise ValueError("x must be 2-D [M, K]")
