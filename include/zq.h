@@ -234,7 +234,8 @@ int qwz_embedding(const void* ids, zq_dtype it, int64_t T, const int8_t* codes, 
  *   dy [T][D] of dtype gt (read), dw [V][D] of dtype wt (written)
  *   workspace: device memory of zq_embedding_grad_bytes(T, V, D) bytes or more, 16-byte
  *   aligned, the call's own until it has run (may be NULL where that is 0: few tokens).
- *   T, V <= 2^30 (ZQ_E_SIZE); a workspace that is too small is ZQ_E_SIZE too. */
+ *   T, V <= 2^30, and T * ceil(V / 512) <= 2^41, since every 512 rows look through all
+ *   ids (about 2 s for as many): else ZQ_E_SIZE, as is a workspace that is too small. */
 int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, zq_dtype gt, int64_t V, int64_t D,
                       float scale, int accumulate, void* dw, zq_dtype wt, void* workspace, int64_t workspace_bytes,
                       void* stream);

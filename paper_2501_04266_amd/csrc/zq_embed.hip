@@ -118,6 +118,9 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kRangeBits = 9, kMaxRange = 1 << kRangeBits;  // rows of a workgroup's range at most (36 KiB of LDS)
 constexpr int kPart = 64;        // positions of a segment
 constexpr int64_t kMaxTokens = 1 << 30;
+// Ids that the sorting workgroups read in all, every one of a range of rows the T ids:
+// 2^37 take about 0.1 s, so the most a call takes is about 2 s of the GPU.
+constexpr int64_t kMaxReads = int64_t(1) << 41;
 
 // What this wave's lanes wrote and read in LDS before comes before what they do after.
 __device__ __forceinline__ void order_lds() {
@@ -640,6 +643,8 @@ int embed(const void* ids, int it, int64_t T, const void* table, const float* sc
 // columns 45 us, 38 in three launches; 1,024 tokens took 100.
 bool in_one_launch(int64_t T, int64_t V, int64_t D) { return T <= kFewTokens && (D == 0 || V <= (1 << 27) / D); }
 
+int64_t ranges_of(int64_t V) { return (V + kMaxRange - 1) / kMaxRange; }
+
 // Workspace of the gradient: first positions (V + 1), the order (T), the segments'
 // sums (2 rows of D each), each from a 16-byte boundary on.
 int64_t up16(int64_t b) { return (b + 15) & ~(int64_t)15; }
@@ -667,6 +672,7 @@ int qwz_embedding(const void* ids, zq_dtype it, int64_t T, const int8_t* codes, 
 int64_t zq_embedding_grad_bytes(int64_t T, int64_t V, int64_t D) {
   if (T < 0 || T > kMaxTokens || V < 0 || V > kMaxTokens || D < 0 || D > kMaxRow) return -1;
   if (in_one_launch(T, V, D)) return 0;
+  if (T * ranges_of(V) > kMaxReads) return -1;
   return start_bytes(V) + order_bytes(T) + (T < kPart ? 0 : 8 * ((T + kPart - 1) / kPart) * D);
 }
 
@@ -713,7 +719,7 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
   // workgroup reads all ids (about T ranges parts 4e-7 us), while the parts share out
   // the work on the tokens of a range that most tokens fall into (T / parts 6e-4 us):
   // the least sum is at the square root of 1,700 / ranges.
-  const int64_t ranges = (V + kMaxRange - 1) / kMaxRange;
+  const int64_t ranges = ranges_of(V);
   int parts = 1;
   while (parts < 16 && (int64_t)(parts + 1) * 1024 <= T && (2 * parts + 1) * (2 * parts + 1) * ranges < 4 * 1700) ++parts;
   const int64_t sorts = ranges * parts;
