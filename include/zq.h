@@ -314,7 +314,9 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
  *   y       [M][N] float row-major (written)
  * K a multiple of 64, at most 2^22 (ZQ_E_SIZE); M, N >= 0 arbitrary; K = 0 writes
  * zeros.  x and packed 16-byte aligned, scales and y 4-byte aligned.  Meant for few
- * rows: the weight is read again for every 64 rows of x.
+ * rows: the weight is read again for every 64 rows of x.  (Up to 256 rows it is faster
+ * than dequantising the weight and a library's product: 24,576 x 6,144, 256 rows 124 us
+ * and 186; at 512 rows 235 and 208.)
  *   workspace: device memory of zq_int4_dequant_gemm_bytes(M, N, K) bytes or more, 4-byte
  *   aligned, the call's own until it has run (sums over slices of a long K; may be NULL
  *   where that is 0); one that is too small is ZQ_E_SIZE. */

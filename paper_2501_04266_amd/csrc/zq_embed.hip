@@ -56,8 +56,9 @@ __device__ __forceinline__ int64_t id_at(const void* ids, bool wide, int64_t t) 
 // row starts E before its end (it repeats elements of the piece before it where E does
 // not divide D); E = 1 serves rows shorter than 8.  y is written past the caches, which
 // are left to the table's rows: tokens repeat (16,384 tokens of 6,144 bf16 elements, ids
-// of frequency 1 / rank: 53 us, 5.1 TB/s, 64 with plain stores; from INT8 44 and 68).  Slices of
-// the columns by XCD, so that each XCD's L2 holds other columns, measured slower (65).
+// of frequency 1 / rank, three sets of inputs in turn: 57 us, 4.8 TB/s, 64 with plain stores;
+// from INT8 44 and 68; one set again and again 47).  Slices of the columns by XCD, so that
+// each XCD's L2 holds other columns, measured slower (65).
 template <int WT, int YT, int E>
 __global__ void __launch_bounds__(kEmbedThreads)
     k_embed(unsigned first, const void* __restrict__ ids, bool wide, const void* __restrict__ table,
@@ -99,9 +100,9 @@ __global__ void __launch_bounds__(kEmbedThreads)
 
 // ---------------------------------------------------------------- gradient
 //
-// 1. k_sort_ids (14 us for 16,384 of 50,000 rows, 18 for 40,001 of
-//    16,411: latency of the loads and the LDS counts): the tokens in the order of their ids, ties in the order of the
-//    tokens, and each row's first position in that order.  A workgroup owns a
+// 1. k_sort_ids (14 us for 16,384 tokens and 50,000 rows, 18 for 40,001 and 16,411:
+//    latency of the loads and the LDS counts): the tokens in the order of their ids, ties in
+//    the order of the tokens, and each row's first position in that order.  A workgroup owns a
 //    range of rows and a part of the tokens, and reads all ids: first it counts its
 //    rows' tokens, in its part and before and after it, and those of the rows before
 //    its own, which gives its place in the order without another workgroup's count;
@@ -115,7 +116,7 @@ __global__ void __launch_bounds__(kEmbedThreads)
 // Up to 512 tokens take k_grad_few instead, one launch.
 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kRangeBits = 9, kMaxRange = 1 << kRangeBits;  // rows of a workgroup's range at most (36 KiB of LDS)
+constexpr int kRangeBits = 9, kMaxRange = 1 << kRangeBits;  // rows of a workgroup's range at most (48 KiB of LDS)
 constexpr int kPart = 64;        // positions of a segment
 constexpr int64_t kMaxTokens = 1 << 30;
 // Ids that the sorting workgroups read in all, every one of a range of rows the T ids:
@@ -716,7 +717,8 @@ int zq_embedding_grad(const void* ids, zq_dtype it, int64_t T, const void* dy, z
   const int64_t row_groups = grid_for(V * per, kEmbedThreads / 64);
   if (row_groups == 0 || (segs && seg_groups == 0) || row_groups + seg_groups > kMaxGrid) return ZQ_E_SIZE;
   // Sorting workgroups: ranges of 512 rows, times parts of the tokens.  Every
-  // workgroup reads all ids (about T ranges parts 4e-7 us), while the parts share out
+  // workgroup reads all ids (about T ranges parts 4e-7 us; 8.5e-7 for millions of ids,
+  // which come from further away), while the parts share out
   // the work on the tokens of a range that most tokens fall into (T / parts 6e-4 us):
   // the least sum is at the square root of 1,700 / ranges.
   const int64_t ranges = ranges_of(V);

@@ -15,7 +15,7 @@
 // LDS in the order of the waves, the slices' sums in a second launch.
 //
 // What bounds it: the weight's bytes where they are many and the rows of x few
-// (5 rows, 50,001 x 6,144: 35 us, 4.7 TB/s of the 6.4 of a plain copy; 16 rows,
+// (5 rows, 50,001 x 6,144: 37 us, 4.5 TB/s of the 6.4 of a plain copy; 16 rows,
 // 40,000 x 6,144: 38 us), close behind it the instructions that turn codes into
 // operands (about 330 cycles of a SIMD for 2,048 codes: 13 a word for 8 codes,
 // the moves between lanes, the addresses).  Up to about 8 MiB of weight a launch
@@ -204,8 +204,8 @@ __device__ __forceinline__ void stage_x(u32x4* lds, __amdgpu_buffer_rsrc_t xres,
 // elements m, where g = c % 4.  The matrix cores have room for that (16 cycles of about
 // 150 per operand), and no lane needs codes that another one loaded, beyond the
 // transposition.  Each column has one scale, whatever the block size.  Two pieces in
-// flight (3 and 4 measured no faster).  One row, 18,432 x 6,144: 17 us; 24,576 x 6,144:
-// 21 us, 3.8 TB/s.
+// flight (3 and 4 measured no faster).  One row, 18,432 x 6,144: 16 us; 24,576 x 6,144:
+// 20 us, 4.0 TB/s; 6,144 x 24,576: 24 us.
 // MR: rows of x, 1, 2 or 4.
 template <int XT, int MR, int D>
 __global__ void __launch_bounds__(kGemmThreads)

@@ -61,7 +61,7 @@ class TiedEmbedding:
 
     def step(self):
         """Reduces the slices to their mean, clips it and updates the table; returns the
-        mean's norm (on the GPU)."""
+        mean's norm (on the GPU, in a buffer that the next step writes)."""
         zq.qgz_reduce_level(self.sent.view(-1), self.sent_scales.view(-1), self.batches, self.n, G_BLOCK,
                             packed_out=self.reduced, scales_out=self.reduced_scales)
         zq.grad_norm(self.grads, 1.0 / self.batches, out=self.norm)
