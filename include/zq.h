@@ -67,6 +67,8 @@ typedef int zq_dtype;
 enum { ZQ_F32 = 0, ZQ_F16 = 1, ZQ_BF16 = 2 };
 enum { ZQ_I32 = 3, ZQ_I64 = 4 };  /* token ids (embedding calls) */
 enum { ZQ_INT4 = 5 };             /* packed INT4 codes with block scales (gradient tables) */
+enum { ZQ_INT8 = 6 };             /* INT8 codes with block scales (the weight an AdamW step writes) */
+enum { ZQ_F8 = 7 };               /* 8-bit moments of an AdamW step with block scales */
 
 enum {
   ZQ_OK = 0,
@@ -323,6 +325,183 @@ int zq_grad_clip(const zq_grad_plan* plan, const void* table, const float* norm,
 int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, const float* scales, int64_t M, int64_t N,
                          int64_t K, int32_t block, float* y, void* workspace, int64_t workspace_bytes, void* stream);
 int64_t zq_int4_dequant_gemm_bytes(int64_t M, int64_t N, int64_t K); /* -1 for sizes outside the limits */
+
+/* ---- The optimizer's step ------------------------------------------------------
+ * One AdamW step over any number of tensors in one launch: the owner's shard of the
+ * optimizer states (Design, Optimizer-State Partitioning) updated from the gradient
+ * shards as the reduce levels leave them, clipped on the way, and the weight written
+ * in the form that is gathered next.  For every element, with t the step, fl() as
+ * above, and c = fl(scale * min(1, fl(max_norm / fl(norm[0] + 1e-6)))), or scale
+ * where norm is NULL:
+ *   g = fl(grad * c)                  an INT4 shard: fl(q * fl(s * c)), as zq_grad_clip
+ *   m = fl(fl(b1 * m) + fl(fl(1 - b1) * g))
+ *   v = fl(fl(b2 * v) + fl(fl(1 - b2) * fl(g * g)))
+ *   d = fl(fl(sqrt(v) * fl(1 / sqrt(1 - b2^t))) + eps)
+ *   p = cvt(fl(fl(p * fl(1 - lr * lr_scale * weight_decay))
+ *              - fl(fl(lr * lr_scale / (1 - b1^t)) * fl(m / d))))
+ * b1, b2 and eps rounded to binary32; what depends on the step or on lr computed in
+ * binary64 and rounded once.  A norm that is not finite leaves everything as it is.
+ *
+ * A tensor:
+ *   param  [n] of param_dtype (F32 / F16 / BF16), updated in place
+ *   grad   [n] of grad_dtype, or an INT4 shard (ZQ_INT4: packed codes at any address,
+ *          grad_scales, grad_block)
+ *   m, v   [n] floats (state_dtype ZQ_F32), or ZQ_F8: a byte an element and a float a
+ *          block of state_block elements (m_scales, v_scales [ceil(n/state_block)]); m as
+ *          e4m3 (OCP: 4 exponent bits of bias 7, 3 mantissa bits, largest 448), v as e5m2
+ *          (bias 15, largest 57344; never negative), times their block's scale.  All zero
+ *          bytes and scales are a fresh state.
+ *   out    NULL, or what receives the new weight beside param: [n] of out_dtype (rounded
+ *          from param as stored), or ZQ_INT8: what qwz_quantize of the new param writes
+ *          (int8 codes at any address, out_scales, out_block)
+ * Writing 8-bit moments: a = largest magnitude of the block, top = 448 or 57344; a below
+ * 2^-110: scale 0 and codes 0; else scale = fl(a / top), and fl(|x| * fl(top / a)) is
+ * rounded to a neighbouring code, up with the chance of the part cut off (16 bits of it),
+ * so that changes smaller than a step are kept on average: nearest rounding would lose
+ * every change of v by less than an eighth.  The bits drawn for element i of tensor k are
+ * a function of (t, k, i) alone: the same step gives the same result.  With w = mix(key ^
+ * (i mod 2^32)), key = mix(mix(mix(t) + k * 0x9E3779B9) + i / 2^32) (the outer mix only
+ * where i / 2^32 > 0), mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *=
+ * 0x3B67AE85, x ^= x >> 16 on 32 bits: m is rounded by w's low half, v by its high one.
+ * Elements that are not finite leave the codes of their block unspecified.
+ * Element arrays need the alignment of their elements, scales 4 bytes.  Nothing that is
+ * written may overlap anything else of the table. */
+typedef struct {
+  void* param;
+  const void* grad;
+  const float* grad_scales; /* ZQ_INT4 only */
+  void* m;
+  float* m_scales;          /* ZQ_F8 only */
+  void* v;
+  float* v_scales;          /* ZQ_F8 only */
+  void* out;
+  float* out_scales;        /* ZQ_INT8 only */
+  int64_t n;
+  double weight_decay;
+  double lr_scale;          /* of this tensor; 1 for the step's lr as it is */
+  int32_t param_dtype;
+  int32_t grad_dtype;
+  int32_t state_dtype;
+  int32_t out_dtype;        /* with out */
+  int32_t grad_block;       /* ZQ_INT4 only */
+  int32_t state_block;      /* ZQ_F8 only */
+  int32_t out_block;        /* ZQ_INT8 only */
+  int32_t reserved;
+} zq_adamw;
+
+/* Sizes of a table of tensors; filled by zq_adamw_plan_make. */
+typedef struct {
+  int64_t bytes; /* of the table */
+  int64_t pieces;
+  int32_t count;
+  int32_t reserved;
+} zq_adamw_plan;
+
+/* A step's numbers.  0 <= beta1, beta2 < 1, eps >= 0, step >= 1, lr finite, and with a
+ * norm max_norm >= 0 (else ZQ_E_SIZE). */
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t step;   /* 1 for the first */
+  float max_norm; /* with a norm */
+  float scale;    /* of the gradients: undoes a loss scale, averages micro-batches */
+} zq_adamw_args;
+
+/* As zq_grad_plan_make and zq_grad_plan_table: the checks and the table, host only.  The
+ * caller copies the table to 16-byte aligned device memory once for tensors that stay
+ * where they are.  Calls with one table must be ordered. */
+int zq_adamw_plan_make(const zq_adamw* tensors, int32_t count, zq_adamw_plan* plan);
+int zq_adamw_plan_table(const zq_adamw* tensors, const zq_adamw_plan* plan, void* host_table);
+
+/* The step.  plan and args on the host, table on the device.  norm: NULL, or a float on
+ * the device (zq_grad_norm's, called with the same scale).  step, lr: NULL, or an
+ * int64_t / a float on the device that is read in place of args' when the work runs
+ * (one more small launch), for calls captured into a graph; a step below 1 there counts
+ * as 1. */
+int zq_adamw_step(const zq_adamw_plan* plan, void* table, const zq_adamw_args* args, const int64_t* step,
+                  const float* lr, const float* norm, void* stream);
+
+/* ---- RMS norm -------------------------------------------------------------------
+ * The root-mean-square norm of T rows of D elements, after the residual's addition:
+ *   h    = cvt(fl(x + residual))                     x itself without a residual
+ *   rstd = 1 / sqrt(sum_d h[t][d]^2 / D + eps)       in binary64, rounded once
+ *   y    = cvt(fl(fl(h * rstd) * weight))            weight NULL: cvt(fl(h * rstd))
+ *   x, residual (may be NULL) [T][D] of dtype xt, weight [D] of dtype wt (read)
+ *   h     [T][D] of xt: the sum, which is the next residual; required with a residual,
+ *         else NULL (nothing is written).  May be residual's or x's own memory.
+ *   y     [T][D] of yt, rstd [T] floats (NULL: not wanted) (written)
+ * D from 1 to 2^24, eps >= 0 (ZQ_E_SIZE).  Element arrays need the alignment of their
+ * elements; outputs overlap nothing but as said.  A row of zeros with eps 0 gives NaN. */
+int zq_rms_norm(const void* x, const void* residual, zq_dtype xt, const void* weight, zq_dtype wt, int64_t T,
+                int64_t D, double eps, void* h, void* y, zq_dtype yt, float* rstd, void* stream);
+
+/* qwz_rms_norm: the same with y in the INT8 format, the codes and scales that
+ * qwz_quantize gives for the binary32 values before the last rounding: an activation
+ * kept or sent at half of bf16.  D a multiple of block (ZQ_E_SIZE).
+ *   codes [T*D], scales [T*D/block] (written) */
+int qwz_rms_norm(const void* x, const void* residual, zq_dtype xt, const void* weight, zq_dtype wt, int64_t T,
+                 int64_t D, double eps, void* h, int8_t* codes, float* scales, int32_t block, float* rstd,
+                 void* stream);
+
+/* zq_rms_norm_grad: with xh = fl(h * rstd), gw = fl(dy * weight) (dy without a weight),
+ *   dx[t][d] = cvt(rstd * (gw - xh * sum_d(gw * xh) / D) + dh[t][d])
+ *   dw[d]    = cvt(sum_t dy[t][d] * xh[t][d])        accumulate != 0: added to what dw holds
+ * dx is the gradient of x and of residual alike; dh (may be NULL) is the one that reaches
+ * h by itself, along the residual's way.  Sums in binary32 in a fixed order that follows
+ * from T and D alone: the same bits in every run.
+ *   dy [T][D] of gt, h [T][D] of xt, weight [D] of wt (or NULL), rstd [T], dh [T][D] of xt
+ *   dx [T][D] of xt (may be dh's own memory), dw [D] of dwt (NULL: not wanted)
+ *   workspace: device memory of zq_rms_norm_grad_bytes(T, D) bytes or more, 16-byte
+ *   aligned, the call's own until it has run (may be NULL where that is 0) */
+int zq_rms_norm_grad(const void* dy, zq_dtype gt, const void* h, zq_dtype xt, const void* weight, zq_dtype wt,
+                     const float* rstd, const void* dh, int64_t T, int64_t D, void* dx, int accumulate, void* dw,
+                     zq_dtype dwt, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t zq_rms_norm_grad_bytes(int64_t T, int64_t D); /* -1 for sizes outside the limits */
+
+/* ---- The loss at the output head ------------------------------------------------
+ * Log-probabilities of given tokens, and the clipped policy loss with a KL term and its
+ * gradient, from rows of V logits.  Row t of logits starts at element t * ld (ld >= V:
+ * heads padded to a wider row).  A logit of -infinity names a token that cannot occur:
+ * probability and gradient 0.  An id outside [0, V), or a row without any logit above
+ * -infinity, names no token: logp 0, no loss, a gradient of zeros.
+ *
+ * zq_token_logp: logp[t] = scale * (z[a] - max z) - log(sum_v exp(scale * (z[v] - max z))),
+ * a = ids[t]; exponentials in binary32, the rest in binary64, rounded once.
+ *   logits of dtype lt, ids [T] of type it = ZQ_I32 or ZQ_I64 (read), logp [T] (written)
+ *   scale > 0: 1 / temperature.  V from 1 to 2^24, T <= 2^30 (ZQ_E_SIZE). */
+int zq_token_logp(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_t ld, const void* ids, zq_dtype it,
+                  float scale, float* logp, void* stream);
+
+/* What zq_policy_loss takes beside the logits: device arrays of T floats, and numbers. */
+typedef struct {
+  const float* old_logp;   /* of the policy that drew the tokens */
+  const float* advantages;
+  const float* weights;    /* of each token in the sums: 0 for one that is masked, whose
+                              other values may then be anything; NULL: 1 each */
+  const float* ref_logp;   /* of the reference policy; needed where kl != 0 */
+  float clip_low, clip_high; /* >= 0; clip_low <= 1 */
+  float kl;                /* factor of the KL term, >= 0; 0: none */
+  float scale;             /* of the logits, > 0: 1 / temperature */
+  float grad_scale;        /* of the gradient: a loss scale, the gradient of the loss */
+  int32_t reserved;
+} zq_policy;
+
+/* zq_policy_loss: with logp as above, r = exp(logp - old_logp), A = advantages, lo = 1 -
+ * clip_low, hi = 1 + clip_high, u = ref_logp - logp:
+ *   policy[t] = -min(r * A, clip(r, lo, hi) * A)       KL[t] = exp(u) - u - 1
+ *   sums = { sum w (policy + kl * KL), sum w policy, sum w KL, sum w [r is clipped] }
+ *   grad[t][v] = grad_scale * w * scale * (kl * (1 - exp(u)) - (r is clipped ? 0 : r * A))
+ *                * ((v == ids[t]) - softmax(scale * z)[v])
+ * r is clipped where A > 0 and r > hi, or A < 0 and r < lo.  Terms and sums are binary64,
+ * in a fixed order; sums[0] is the loss.
+ *   sums [4], logp [T] floats (written; logp NULL: not wanted)
+ *   grad rows of dtype gt from element t * ldg (ldg >= V; what lies between rows stays as
+ *        it is); may be logits itself with gt = lt and ldg = ld; NULL: not wanted
+ *   workspace: device memory of zq_policy_loss_bytes(T) bytes or more, 16-byte aligned,
+ *   the call's own until it has run */
+int zq_policy_loss(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_t ld, const void* ids, zq_dtype it,
+                   const zq_policy* policy, float* sums, float* logp, void* grad, zq_dtype gt, int64_t ldg,
+                   void* workspace, int64_t workspace_bytes, void* stream);
+int64_t zq_policy_loss_bytes(int64_t T); /* -1 for sizes outside the limits */
 
 /* Size helpers (host only): number of scales ceil(n/block) (-1 on a bad
  * block or n < 0), and INT4 bytes ceil(n/2) (-1 for n < 0). */

@@ -9,8 +9,12 @@ kernel does.
 from ._lib import (  # noqa: F401
     LIB_PATH,
     STATUS,
+    AdamWTable,
     GradTable,
     ZQError,
+    adamw_states,
+    adamw_step,
+    adamw_table,
     embedding,
     embedding_grad,
     embedding_grad_bytes,
@@ -23,6 +27,8 @@ from ._lib import (  # noqa: F401
     int4_dequant_gemm_bytes,
     lib,
     num_scales,
+    policy_loss,
+    policy_loss_bytes,
     qgz_dequantize,
     qgz_quantize,
     qgz_reduce_dequantize,
@@ -33,4 +39,9 @@ from ._lib import (  # noqa: F401
     qwz_dequantize,
     qwz_embedding,
     qwz_quantize,
+    qwz_rms_norm,
+    rms_norm,
+    rms_norm_grad,
+    rms_norm_grad_bytes,
+    token_logp,
 )

@@ -14,14 +14,16 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("ZQ_LIBRARY") or os.path.join(_PKG, "libzq.so")
 
 ZQ_F32, ZQ_F16, ZQ_BF16 = 0, 1, 2
-ZQ_I32, ZQ_I64, ZQ_INT4 = 3, 4, 5
+ZQ_I32, ZQ_I64, ZQ_INT4, ZQ_INT8, ZQ_F8 = 3, 4, 5, 6, 7
 STATUS = {0: "ZQ_OK", -1: "ZQ_E_NULL", -2: "ZQ_E_BLOCK", -3: "ZQ_E_DTYPE", -4: "ZQ_E_ALIGN",
           -5: "ZQ_E_SIZE", -6: "ZQ_E_P", -7: "ZQ_E_HIP", -8: "ZQ_E_ALIAS"}
 EXPORTS = ["qwz_quantize", "qwz_dequantize", "qgz_quantize", "qgz_reduce_level", "qgz_dequantize",
            "qgz_reduce_dequantize", "qgz_reduce_level_gather", "qgz_reduce_level_gather_noalloc",
            "qwz_dequant_gemm", "zq_embedding", "qwz_embedding", "zq_embedding_grad", "zq_embedding_grad_bytes",
            "zq_grad_plan_make", "zq_grad_plan_table", "zq_grad_norm", "zq_grad_clip", "zq_int4_dequant_gemm",
-           "zq_int4_dequant_gemm_bytes",
+           "zq_int4_dequant_gemm_bytes", "zq_adamw_plan_make", "zq_adamw_plan_table", "zq_adamw_step",
+           "zq_rms_norm", "qwz_rms_norm", "zq_rms_norm_grad", "zq_rms_norm_grad_bytes",
+           "zq_token_logp", "zq_policy_loss", "zq_policy_loss_bytes",
            "zq_num_scales", "zq_int4_bytes", "zq_status_string"]
 
 _TORCH_DT = {torch.float32: ZQ_F32, torch.float16: ZQ_F16, torch.bfloat16: ZQ_BF16}
@@ -41,6 +43,34 @@ class _GradPlan(ctypes.Structure):  # zq_grad_plan
                 ("count", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class _AdamW(ctypes.Structure):  # zq_adamw
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("grad_scales", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("m_scales", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("out", ctypes.c_void_p), ("out_scales", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double), ("lr_scale", ctypes.c_double),
+                ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("grad_block", ctypes.c_int32), ("state_block", ctypes.c_int32),
+                ("out_block", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _AdamWPlan(ctypes.Structure):  # zq_adamw_plan
+    _fields_ = [("bytes", ctypes.c_int64), ("pieces", ctypes.c_int64), ("count", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class _AdamWArgs(ctypes.Structure):  # zq_adamw_args
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("max_norm", ctypes.c_float),
+                ("scale", ctypes.c_float)]
+
+
+class _Policy(ctypes.Structure):  # zq_policy
+    _fields_ = [("old_logp", ctypes.c_void_p), ("advantages", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("ref_logp", ctypes.c_void_p), ("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float),
+                ("kl", ctypes.c_float), ("scale", ctypes.c_float), ("grad_scale", ctypes.c_float),
+                ("reserved", ctypes.c_int32)]
+
+
 class ZQError(RuntimeError):
     def __init__(self, status, what):
         self.status = status
@@ -56,6 +86,7 @@ def lib():
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2501_04266_amd.build`")
     L = ctypes.CDLL(LIB_PATH)
     vp, i64, i32, ci, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_float
+    f64 = ctypes.c_double
     sig = {
         "qwz_quantize": [vp, ci, i64, i32, vp, vp, vp],
         "qwz_dequantize": [vp, vp, i64, i32, vp, ci, vp],
@@ -74,6 +105,14 @@ def lib():
         "zq_grad_norm": [vp, vp, f32, vp, vp],
         "zq_grad_clip": [vp, vp, vp, f32, f32, vp],
         "zq_int4_dequant_gemm": [vp, ci, vp, vp, i64, i64, i64, i32, vp, vp, i64, vp],
+        "zq_adamw_plan_make": [vp, i32, vp],
+        "zq_adamw_plan_table": [vp, vp, vp],
+        "zq_adamw_step": [vp, vp, vp, vp, vp, vp, vp],
+        "zq_rms_norm": [vp, vp, ci, vp, ci, i64, i64, f64, vp, vp, ci, vp, vp],
+        "qwz_rms_norm": [vp, vp, ci, vp, ci, i64, i64, f64, vp, vp, vp, i32, vp, vp],
+        "zq_rms_norm_grad": [vp, ci, vp, ci, vp, ci, vp, vp, i64, i64, vp, ci, vp, ci, vp, i64, vp],
+        "zq_token_logp": [vp, ci, i64, i64, i64, vp, ci, f32, vp, vp],
+        "zq_policy_loss": [vp, ci, i64, i64, i64, vp, ci, vp, vp, vp, vp, ci, i64, vp, i64, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -82,6 +121,8 @@ def lib():
     L.zq_int4_bytes.argtypes, L.zq_int4_bytes.restype = [i64], i64
     L.zq_embedding_grad_bytes.argtypes, L.zq_embedding_grad_bytes.restype = [i64, i64, i64], i64
     L.zq_int4_dequant_gemm_bytes.argtypes, L.zq_int4_dequant_gemm_bytes.restype = [i64, i64, i64], i64
+    L.zq_rms_norm_grad_bytes.argtypes, L.zq_rms_norm_grad_bytes.restype = [i64, i64], i64
+    L.zq_policy_loss_bytes.argtypes, L.zq_policy_loss_bytes.restype = [i64], i64
     L.zq_status_string.argtypes, L.zq_status_string.restype = [ci], ctypes.c_char_p
     _lib = L
     return L
@@ -174,6 +215,8 @@ _U8 = (torch.uint8,)
 _F32 = (torch.float32,)
 _IDS = tuple(_ID_DT)
 _HALF = (torch.bfloat16, torch.float16)
+_I64 = (torch.int64,)
+_F8 = {"exp_avg": torch.float8_e4m3fn, "exp_avg_sq": torch.float8_e5m2}
 
 
 def _check(status, what):
@@ -579,3 +622,365 @@ def int4_dequant_gemm(x, packed, scales, N, block=128, y=None, workspace=None, s
                                       scales_at or _dev(scales, "scales"), M, N, K, block, y_at or _dev(y, "y"), at,
                                       size, _stream(stream)), "int4_dequant_gemm")
     return y
+
+
+def adamw_states(params, bits=32, block=256):
+    """Fresh moments for adamw_table: (exp_avg, exp_avg_sq), a list each with an entry per
+    parameter: binary32 zeros, or with bits=8 tuples (codes, scales, block) of float8 zeros
+    (e4m3 and e5m2) and a binary32 scale a block."""
+    if bits not in (32, 8):
+        raise ValueError(f"bits is {bits}; expected 32 or 8")
+    lists = []
+    for name in ("exp_avg", "exp_avg_sq"):
+        if bits == 32:
+            lists.append([torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in params])
+        else:
+            lists.append([(torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(_F8[name]),
+                           torch.zeros(_alloc_nsc(p.numel(), block), dtype=torch.float32, device=p.device), block)
+                          for p in params])
+    return tuple(lists)
+
+
+class AdamWTable:
+    """The tensors of an optimizer's step (adamw_table makes it).  Holds them; they may
+    change their values, not their places.  Calls with one table must be ordered (one
+    stream, or events)."""
+
+    def __init__(self, tensors, plan, table):
+        self.tensors, self.plan, self.table = tensors, plan, table
+        self.params = tensors[0]
+
+
+def _per_tensor(v, n, name):
+    v = list(v) if isinstance(v, (list, tuple)) else [v] * n
+    if len(v) != n:
+        raise ValueError(f"{len(v)} {name} for {n} parameters")
+    return v
+
+
+def adamw_table(params, grads, exp_avg, exp_avg_sq, outs=None, weight_decay=0.0, lr_scale=1.0):
+    """AdamWTable of a list of parameters (f32 / f16 / bf16, updated in place) with their
+    gradients and moments, built once for tensors that stay in place.
+    grads: dense tensors (f32 / f16 / bf16) or INT4 shards (packed, scales, n, block).
+    exp_avg, exp_avg_sq: float32 tensors, or (codes, scales, block) with codes
+    float8_e4m3fn and float8_e5m2 and scales float32 [ceil(n/block)] (adamw_states makes
+    either).  outs: None, or per parameter None, a dense tensor (f32 / f16 / bf16) that
+    receives the new weight, or (codes int8, scales, block): what qwz_quantize of it
+    writes.  weight_decay, lr_scale: numbers, or one per parameter."""
+    lists = [list(params), list(grads), list(exp_avg), list(exp_avg_sq)]
+    count = len(lists[0])
+    lists.append([None] * count if outs is None else list(outs))
+    for name, one in zip(("grads", "exp_avg", "exp_avg_sq", "outs"), lists[1:]):
+        if len(one) != count:
+            raise ValueError(f"{len(one)} {name} for {count} parameters")
+    decays, rates = _per_tensor(weight_decay, count, "weight_decay"), _per_tensor(lr_scale, count, "lr_scale")
+    entries = (_AdamW * max(1, count))()
+    dev = lists[0][0].device if count else None
+    for i, (p, g, m, v, o, e) in enumerate(zip(*lists, entries)):
+        def at(t, name, need, dtypes):
+            _need(t, f"{name}[{i}]", need, dtypes)
+            if t.device != dev:
+                raise ValueError(f"{name}[{i}] is on {t.device}, the parameters on {dev}")
+            return _dev(t, f"{name}[{i}]")
+        e.param, e.n = at(p, "params", 0, _ELEM), p.numel()
+        e.param_dtype, n = _TORCH_DT[p.dtype], e.n
+        if isinstance(g, (tuple, list)):
+            packed, scales, of, block = g
+            if of != n:
+                raise ValueError(f"grads[{i}] has {of} elements, its parameter {n}")
+            e.grad, e.grad_dtype, e.grad_block = at(packed, "grads", int4_bytes(n), _U8), ZQ_INT4, block
+            e.grad_scales = at(scales, "grads", _nsc(n, block), _F32)
+        else:
+            e.grad = at(g, "grads", n, _ELEM)
+            if g.numel() != n:
+                raise ValueError(f"grads[{i}] has {g.numel()} elements, its parameter {n}")
+            e.grad_dtype = _TORCH_DT[g.dtype]
+        if isinstance(m, (tuple, list)) != isinstance(v, (tuple, list)):
+            raise ValueError(f"exp_avg[{i}] and exp_avg_sq[{i}] are not held alike")
+        if isinstance(m, (tuple, list)):
+            if m[2] != v[2]:
+                raise ValueError(f"exp_avg[{i}] has blocks of {m[2]}, exp_avg_sq[{i}] of {v[2]}")
+            e.state_dtype, e.state_block = ZQ_F8, m[2]
+            e.m, e.v = at(m[0], "exp_avg", n, (_F8["exp_avg"],)), at(v[0], "exp_avg_sq", n, (_F8["exp_avg_sq"],))
+            e.m_scales = at(m[1], "exp_avg", _nsc(n, m[2]), _F32)
+            e.v_scales = at(v[1], "exp_avg_sq", _nsc(n, m[2]), _F32)
+        else:
+            e.state_dtype = ZQ_F32
+            e.m, e.v = at(m, "exp_avg", n, _F32), at(v, "exp_avg_sq", n, _F32)
+        if isinstance(o, (tuple, list)):
+            e.out, e.out_dtype, e.out_block = at(o[0], "outs", n, _I8), ZQ_INT8, o[2]
+            e.out_scales = at(o[1], "outs", _nsc(n, o[2]), _F32)
+        elif o is not None:
+            e.out = at(o, "outs", n, _ELEM)
+            e.out_dtype = _TORCH_DT[o.dtype]
+        e.weight_decay, e.lr_scale = decays[i], rates[i]
+    plan = _AdamWPlan()
+    _check(lib().zq_adamw_plan_make(entries, count, ctypes.byref(plan)), "adamw_table")
+    host = torch.zeros(plan.bytes, dtype=torch.uint8)
+    _check(lib().zq_adamw_plan_table(entries, ctypes.byref(plan), host.data_ptr()), "adamw_table")
+    return AdamWTable(lists, plan, host.to(dev or torch.device("cuda", torch.cuda.current_device())))
+
+
+def adamw_step(table, step, lr, betas=(0.9, 0.999), eps=1e-8, norm=None, max_norm=None, scale=1.0, stream=None):
+    """One AdamW step over an AdamWTable, in one launch; returns the parameters, updated
+    in place.  step counts from 1.  With norm (grad_norm's, on the GPU, called with the
+    same scale) gradients are clipped to max_norm on the way, as grad_clip does, and a
+    norm that is not finite leaves everything as it is; scale multiplies the gradients.
+    step (int64) and lr (float32) may be GPU tensors of one element, read when the work
+    runs: what a captured step needs to go on.  8-bit moments are rounded up or down by
+    bits that follow from the step, so the same step gives the same result."""
+    if not isinstance(table, AdamWTable):
+        raise TypeError("table must be an AdamWTable")
+    a = _AdamWArgs(0.0, betas[0], betas[1], eps, 0, 0.0, scale)
+    step_at = lr_at = norm_at = None
+    if isinstance(step, torch.Tensor):
+        _need(step, "step", 1, _I64)
+        step_at = _dev(step, "step")
+    else:
+        a.step = step
+    if isinstance(lr, torch.Tensor):
+        _need(lr, "lr", 1, _F32)
+        lr_at = _dev(lr, "lr")
+    else:
+        a.lr = lr
+    if norm is not None:
+        if max_norm is None:
+            raise ValueError("norm clips to max_norm: give it")
+        _need(norm, "norm", 1, _F32)
+        norm_at, a.max_norm = _dev(norm, "norm"), max_norm
+    _here(table=table.table, step=step if step_at else None, lr=lr if lr_at else None, norm=norm)
+    _check(lib().zq_adamw_step(ctypes.byref(table.plan), table.table.data_ptr(), ctypes.byref(a), step_at, lr_at,
+                               norm_at, _stream(stream)), "adamw_step")
+    return table.params
+
+
+def _here(**tensors):
+    """The call runs on the current device, and its tensors (None: not given) are there."""
+    now = torch._C._cuda_getDevice()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != now:
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{now}")
+
+
+def _rows(x, name="x"):
+    """(rows, row length) of a tensor whose last dimension is normed."""
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"{name} has shape {tuple(x.shape)}; expected [..., D]")
+    return x.numel() // x.shape[-1], x.shape[-1]
+
+
+def _like(t, name, x, dtypes):
+    """The address of a tensor of x's shape (None stays None)."""
+    if t is None:
+        return None
+    at = _ptr(t, name, x.numel(), dtypes)
+    if t.shape != x.shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; expected {tuple(x.shape)}")
+    return at or _dev(t, name)
+
+
+def _weight(weight, D):
+    """(address, dtype code) of a norm's weight, which may be None."""
+    if weight is None:
+        return None, ZQ_F32
+    at = _ptr(weight, "weight", D, _ELEM)
+    if weight.numel() != D:
+        raise ValueError(f"weight holds {weight.numel()} elements; rows have {D}")
+    return at or _dev(weight, "weight"), _TORCH_DT[weight.dtype]
+
+
+def _rms_args(x, weight, residual, hidden, rstd, stream):
+    T, D = _rows(x)
+    x_at = _ptr(x, "x", T * D, _ELEM) or _dev(x, "x")
+    w_at, wt = _weight(weight, D)
+    res_at = _like(residual, "residual", x, (x.dtype,))
+    if residual is None:
+        if hidden is not None:
+            raise ValueError("hidden receives x + residual: give the residual")
+        hidden = x
+    elif hidden is None:
+        hidden = _output(stream, x.device, x.dtype, *x.shape)
+    h_at = _like(hidden, "hidden", x, (x.dtype,)) if residual is not None else None
+    if rstd is None:
+        rstd = _output(stream, x.device, torch.float32, T)
+    r_at = _ptr(rstd, "rstd", T, _F32) or _dev(rstd, "rstd")
+    _here(x=x, weight=weight, residual=residual, hidden=hidden, rstd=rstd)
+    return T, D, x_at, w_at, wt, res_at, hidden, h_at, rstd, r_at
+
+
+def rms_norm(x, weight, residual=None, eps=1e-6, out_dtype=None, out=None, hidden=None, rstd=None, stream=None):
+    """Root-mean-square norm of x's last dimension after the residual's addition:
+    (y, h, rstd) with h = x + residual (x itself without one), rstd = 1 / sqrt(mean(h^2)
+    + eps) of each row (binary64, rounded once) and y = h * rstd * weight.  x f32 / f16 /
+    bf16 [..., D], residual of its type and shape, weight f32 / f16 / bf16 [D] or None
+    (ones); y of out_dtype (x's if not given).  out, hidden, rstd: where y, h and rstd go;
+    hidden may be residual or x itself.  h and rstd are what rms_norm_grad takes."""
+    T, D, x_at, w_at, wt, res_at, h, h_at, rstd, r_at = _rms_args(x, weight, residual, hidden, rstd, stream)
+    if out is None:
+        out = _output(stream, x.device, out_dtype or x.dtype, *x.shape)
+    y_at = _like(out, "out", x, _ELEM)
+    _here(out=out)
+    _check(lib().zq_rms_norm(x_at, res_at, _TORCH_DT[x.dtype], w_at, wt, T, D, eps, h_at, y_at, _TORCH_DT[out.dtype],
+                             r_at, _stream(stream)), "rms_norm")
+    return out, h, rstd
+
+
+def qwz_rms_norm(x, weight, residual=None, eps=1e-6, block=256, codes=None, scales=None, hidden=None, rstd=None,
+                 stream=None):
+    """rms_norm with its output in the INT8 format: (codes, scales, h, rstd), codes int8 of
+    x's shape and scales [numel / block], what qwz_quantize gives for the unrounded y.  D
+    must be a multiple of block."""
+    T, D, x_at, w_at, wt, res_at, h, h_at, rstd, r_at = _rms_args(x, weight, residual, hidden, rstd, stream)
+    if codes is None:
+        codes = _output(stream, x.device, torch.int8, *x.shape)
+    if scales is None:
+        scales = _output(stream, x.device, torch.float32, _alloc_nsc(T * D, block))
+    c_at = _ptr(codes, "codes", T * D, _I8)
+    s_at = _ptr(scales, "scales", _nsc(T * D, block), _F32)
+    c_at, s_at = c_at or _dev(codes, "codes"), s_at or _dev(scales, "scales")
+    _here(codes=codes, scales=scales)
+    _check(lib().qwz_rms_norm(x_at, res_at, _TORCH_DT[x.dtype], w_at, wt, T, D, eps, h_at, c_at, s_at, block, r_at,
+                              _stream(stream)), "qwz_rms_norm")
+    return codes, scales, h, rstd
+
+
+def rms_norm_grad_bytes(T, D):
+    """Bytes of workspace rms_norm_grad takes for T rows of D elements."""
+    n = lib().zq_rms_norm_grad_bytes(T, D)
+    if n < 0:
+        raise ValueError(f"rms_norm_grad does not take T={T}, D={D}")
+    return n
+
+
+def rms_norm_grad(dy, h, weight, rstd, dh=None, out=None, dweight=None, accumulate=False, workspace=None, stream=None):
+    """Gradient of rms_norm: (dx, dweight).  dy is the gradient of y [..., D], h and rstd
+    what rms_norm returned, dh (of h's type, or None) the gradient that reaches h by
+    itself.  dx [..., D] of h's type is the gradient of x and of the residual; out may be
+    dh.  dweight [D] is float32 if not given; with accumulate it is added to the given
+    one.  Sums are binary32 in a fixed order.  workspace: uint8, rms_norm_grad_bytes(rows,
+    D) or more; allocated if not given."""
+    T, D = _rows(h, "h")
+    h_at = _ptr(h, "h", T * D, _ELEM)
+    dy_at = _like(dy, "dy", h, _ELEM)
+    w_at, wt = _weight(weight, D)
+    r_at = _ptr(rstd, "rstd", T, _F32)
+    dh_at = _like(dh, "dh", h, (h.dtype,))
+    if out is None:
+        out = _output(stream, h.device, h.dtype, *h.shape)
+    out_at = _like(out, "out", h, (h.dtype,))
+    if dweight is None:
+        if accumulate:
+            raise ValueError("accumulate adds to dweight: give it")
+        dweight = _output(stream, h.device, torch.float32, D)
+    dw_at = _ptr(dweight, "dweight", D, _ELEM)
+    if dweight.numel() != D:
+        raise ValueError(f"dweight holds {dweight.numel()} elements; rows have {D}")
+    h_at, r_at, dw_at = h_at or _dev(h, "h"), r_at or _dev(rstd, "rstd"), dw_at or _dev(dweight, "dweight")
+    _here(h=h, dy=dy, weight=weight, rstd=rstd, dh=dh, out=out, dweight=dweight, workspace=workspace)
+    ws_at, ws_size = _given_workspace(workspace, rms_norm_grad_bytes(T, D), h.device, stream)
+    _check(lib().zq_rms_norm_grad(dy_at, _TORCH_DT[dy.dtype], h_at, _TORCH_DT[h.dtype], w_at, wt, r_at, dh_at, T, D,
+                                  out_at, int(bool(accumulate)), dw_at, _TORCH_DT[dweight.dtype], ws_at, ws_size,
+                                  _stream(stream)), "rms_norm_grad")
+    return out, dweight
+
+
+def _logits(t, name, dtypes, rows=None):
+    """(address, rows, V, distance of rows) of logits [..., V]: contiguous, or of two
+    dimensions with rows further apart (a padded head's logits[:, :V])."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}; expected one of {[str(d) for d in dtypes]}")
+    T, V = _rows(t, name)
+    if rows is not None and T != rows:
+        raise ValueError(f"{name} has {T} rows; expected {rows}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a GPU tensor")
+    if t.is_contiguous():
+        return t.data_ptr(), T, V, V
+    if t.dim() != 2 or (V > 1 and t.stride(1) != 1) or t.stride(0) < V:
+        raise ValueError(f"{name} must be contiguous, or rows of contiguous elements")
+    return t.data_ptr(), T, V, t.stride(0)
+
+
+def _per_row(t, name, T):
+    if t is None:
+        return None
+    at = _ptr(t, name, T, _F32)
+    if t.numel() != T:
+        raise ValueError(f"{name} holds {t.numel()} elements; {T} needed")
+    return at or _dev(t, name)
+
+
+def _token_ids(ids, T):
+    at = _ptr(ids, "ids", T, _IDS)
+    if ids.numel() != T:
+        raise ValueError(f"{ids.numel()} ids for {T} rows of logits")
+    return at or _dev(ids, "ids")
+
+
+def token_logp(logits, ids, scale=1.0, out=None, stream=None):
+    """Log-probability of one token a row: log_softmax(scale * logits)[..., ids], float32 of
+    ids' shape.  logits f32 / f16 / bf16 [..., V], contiguous or a padded head's
+    logits[:, :V]; ids int32 or int64, one a row; scale is 1 / temperature.  An id outside
+    [0, V) gives 0."""
+    l_at, T, V, ld = _logits(logits, "logits", _ELEM)
+    ids_at = _token_ids(ids, T)
+    if out is None:
+        out = _output(stream, logits.device, torch.float32, *ids.shape)
+    out_at = _per_row(out, "out", T)
+    _here(logits=logits, ids=ids, out=out)
+    _check(lib().zq_token_logp(l_at, _TORCH_DT[logits.dtype], T, V, ld, ids_at, _ID_DT[ids.dtype], scale, out_at,
+                               _stream(stream)), "token_logp")
+    return out
+
+
+def policy_loss_bytes(T):
+    """Bytes of workspace policy_loss takes for T rows of logits."""
+    n = lib().zq_policy_loss_bytes(T)
+    if n < 0:
+        raise ValueError(f"policy_loss does not take T={T}")
+    return n
+
+
+def policy_loss(logits, ids, old_logp, advantages, weights=None, ref_logp=None, clip=(0.2, 0.2), kl=0.0, scale=1.0,
+                grad_scale=1.0, grad=True, grad_dtype=None, logp=None, workspace=None, stream=None):
+    """The clipped policy loss with a KL term from logits [..., V], and the logits' gradient:
+    (sums, logp, grad).  With logp = token_logp(logits, ids, scale), r = exp(logp -
+    old_logp) and u = ref_logp - logp the loss of a token is -min(r * A, clip(r, 1 -
+    clip[0], 1 + clip[1]) * A) + kl * (exp(u) - u - 1), A its advantage; sums (float32,
+    4) holds the sums over tokens, by weight, of the loss, its first term, the KL, and of
+    the tokens whose ratio is clipped.
+    ids as token_logp takes them (outside [0, V): no loss, a gradient of zeros);
+    old_logp, advantages, weights (None: 1 each; 0: masked), ref_logp (needed for kl)
+    float32, one a row; scale > 0 is 1 / temperature.
+    grad: True (a tensor of logits' shape and of grad_dtype, logits' if not given), a
+    tensor to write to (of logits' shape; logits itself for in place), or False (None is
+    returned); times grad_scale.  workspace: uint8, policy_loss_bytes(rows) or more;
+    allocated if not given."""
+    l_at, T, V, ld = _logits(logits, "logits", _ELEM)
+    ids_at = _token_ids(ids, T)
+    p = _Policy(_per_row(old_logp, "old_logp", T), _per_row(advantages, "advantages", T),
+                _per_row(weights, "weights", T), _per_row(ref_logp, "ref_logp", T), clip[0], clip[1], kl, scale,
+                grad_scale, 0)
+    g_at, gt, ldg = None, ZQ_F32, V
+    if grad is True:
+        grad = _output(stream, logits.device, grad_dtype or logits.dtype, *logits.shape)
+    if grad is False or grad is None:
+        grad = None
+    else:
+        g_at, _, gV, ldg = _logits(grad, "grad", _ELEM, T)
+        if gV != V:
+            raise ValueError(f"grad has rows of {gV}; logits of {V}")
+        gt = _TORCH_DT[grad.dtype]
+    sums = _output(stream, logits.device, torch.float32, 4)
+    if logp is None:
+        logp = _output(stream, logits.device, torch.float32, *ids.shape)
+    logp_at = _per_row(logp, "logp", T)
+    _here(logits=logits, ids=ids, old_logp=old_logp, advantages=advantages, weights=weights, ref_logp=ref_logp,
+          grad=grad, logp=logp, workspace=workspace)
+    ws_at, ws_size = _given_workspace(workspace, policy_loss_bytes(T), logits.device, stream)
+    _check(lib().zq_policy_loss(l_at, _TORCH_DT[logits.dtype], T, V, ld, ids_at, _ID_DT[ids.dtype], ctypes.byref(p),
+                                _dev(sums, "sums"), logp_at, g_at, gt, ldg, ws_at, ws_size,
+                                _stream(stream)), "policy_loss")
+    return sums, logp, grad

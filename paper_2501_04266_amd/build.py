@@ -18,7 +18,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libzq.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("zq_kernels.hip", "zq_gemm.hip", "zq_embed.hip", "zq_norm.hip",
-                                             "zq_int4_gemm.hip", "zq_api.hip")]
+                                             "zq_int4_gemm.hip", "zq_adamw.hip", "zq_rms.hip",
+                                             "zq_loss.hip", "zq_api.hip")]
 PROBE_LIB = os.path.join(PKG, "libzq_probe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "zq_probe.hip")]
 

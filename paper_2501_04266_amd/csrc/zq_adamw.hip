@@ -1,0 +1,584 @@
+// zq_adamw.hip -- one AdamW step over many tensors, on gfx950.
+//
+//   g = fl(grad * c)      m = fl(fl(b1 m) + fl(om1 g))      v = fl(fl(b2 v) + fl(om2 fl(g g)))
+//   p = cvt(fl(fl(p decay) - fl(alpha fl(m / fl(fl(sqrt(v) root) + eps)))))
+//
+// with c the clipping factor from a norm on the device, and the step's numbers alpha,
+// decay, root computed in binary64.  Gradients are dense or INT4 shards (read as they
+// are), moments binary32 or 8-bit floats with a scale a block, and the new weight can go
+// out a second time in 16 bits or as INT8 codes and scales.
+//
+// Bound by memory: with binary32 weights and moments, bf16 gradients and a bf16 copy an
+// element moves 28 bytes, with INT4 gradients, 8-bit moments and an INT8 copy 13.7.  One
+// pass: the moments' scales and the INT8 copy's need the largest value of a block that is
+// only known after the update, so a wave holds whole blocks (1,024 elements, the largest
+// block) in registers, updates them, and takes the blocks' maxima across its lanes.
+//
+// One launch covers all tensors, a workgroup a piece of 4,096 elements; a map in the
+// table says which tensor a piece belongs to.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <cmath>
+
+#include "zq.h"
+#include "zq_device.h"
+#include "zq_host.h"
+#include "zq_vec.h"
+
+#pragma clang fp contract(off)
+
+namespace zq {
+namespace {
+
+constexpr int kAdamThreads = 256;
+constexpr int kPiece = 4096;             // elements of a workgroup
+constexpr int kWaveElems = 1024;         // of a wave: whole blocks of any size
+constexpr int kSteps = kWaveElems / 256; // 4 elements a lane and step
+constexpr int kInt4 = 3, kInt8 = 4;      // type codes beside ZQ_F32 / ZQ_F16 / ZQ_BF16
+constexpr int kNone = -1;
+
+// One tensor of the table.
+struct Entry {
+  char* p;
+  const char* g;
+  const float* gs;
+  char* m;
+  float* ms;
+  char* v;
+  float* vs;
+  char* out;
+  float* outs;
+  int64_t n;
+  int64_t piece0;  // pieces of the tensors before it
+  double decay, lr_scale;
+  int8_t pt, gt, ot, state8;
+  int8_t lgG, lgS, lgO, pad;
+};
+static_assert(sizeof(Entry) == 112, "table layout");
+
+// The step's numbers.
+struct Coef {
+  double lr, bias1;  // bias1 = 1 - b1^t
+  float b1, om1, b2, om2, root, eps, max_norm, scale;
+  uint32_t key, pad;
+};
+static_assert(sizeof(Coef) == 56, "table layout");
+
+// Table: the numbers of a step whose count or rate is on the device, the entries, the
+// entry of each piece.
+constexpr int64_t kEntriesAt = 64;
+__host__ __device__ inline int64_t map_at(int entries) { return kEntriesAt + (int64_t)entries * (int64_t)sizeof(Entry); }
+
+// ---------------------------------------------------------------- numbers of a step
+
+// 32 bits to 32 that look drawn: every bit of x reaches every bit of the result (two
+// multiplications by odd numbers, shifted halves folded in between).
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0x6A09E667u;
+  x ^= x >> 15;
+  x *= 0x3B67AE85u;
+  return x ^ (x >> 16);
+}
+
+__host__ __device__ inline Coef coef_of(const zq_adamw_args& a, int64_t step, double lr) {
+  Coef c = {};
+  if (step < 1) step = 1;
+  c.lr = lr;
+  c.bias1 = 1.0 - pow(a.beta1, (double)step);
+  c.b1 = (float)a.beta1;
+  c.om1 = (float)(1.0 - a.beta1);
+  c.b2 = (float)a.beta2;
+  c.om2 = (float)(1.0 - a.beta2);
+  c.root = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)step)));
+  c.eps = (float)a.eps;
+  c.max_norm = a.max_norm;
+  c.scale = a.scale;
+  c.key = mix((uint32_t)step);
+  return c;
+}
+
+__global__ void k_adamw_numbers(char* __restrict__ table, zq_adamw_args a, const int64_t* __restrict__ step,
+                                const float* __restrict__ lr) {
+  if (threadIdx.x == 0) *reinterpret_cast<Coef*>(table) = coef_of(a, step ? *step : a.step, lr ? (double)*lr : a.lr);
+}
+
+// ---------------------------------------------------------------- 8-bit floats and blocks
+
+// e4m3 with a sign (bias 7) or e5m2 without (bias 15): a code's bits are the top of a
+// binary32 number's exponent and mantissa, times a power of two.
+template <bool SIGNED>
+struct F8 {
+  static constexpr int shift = SIGNED ? 20 : 21;
+  static constexpr float top = SIGNED ? 448.0f : 57344.0f;
+  static constexpr float unit = SIGNED ? 0x1p-120f : 0x1p-112f;  // code = bits(value * unit) >> shift
+  static constexpr float back = SIGNED ? 0x1p120f : 0x1p112f;
+  static constexpr uint32_t last = SIGNED ? 126u : 123u;         // the code of top
+  static __device__ __forceinline__ float value(uint32_t code) {
+    const uint32_t mag = (code & 0x7fu) << shift;
+    return u2f(SIGNED ? mag | (code & 0x80u) << 24 : mag) * back;
+  }
+  // drawn: 16 random bits
+  static __device__ __forceinline__ uint32_t code(float x, float r, uint32_t drawn) {
+    const float y = (fabsf(x) * r) * unit;
+    uint32_t c = (f2u(y) + (drawn << (shift - 16)) + (1u << (shift - 17))) >> shift;
+    c = c < last ? c : last;
+    return SIGNED && x < 0.0f ? c | 0x80u : c;
+  }
+};
+
+// The largest of `v` (bits of non-negative numbers, which order as they do) over each
+// group of `lanes` lanes, 1 to 64, the same in all lanes of the wave.
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes) {
+  if (lanes >= 2) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));    // quad_perm 1,0,3,2
+  if (lanes >= 4) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));    // quad_perm 2,3,0,1
+  if (lanes >= 8) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));   // row_half_mirror
+  if (lanes >= 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, false));  // row_mirror
+  if (lanes >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+  if (lanes >= 64) v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+  return v;
+}
+
+// The largest magnitude of each step's block (2^lgB elements, 32 to 1,024).
+__device__ __forceinline__ void block_max(const float (&x)[kSteps][4], int lgB, float (&a)[kSteps]) {
+  uint32_t w[kSteps];
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    uint32_t t = 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) t = max(t, f2u(x[u][k]) & 0x7fffffffu);
+    w[u] = lanes_max(t, lgB < 8 ? 1 << (lgB - 2) : 64);
+  }
+  if (lgB >= 9) {
+#pragma unroll
+    for (int u = 0; u < kSteps; u += 2) w[u] = w[u + 1] = max(w[u], w[u + 1]);
+  }
+  if (lgB >= 10) {
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) w[u] = max(w[0], w[2]);
+  }
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) a[u] = u2f(w[u]);
+}
+
+// ---------------------------------------------------------------- loads and stores of 4 elements
+
+template <int DT, bool FULL>
+__device__ __forceinline__ void load4(const char* base, int64_t i, int64_t n, uint32_t (&w)[4]) {
+  constexpr int S = dt_size<DT>();
+  if (FULL || i + 4 <= n) {
+    uint32_t t[S];
+    load_words_any<true>(base + i * S, t);
+#pragma unroll
+    for (int k = 0; k < S; ++k) w[k] = t[k];
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = 0u;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    if (i + k >= n) continue;
+    if constexpr (S == 4) w[k] = reinterpret_cast<const uint32_t*>(base)[i + k];
+    else w[k / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(base)[i + k] << (16 * (k & 1));
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ void widen4(const uint32_t (&w)[4], float (&x)[4]) {
+  widen<DT>(w, x);
+}
+
+template <int DT, bool FULL>
+__device__ __forceinline__ void store4(char* base, int64_t i, int64_t n, const float (&x)[4]) {
+  if (FULL || i + 4 <= n) {
+    store_elems<DT, 4, true>(base, i, x);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const float t[1] = {x[k]};
+    if (i + k < n) store_elems<DT, 1>(base, i + k, t);
+  }
+}
+
+// 4 bytes at byte i of n
+template <bool FULL>
+__device__ __forceinline__ uint32_t load4b(const char* base, int64_t i, int64_t n) {
+  if (FULL || i + 4 <= n) return *reinterpret_cast<const u32_any*>(base + i);
+  uint32_t w = 0u;
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (i + k < n) w |= (uint32_t)(uint8_t)base[i + k] << (8 * k);
+  return w;
+}
+template <bool FULL>
+__device__ __forceinline__ void store4b(char* base, int64_t i, int64_t n, uint32_t w) {
+  if (FULL || i + 4 <= n) {
+    *reinterpret_cast<u32_any*>(base + i) = w;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (i + k < n) base[i + k] = (char)(w >> (8 * k));
+}
+
+// 4 INT4 codes from element i, a multiple of 4, in the low 16 bits
+template <bool FULL>
+__device__ __forceinline__ uint32_t load_int4(const char* base, int64_t i, int64_t n) {
+  if (FULL || i + 4 <= n) return *reinterpret_cast<const u16_any*>(base + i / 2);
+  uint32_t w = 0u;
+  if (i < n) w = (uint8_t)base[i / 2];
+  if (i + 2 < n) w |= (uint32_t)(uint8_t)base[i / 2 + 1] << 8;
+  // the high half of the last byte of an odd count is no code
+  return n > i && ((n - i) & 1) ? w & ((1u << (4 * (n - i))) - 1u) : w;
+}
+
+// writes x as 8-bit floats and their blocks' scales
+template <bool SIGNED, bool FULL>
+__device__ __forceinline__ void store_state8(const float (&x)[kSteps][4], const uint32_t (&drawn)[kSteps][4], char* codes,
+                                             float* scales, int lgB, int64_t i0, int64_t n) {
+  float a[kSteps];
+  block_max(x, lgB, a);
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int64_t i = i0 + u * 256;
+    const bool fits = a[u] >= 0x1p-110f;
+    const float s = fits ? a[u] / F8<SIGNED>::top : 0.0f, r = fits ? F8<SIGNED>::top / a[u] : 0.0f;
+    uint32_t w = 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      w |= F8<SIGNED>::code(x[u][k], r, SIGNED ? drawn[u][k] & 0xffffu : drawn[u][k] >> 16) << (8 * k);
+    store4b<FULL>(codes, i, n, w);
+    if ((i & ((1 << lgB) - 1)) == 0 && (FULL || i < n)) scales[i >> lgB] = s;
+  }
+}
+
+// writes x as INT8 codes and scales, as the weights' quantiser does
+template <bool FULL>
+__device__ __forceinline__ void store_int8(const float (&x)[kSteps][4], char* codes, float* scales, int lgB, int64_t i0,
+                                           int64_t n) {
+  float a[kSteps];
+  block_max(x, lgB, a);
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int64_t i = i0 + u * 256;
+    const bool fits = a[u] >= 0x1p-119f;
+    const float s = fits ? a[u] / 127.0f : 0.0f, r = fits ? 127.0f / a[u] : 0.0f;
+    uint32_t w = 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w |= ((uint32_t)(int)rintf(x[u][k] * r) & 0xffu) << (8 * k);
+    store4b<FULL>(codes, i, n, w);
+    if ((i & ((1 << lgB) - 1)) == 0 && (FULL || i < n)) scales[i >> lgB] = s;
+  }
+}
+
+// ---------------------------------------------------------------- a wave's 1,024 elements
+
+template <int PT, int GT, bool S8, bool FULL>
+__device__ __forceinline__ void update(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0) {
+  const int64_t n = en.n;
+  // all loads first
+  uint32_t pw[kSteps][4], gw[kSteps][4], mw[kSteps][4], vw[kSteps][4];
+  float gs[kSteps], ms[kSteps], vs[kSteps];
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int64_t i = i0 + u * 256;
+    load4<PT, FULL>(en.p, i, n, pw[u]);
+    if constexpr (GT == kInt4) {
+      gw[u][0] = load_int4<FULL>(en.g, i, n);
+      gs[u] = FULL || i < n ? en.gs[i >> en.lgG] : 0.0f;
+    } else {
+      load4<GT, FULL>(en.g, i, n, gw[u]);
+    }
+    if constexpr (S8) {
+      mw[u][0] = load4b<FULL>(en.m, i, n);
+      vw[u][0] = load4b<FULL>(en.v, i, n);
+      ms[u] = FULL || i < n ? en.ms[i >> en.lgS] : 0.0f;
+      vs[u] = FULL || i < n ? en.vs[i >> en.lgS] : 0.0f;
+    } else {
+      load4<ZQ_F32, FULL>(en.m, i, n, mw[u]);
+      load4<ZQ_F32, FULL>(en.v, i, n, vw[u]);
+    }
+  }
+  const double lr = c.lr * en.lr_scale;
+  const float alpha = (float)(lr / c.bias1), decay = (float)(1.0 - lr * en.decay);
+
+  float p[kSteps][4], m[kSteps][4], v[kSteps][4];
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    float g[4];
+    widen4<PT>(pw[u], p[u]);
+    if constexpr (GT == kInt4) {
+      const float s = gs[u] * clip;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g[k] = (float)((int32_t)(gw[u][0] << (28 - 4 * k)) >> 28) * s;
+    } else {
+      widen4<GT>(gw[u], g);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g[k] = g[k] * clip;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float m0, v0;
+      if constexpr (S8) {
+        m0 = F8<true>::value(mw[u][0] >> (8 * k) & 0xffu) * ms[u];
+        v0 = F8<false>::value(vw[u][0] >> (8 * k) & 0xffu) * vs[u];
+      } else {
+        m0 = u2f(mw[u][k]);
+        v0 = u2f(vw[u][k]);
+      }
+      m[u][k] = m0 * c.b1 + g[k] * c.om1;
+      v[u][k] = v0 * c.b2 + (g[k] * g[k]) * c.om2;
+      const float d = sqrtf(v[u][k]) * c.root + c.eps;
+      p[u][k] = p[u][k] * decay - (m[u][k] / d) * alpha;
+    }
+  }
+
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int64_t i = i0 + u * 256;
+    store4<PT, FULL>(en.p, i, n, p[u]);
+    if constexpr (!S8) {
+      store4<ZQ_F32, FULL>(en.m, i, n, m[u]);
+      store4<ZQ_F32, FULL>(en.v, i, n, v[u]);
+    }
+  }
+  if constexpr (S8) {
+    uint32_t key = mix(c.key + (uint32_t)tensor * 0x9E3779B9u);
+    if ((i0 >> 32) != 0) key = mix(key + (uint32_t)(i0 >> 32));  // the same for a piece
+    uint32_t drawn[kSteps][4];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) drawn[u][k] = mix(key ^ ((uint32_t)i0 + (uint32_t)(u * 256 + k)));
+    }
+    store_state8<true, FULL>(m, drawn, en.m, en.ms, en.lgS, i0, n);
+    store_state8<false, FULL>(v, drawn, en.v, en.vs, en.lgS, i0, n);
+  }
+  if (en.ot == kNone) return;
+  if constexpr (PT != ZQ_F32) {  // the copy is of the weight as stored
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p[u][k] = PT == ZQ_BF16 ? u2f(bf16x2_bits(p[u][k], 0.0f) << 16) : h2f(f2h(p[u][k]));
+    }
+  }
+  if (en.ot == kInt8) {
+    if constexpr (!FULL) {  // what lies behind the end counts in no block
+#pragma unroll
+      for (int u = 0; u < kSteps; ++u) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i0 + u * 256 + k >= n) p[u][k] = 0.0f;
+      }
+    }
+    store_int8<FULL>(p, en.out, en.outs, en.lgO, i0, n);
+    return;
+  }
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int64_t i = i0 + u * 256;
+    if (en.ot == ZQ_BF16) store4<ZQ_BF16, FULL>(en.out, i, n, p[u]);
+    else if (en.ot == ZQ_F16) store4<ZQ_F16, FULL>(en.out, i, n, p[u]);
+    else store4<ZQ_F32, FULL>(en.out, i, n, p[u]);
+  }
+}
+
+template <int PT, int GT, bool S8>
+__device__ __forceinline__ void update_any(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0, bool full) {
+  if (full) update<PT, GT, S8, true>(en, c, clip, tensor, i0);
+  else update<PT, GT, S8, false>(en, c, clip, tensor, i0);
+}
+
+template <int PT, bool S8>
+__device__ __forceinline__ void update_grad(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0, bool full) {
+  switch (en.gt) {
+    case ZQ_F32: update_any<PT, ZQ_F32, S8>(en, c, clip, tensor, i0, full); break;
+    case ZQ_F16: update_any<PT, ZQ_F16, S8>(en, c, clip, tensor, i0, full); break;
+    case ZQ_BF16: update_any<PT, ZQ_BF16, S8>(en, c, clip, tensor, i0, full); break;
+    default: update_any<PT, kInt4, S8>(en, c, clip, tensor, i0, full); break;
+  }
+}
+
+template <bool S8>
+__device__ __forceinline__ void update_param(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0, bool full) {
+  switch (en.pt) {
+    case ZQ_F32: update_grad<ZQ_F32, S8>(en, c, clip, tensor, i0, full); break;
+    case ZQ_F16: update_grad<ZQ_F16, S8>(en, c, clip, tensor, i0, full); break;
+    default: update_grad<ZQ_BF16, S8>(en, c, clip, tensor, i0, full); break;
+  }
+}
+
+__global__ void __launch_bounds__(kAdamThreads)
+    k_adamw(unsigned first, const char* __restrict__ table, int count, Coef given, int from_table,
+            const float* __restrict__ norm) {
+  const int* entry_of = reinterpret_cast<const int*>(table + map_at(count));
+  const unsigned piece = first + blockIdx.x;
+  const int tensor = entry_of[piece];
+  const Entry en = reinterpret_cast<const Entry*>(table + kEntriesAt)[tensor];
+  const Coef c = from_table ? *reinterpret_cast<const Coef*>(table) : given;
+  float clip = c.scale;
+  if (norm) {
+    const float t = *norm;
+    if (!(fabsf(t) <= 0x1.fffffep127f)) return;  // infinite or NaN
+    const float ratio = c.max_norm / (t + 1e-6f);
+    clip = c.scale * (ratio > 1.0f ? 1.0f : ratio);
+  }
+  const int64_t e0 = ((int64_t)piece - en.piece0) * kPiece;
+  const int64_t i0 = e0 + (threadIdx.x >> 6) * kWaveElems + (threadIdx.x & 63) * 4;
+  const bool full = e0 + kPiece <= en.n;
+  if (en.state8) update_param<true>(en, c, clip, tensor, i0, full);
+  else update_param<false>(en, c, clip, tensor, i0, full);
+}
+
+// ---------------------------------------------------------------- table
+
+int64_t pieces_of(int64_t n) { return (n + kPiece - 1) / kPiece; }
+
+int check(const zq_adamw& t) {
+  if (t.n < 0 || t.n > INT64_MAX / 16) return ZQ_E_SIZE;
+  const bool int4 = t.grad_dtype == ZQ_INT4, s8 = t.state_dtype == ZQ_F8, int8 = t.out_dtype == ZQ_INT8;
+  if (!dtype_ok(t.param_dtype) || !(int4 || dtype_ok(t.grad_dtype)) || !(s8 || t.state_dtype == ZQ_F32)) return ZQ_E_DTYPE;
+  if (t.out && !(int8 || dtype_ok(t.out_dtype))) return ZQ_E_DTYPE;
+  if ((int4 && log2_block(t.grad_block) < 0) || (s8 && log2_block(t.state_block) < 0)) return ZQ_E_BLOCK;
+  if (t.out && int8 && log2_block(t.out_block) < 0) return ZQ_E_BLOCK;
+  if (!std::isfinite(t.weight_decay) || !std::isfinite(t.lr_scale)) return ZQ_E_SIZE;
+  if (t.n == 0) return ZQ_OK;
+  if (!t.param || !t.grad || !t.m || !t.v || (int4 && !t.grad_scales) || (s8 && (!t.m_scales || !t.v_scales))) return ZQ_E_NULL;
+  if (t.out && int8 && !t.out_scales) return ZQ_E_NULL;
+  if (!aligned(t.param, elem_bytes(t.param_dtype)) || (!int4 && !aligned(t.grad, elem_bytes(t.grad_dtype)))) return ZQ_E_ALIGN;
+  if (int4 && !aligned(t.grad_scales, 4)) return ZQ_E_ALIGN;
+  if (s8 ? !aligned(t.m_scales, 4) || !aligned(t.v_scales, 4) : !aligned(t.m, 4) || !aligned(t.v, 4)) return ZQ_E_ALIGN;
+  if (t.out && (int8 ? !aligned(t.out_scales, 4) : !aligned(t.out, elem_bytes(t.out_dtype)))) return ZQ_E_ALIGN;
+  return ZQ_OK;
+}
+
+int check_overlaps(const zq_adamw* tensors, int32_t count) {
+  std::vector<Span> spans;
+  spans.reserve(9 * (size_t)count);
+  for (int32_t i = 0; i < count; ++i) {
+    const zq_adamw& t = tensors[i];
+    const int64_t n = t.n;
+    const bool s8 = t.state_dtype == ZQ_F8;
+    put_span(spans, t.param, n * elem_bytes(t.param_dtype), true);
+    if (t.grad_dtype == ZQ_INT4) {
+      put_span(spans, t.grad, (n + 1) / 2, false);
+      put_span(spans, t.grad_scales, 4 * num_scales(n, t.grad_block), false);
+    } else {
+      put_span(spans, t.grad, n * elem_bytes(t.grad_dtype), false);
+    }
+    put_span(spans, t.m, s8 ? n : 4 * n, true);
+    put_span(spans, t.v, s8 ? n : 4 * n, true);
+    if (s8) {
+      put_span(spans, t.m_scales, 4 * num_scales(n, t.state_block), true);
+      put_span(spans, t.v_scales, 4 * num_scales(n, t.state_block), true);
+    }
+    if (t.out && t.out_dtype == ZQ_INT8) {
+      put_span(spans, t.out, n, true);
+      put_span(spans, t.out_scales, 4 * num_scales(n, t.out_block), true);
+    } else if (t.out) {
+      put_span(spans, t.out, n * elem_bytes(t.out_dtype), true);
+    }
+  }
+  return check_spans(spans);
+}
+
+Entry entry_for(const zq_adamw& t) {
+  Entry e = {};
+  const bool int4 = t.grad_dtype == ZQ_INT4, s8 = t.state_dtype == ZQ_F8, int8 = t.out && t.out_dtype == ZQ_INT8;
+  e.p = static_cast<char*>(t.param);
+  e.g = static_cast<const char*>(t.grad);
+  e.gs = t.grad_scales;
+  e.m = static_cast<char*>(t.m);
+  e.ms = t.m_scales;
+  e.v = static_cast<char*>(t.v);
+  e.vs = t.v_scales;
+  e.out = static_cast<char*>(t.out);
+  e.outs = t.out_scales;
+  e.n = t.n;
+  e.decay = t.weight_decay;
+  e.lr_scale = t.lr_scale;
+  e.pt = (int8_t)t.param_dtype;
+  e.gt = (int8_t)(int4 ? kInt4 : t.grad_dtype);
+  e.ot = (int8_t)(!t.out ? kNone : int8 ? kInt8 : t.out_dtype);
+  e.state8 = s8;
+  e.lgG = (int8_t)(int4 ? log2_block(t.grad_block) : 0);
+  e.lgS = (int8_t)(s8 ? log2_block(t.state_block) : 0);
+  e.lgO = (int8_t)(int8 ? log2_block(t.out_block) : 0);
+  return e;
+}
+
+int plan_table(const zq_adamw* tensors, int32_t count, zq_adamw_plan* plan) {
+  if (!plan || (count > 0 && !tensors)) return ZQ_E_NULL;
+  if (count < 0) return ZQ_E_SIZE;
+  zq_adamw_plan p = {};
+  p.count = count;
+  for (int32_t i = 0; i < count; ++i) {
+    const int rc = check(tensors[i]);
+    if (rc != ZQ_OK) return rc;
+    p.pieces += pieces_of(tensors[i].n);
+    if (p.pieces > kMaxGrid) return ZQ_E_SIZE;
+  }
+  const int rc = check_overlaps(tensors, count);
+  if (rc != ZQ_OK) return rc;
+  p.bytes = map_at(count) + 4 * p.pieces;
+  *plan = p;
+  return ZQ_OK;
+}
+
+}  // namespace
+}  // namespace zq
+
+extern "C" {
+
+using namespace zq;
+
+int zq_adamw_plan_make(const zq_adamw* tensors, int32_t count, zq_adamw_plan* plan) {
+  try {
+    return plan_table(tensors, count, plan);
+  } catch (...) {  // more tensors than the host has memory to check for overlaps
+    return ZQ_E_SIZE;
+  }
+}
+
+int zq_adamw_plan_table(const zq_adamw* tensors, const zq_adamw_plan* plan, void* host_table) {
+  if (!plan || !host_table || (plan->count > 0 && !tensors)) return ZQ_E_NULL;
+  char* t = static_cast<char*>(host_table);
+  std::fill(t, t + kEntriesAt, (char)0);
+  Entry* entries = reinterpret_cast<Entry*>(t + kEntriesAt);
+  int* map = reinterpret_cast<int*>(t + map_at(plan->count));
+  int64_t at = 0;
+  for (int32_t i = 0; i < plan->count; ++i) {
+    entries[i] = entry_for(tensors[i]);
+    entries[i].piece0 = at;
+    const int64_t pieces = pieces_of(tensors[i].n);
+    std::fill(map + at, map + at + pieces, i);
+    at += pieces;
+  }
+  return ZQ_OK;
+}
+
+int zq_adamw_step(const zq_adamw_plan* plan, void* table, const zq_adamw_args* args, const int64_t* step,
+                  const float* lr, const float* norm, void* stream) {
+  if (!plan || !table || !args) return ZQ_E_NULL;
+  if (!aligned(table, 16) || (step && !aligned(step, 8)) || (lr && !aligned(lr, 4)) || (norm && !aligned(norm, 4)))
+    return ZQ_E_ALIGN;
+  const auto share = [](double b) { return b >= 0.0 && b < 1.0; };
+  if (!share(args->beta1) || !share(args->beta2) || !(args->eps >= 0.0) || (!step && args->step < 1) ||
+      (!lr && !std::isfinite(args->lr)) || (norm && !(args->max_norm >= 0.0f)))
+    return ZQ_E_SIZE;
+  if (plan->pieces == 0) return ZQ_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Coef c = {};
+  if (step || lr) {
+    const int rc = launch(&k_adamw_numbers, 1u, 64u, st, static_cast<char*>(table), *args, step, lr);
+    if (rc != ZQ_OK) return rc;
+  } else {
+    c = coef_of(*args, args->step, args->lr);
+  }
+  return launch_parts(&k_adamw, plan->pieces, kAdamThreads, st, static_cast<const char*>(table), plan->count, c,
+                      step || lr ? 1 : 0, norm);
+}
+
+}  // extern "C"

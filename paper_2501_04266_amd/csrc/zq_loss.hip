@@ -1,0 +1,382 @@
+// zq_loss.hip -- log-probabilities of given tokens, and the clipped policy loss with its
+// gradient, from rows of logits, on gfx950.
+//
+//   logp = scale (z[a] - m) - log S      m = max z, S = sum exp(scale (z - m))
+//   r = exp(logp - old)   loss = -min(r A, clip(r) A) + kl (exp(u) - u - 1)   u = ref - logp
+//   grad[v] = w scale (dloss/dlogp) ((v == a) - exp(scale (z[v] - m)) / S)
+//
+// Bound by memory: a row of logits is read once, kept in the registers of one workgroup
+// (256 to 1,024 threads, up to 16 vectors of 16 bytes each), and its gradient written
+// once.  exp is v_exp_f32 of a binary32 difference; it is taken twice, for the sum and for
+// the gradient, since a row's exponentials in binary32 would need twice the registers of
+// 16-bit logits.  A thread's sum is binary32 (up to 128 terms), sums over threads and what
+// follows binary64: whether a token is clipped is decided at 1 +- clip, and its logarithm
+// is what the binary32 terms allow.  Rows too long for the registers are read again.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <cmath>
+
+#include "zq.h"
+#include "zq_device.h"
+#include "zq_host.h"
+#include "zq_vec.h"
+
+#pragma clang fp contract(off)
+
+namespace zq {
+namespace {
+
+constexpr int64_t kMaxVocab = 1 << 24;
+constexpr float kInf = __builtin_inff();
+
+struct Loss {
+  const void* logits;
+  const void* ids;
+  int64_t T, V, ld;
+  float scale;
+  int it;
+  float* logp;
+  // the loss's: rows is NULL for log-probabilities alone
+  double* rows;  // [T][4]: the terms of the sums
+  void* grad;
+  int64_t ldg;
+  int gt;
+  const float* old_logp;
+  const float* advantages;
+  const float* weights;
+  const float* ref_logp;
+  float clip_low, clip_high, kl, grad_scale;
+};
+
+template <int DT>
+constexpr int per_vec() { return 16 / dt_size<DT>(); }
+
+// a 16-byte vector of logits from element i of n; -infinity behind the end
+template <int DT>
+__device__ __forceinline__ void load_vec(const char* row, int64_t i, int64_t n, uint32_t (&w)[4]) {
+  constexpr int E = per_vec<DT>();
+  if (i + E <= n) {
+    load_words_any<true>(row + i * dt_size<DT>(), w);
+    return;
+  }
+  constexpr uint32_t none = DT == ZQ_F32 ? 0xff800000u : DT == ZQ_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = none;
+#pragma unroll
+  for (int k = 0; k < E - 1; ++k) {
+    if (i + k >= n) continue;
+    if constexpr (DT == ZQ_F32) {
+      w[k] = reinterpret_cast<const uint32_t*>(row)[i + k];
+    } else {
+      const uint32_t h = reinterpret_cast<const uint16_t*>(row)[i + k];
+      w[k / 2] = k & 1 ? (w[k / 2] & 0xffffu) | h << 16 : (w[k / 2] & 0xffff0000u) | h;
+    }
+  }
+}
+
+template <int GT, int E>
+__device__ __forceinline__ void store_vec(char* row, int64_t i, int64_t n, const float (&v)[E]) {
+  if (i + E <= n) {
+    store_elems<GT, E, true>(row, i, v);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < E; ++k) {
+    const float t[1] = {v[k]};
+    if (i + k < n) store_elems<GT, 1>(row, i + k, t);
+  }
+}
+template <int E>
+__device__ __forceinline__ void store_any(int gt, char* row, int64_t i, int64_t n, const float (&v)[E]) {
+  if (gt == ZQ_F32) store_vec<ZQ_F32>(row, i, n, v);
+  else if (gt == ZQ_BF16) store_vec<ZQ_BF16>(row, i, n, v);
+  else store_vec<ZQ_F16>(row, i, n, v);
+}
+
+template <int R>
+__device__ __forceinline__ float group_max(float v, float* slot) {
+  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float m = slot[0];
+#pragma unroll
+  for (int w = 1; w < R / 64; ++w) m = fmaxf(m, slot[w]);
+  return m;
+}
+template <int R>
+__device__ __forceinline__ double group_sum(double v, double* slot) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = slot[0];
+#pragma unroll
+  for (int w = 1; w < R / 64; ++w) s += slot[w];
+  return s;
+}
+
+// The terms of a token, and the factor of its row of gradients.
+__device__ __forceinline__ double token_terms(const Loss& a, int64_t t, double logp, double* rows) {
+  const double w = a.weights ? (double)a.weights[t] : 1.0;
+  if (w == 0.0) {
+    rows[0] = rows[1] = rows[2] = rows[3] = 0.0;
+    return 0.0;
+  }
+  const double A = a.advantages[t], r = exp(logp - (double)a.old_logp[t]);
+  const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
+  const bool clipped = (A > 0.0 && r > hi) || (A < 0.0 && r < lo);
+  const double pg = -(clipped ? (A > 0.0 ? hi : lo) * A : r * A);
+  double slope = clipped ? 0.0 : -r * A, kl = 0.0;
+  if (a.ref_logp) {
+    const double u = (double)a.ref_logp[t] - logp, e = exp(u);
+    kl = e - u - 1.0;
+    if (a.kl != 0.0f) slope += (double)a.kl * (1.0 - e);
+  }
+  rows[0] = w * (a.kl != 0.0f ? pg + (double)a.kl * kl : pg);
+  rows[1] = w * pg;
+  rows[2] = w * kl;
+  rows[3] = clipped ? w : 0.0;
+  return (double)a.grad_scale * w * (double)a.scale * slope;
+}
+
+// R threads a row, NV vectors each; NV = 0: rows of any length, read again
+template <int LT, int R, int NV>
+__global__ void __launch_bounds__(R) k_loss(unsigned first, Loss a) {
+  constexpr int E = per_vec<LT>();
+  __shared__ float top[R / 64];
+  __shared__ double total[R / 64];
+  __shared__ double factor;
+  const int64_t t = first + blockIdx.x;
+  const int64_t id = a.it == ZQ_I64 ? static_cast<const int64_t*>(a.ids)[t] : static_cast<const int32_t*>(a.ids)[t];
+  const char* row = static_cast<const char*>(a.logits) + t * a.ld * dt_size<LT>();
+  char* grow = a.grad ? static_cast<char*>(a.grad) + t * a.ldg * (a.gt == ZQ_F32 ? 4 : 2) : nullptr;
+  const float k2 = a.scale * 1.44269504088896340736f;  // exp(scale d) = 2^(k2 d)
+  const int64_t step = (int64_t)R * E;
+
+  auto none = [&]() {  // no token: no loss, a gradient of zeros
+    if (threadIdx.x == 0) {
+      if (a.logp) a.logp[t] = 0.0f;
+      if (a.rows) a.rows[4 * t] = a.rows[4 * t + 1] = a.rows[4 * t + 2] = a.rows[4 * t + 3] = 0.0;
+    }
+    if (!grow) return;
+    const float zero[E] = {};
+    for (int64_t i = threadIdx.x * E; i < a.V; i += step) store_any(a.gt, grow, i, a.V, zero);
+  };
+  if (id < 0 || id >= a.V) {
+    none();
+    return;
+  }
+  float za[1];
+  load_elems<LT, 1>(row, id, za);
+
+  uint32_t z[NV > 0 ? NV : 1][4];
+  float m = -kInf;
+  auto max_of = [&](const uint32_t(&w)[4]) {
+    float v[E];
+    widen<LT>(w, v);
+#pragma unroll
+    for (int k = 0; k < E; ++k) m = fmaxf(m, v[k]);
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load_vec<LT>(row, (int64_t)(j * R + threadIdx.x) * E, a.V, z[j]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) max_of(z[j]);
+  } else {
+    for (int64_t i = threadIdx.x * E; i < a.V; i += step) {
+      load_vec<LT>(row, i, a.V, z[0]);
+      max_of(z[0]);
+    }
+  }
+  m = group_max<R>(m, top);
+  if (m == -kInf) {  // no logit above -infinity, or none but NaNs
+    int nan = 0;
+    for (int64_t i = threadIdx.x; i < a.V; i += R) {
+      float v[1];
+      load_elems<LT, 1>(row, i, v);
+      nan |= v[0] != v[0];
+    }
+    if (!__syncthreads_or(nan)) {
+      none();
+      return;
+    }
+  }
+
+  double sum = 0.0;
+  auto sum_of = [&](const uint32_t(&w)[4]) {
+    float v[E], s = 0.0f;
+    widen<LT>(w, v);
+#pragma unroll
+    for (int k = 0; k < E; ++k) s += __builtin_amdgcn_exp2f((v[k] - m) * k2);
+    return s;
+  };
+  if constexpr (NV > 0) {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) s += sum_of(z[j]);
+    sum = (double)s;
+  } else {
+    for (int64_t i = threadIdx.x * E; i < a.V; i += step) {
+      load_vec<LT>(row, i, a.V, z[0]);
+      sum += (double)sum_of(z[0]);
+    }
+  }
+  sum = group_sum<R>(sum, total);
+
+  // one wave's work, the others wait for it if they have a gradient to write
+  if (threadIdx.x < 64) {
+    const double logp = (double)a.scale * ((double)za[0] - (double)m) - log(sum);
+    double rows[4];
+    const double g = a.rows ? token_terms(a, t, logp, rows) : 0.0;
+    if (threadIdx.x == 0) {
+      if (a.logp) a.logp[t] = (float)logp;
+      if (a.rows) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a.rows[4 * t + k] = rows[k];
+      }
+      factor = g;
+    }
+  }
+  if (!grow) return;
+  __syncthreads();
+  const float g = (float)factor, c = (float)(-factor / sum);
+  auto put = [&](const uint32_t(&w)[4], int64_t i) {
+    float v[E];
+    widen<LT>(w, v);
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      v[k] = g == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((v[k] - m) * k2) * c;
+      if (i + k == id) v[k] += g;
+    }
+    store_any(a.gt, grow, i, a.V, v);
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t i = (int64_t)(j * R + threadIdx.x) * E;
+      if (i < a.V) put(z[j], i);
+    }
+  } else {
+    for (int64_t i = threadIdx.x * E; i < a.V; i += step) {
+      load_vec<LT>(row, i, a.V, z[0]);
+      put(z[0], i);
+    }
+  }
+}
+
+// the sums over the rows: each thread its rows in their order, then the threads
+__global__ void __launch_bounds__(1024) k_loss_sums(const double* __restrict__ rows, int64_t T, float* __restrict__ sums) {
+  __shared__ double part[16][4];
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int64_t t = threadIdx.x; t < T; t += 1024) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] += rows[4 * t + k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    for (int o = 32; o; o >>= 1) s[k] += __shfl_xor(s[k], o);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][k] = s[k];
+  }
+  __syncthreads();
+  if (threadIdx.x >= 4) return;
+  double v = 0.0;
+  for (int w = 0; w < 16; ++w) v += part[w][threadIdx.x];
+  sums[threadIdx.x] = (float)v;
+}
+
+// Threads of a row and their vectors, by the row's bytes.
+template <int LT>
+int rows_of(const Loss& a, hipStream_t st) {
+  const int64_t vecs = (a.V + per_vec<LT>() - 1) / per_vec<LT>();
+  if (vecs <= 256 * 2) return launch_parts(&k_loss<LT, 256, 2>, a.T, 256, st, a);
+  if (vecs <= 256 * 4) return launch_parts(&k_loss<LT, 256, 4>, a.T, 256, st, a);
+  if (vecs <= 256 * 8) return launch_parts(&k_loss<LT, 256, 8>, a.T, 256, st, a);
+  if (vecs <= 512 * 8) return launch_parts(&k_loss<LT, 512, 8>, a.T, 512, st, a);
+  if (vecs <= 512 * 12) return launch_parts(&k_loss<LT, 512, 12>, a.T, 512, st, a);
+  if (vecs <= 512 * 16) return launch_parts(&k_loss<LT, 512, 16>, a.T, 512, st, a);
+  if (vecs <= 1024 * 12) return launch_parts(&k_loss<LT, 1024, 12>, a.T, 1024, st, a);
+  if (vecs <= 1024 * 16) return launch_parts(&k_loss<LT, 1024, 16>, a.T, 1024, st, a);
+  return launch_parts(&k_loss<LT, 1024, 0>, a.T, 1024, st, a);
+}
+
+int run(const Loss& a, int lt, hipStream_t st) {
+  return lt == ZQ_F32 ? rows_of<ZQ_F32>(a, st) : lt == ZQ_F16 ? rows_of<ZQ_F16>(a, st) : rows_of<ZQ_BF16>(a, st);
+}
+
+// bytes of T rows of V elements, `ld` apart
+int64_t span(int64_t T, int64_t V, int64_t ld, int64_t e) { return T > 0 ? ((T - 1) * ld + V) * e : 0; }
+
+int check_logits(const void* logits, int lt, int64_t T, int64_t V, int64_t ld, const void* ids, int it, float scale) {
+  if (!dtype_ok(lt) || (it != ZQ_I32 && it != ZQ_I64)) return ZQ_E_DTYPE;
+  if (T < 0 || T > (1 << 30) || V < 1 || V > kMaxVocab || ld < V || ld > ((int64_t)1 << 32)) return ZQ_E_SIZE;
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return ZQ_E_SIZE;
+  if (T == 0) return ZQ_OK;
+  if (!logits || !ids) return ZQ_E_NULL;
+  if (!aligned(logits, elem_bytes(lt)) || !aligned(ids, it == ZQ_I64 ? 8 : 4)) return ZQ_E_ALIGN;
+  return ZQ_OK;
+}
+
+}  // namespace
+}  // namespace zq
+
+extern "C" {
+
+using namespace zq;
+
+int zq_token_logp(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_t ld, const void* ids, zq_dtype it,
+                  float scale, float* logp, void* stream) {
+  const int rc = check_logits(logits, lt, T, V, ld, ids, it, scale);
+  if (rc != ZQ_OK || T == 0) return rc;
+  if (!logp) return ZQ_E_NULL;
+  if (!aligned(logp, 4)) return ZQ_E_ALIGN;
+  if (any_overlap({{logp, 4 * T}}, {{logits, span(T, V, ld, elem_bytes(lt))}, {ids, T * (it == ZQ_I64 ? 8 : 4)}}))
+    return ZQ_E_ALIAS;
+  Loss a = {};
+  a.logits = logits, a.ids = ids, a.T = T, a.V = V, a.ld = ld, a.scale = scale, a.it = it, a.logp = logp;
+  return run(a, lt, static_cast<hipStream_t>(stream));
+}
+
+int64_t zq_policy_loss_bytes(int64_t T) { return T < 0 || T > (1 << 30) ? -1 : 32 * T; }
+
+int zq_policy_loss(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_t ld, const void* ids, zq_dtype it,
+                   const zq_policy* policy, float* sums, float* logp, void* grad, zq_dtype gt, int64_t ldg,
+                   void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!policy) return ZQ_E_NULL;
+  const zq_policy& p = *policy;
+  const int rc = check_logits(logits, lt, T, V, ld, ids, it, p.scale);
+  if (rc != ZQ_OK) return rc;
+  if (grad && !dtype_ok(gt)) return ZQ_E_DTYPE;
+  if (!(p.clip_low >= 0.0f && p.clip_low <= 1.0f) || !(p.clip_high >= 0.0f) || !(p.kl >= 0.0f) ||
+      !std::isfinite(p.clip_high) || !std::isfinite(p.kl) || !std::isfinite(p.grad_scale))
+    return ZQ_E_SIZE;
+  if (grad && (ldg < V || ldg > ((int64_t)1 << 32))) return ZQ_E_SIZE;
+  const int64_t need = zq_policy_loss_bytes(T);
+  if (workspace_bytes < need) return ZQ_E_SIZE;
+  if (!sums || (T > 0 && (!workspace || !p.old_logp || !p.advantages || (p.kl != 0.0f && !p.ref_logp)))) return ZQ_E_NULL;
+  const int64_t ge = grad ? elem_bytes(gt) : 1;
+  if (!aligned(sums, 4) || !aligned(logp, 4) || !aligned(grad, ge) || (T > 0 && !aligned(workspace, 16)) ||
+      !aligned(p.old_logp, 4) || !aligned(p.advantages, 4) || !aligned(p.weights, 4) || !aligned(p.ref_logp, 4))
+    return ZQ_E_ALIGN;
+  const bool in_place = grad && grad == logits && gt == lt && ldg == ld;
+  const Range g = {grad, grad ? span(T, V, ldg, ge) : 0};
+  const Range z = {in_place ? nullptr : logits, in_place ? 0 : span(T, V, ld, elem_bytes(lt))};
+  const Range old = {p.old_logp, 4 * T}, adv = {p.advantages, 4 * T};
+  const Range w = {p.weights, p.weights ? 4 * T : 0}, ref = {p.ref_logp, p.ref_logp ? 4 * T : 0};
+  if (any_overlap({g, {sums, 16}, {logp, logp ? 4 * T : 0}, {need ? workspace : nullptr, need}},
+                  {z, {ids, T * (it == ZQ_I64 ? 8 : 4)}, old, adv, w, ref}))
+    return ZQ_E_ALIAS;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  Loss a = {};
+  a.logits = logits, a.ids = ids, a.T = T, a.V = V, a.ld = ld, a.scale = p.scale, a.it = it, a.logp = logp;
+  a.rows = static_cast<double*>(workspace);
+  a.grad = grad, a.ldg = ldg, a.gt = gt;
+  a.old_logp = p.old_logp, a.advantages = p.advantages, a.weights = p.weights, a.ref_logp = p.ref_logp;
+  a.clip_low = p.clip_low, a.clip_high = p.clip_high, a.kl = p.kl, a.grad_scale = p.grad_scale;
+  if (T > 0) {
+    const int rc2 = run(a, lt, st);
+    if (rc2 != ZQ_OK) return rc2;
+  }
+  return launch(&k_loss_sums, 1u, 1024u, st, static_cast<const double*>(workspace), T, sums);
+}
+
+}  // extern "C"

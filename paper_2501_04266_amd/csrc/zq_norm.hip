@@ -377,37 +377,20 @@ Entry clip_entry(const zq_grad& g) {
 int64_t chunks_of(const Entry& e) { return (e.n + chunk_elems(e.type) - 1) / chunk_elems(e.type); }
 int64_t pieces_of(const Entry& e) { return (e.n + kClipElems - 1) / kClipElems; }
 
-// Outputs must not overlap each other nor another tensor's data: the ranges in
-// the order of their addresses, each output against what starts before its end.
+// Outputs must not overlap each other nor another tensor's data.
 int check_overlaps(const zq_grad* grads, int32_t count) {
-  struct Span {
-    uintptr_t from, to;
-    int tensor;
-    bool out;
-  };
   std::vector<Span> spans;
   spans.reserve(3 * (size_t)count);
-  auto put = [&](const void* p, int64_t bytes, int tensor, bool out) {
-    if (p && bytes > 0) spans.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, tensor, out});
-  };
   for (int32_t i = 0; i < count; ++i) {
     const zq_grad& g = grads[i];
     const Entry n = norm_entry(g), c = clip_entry(g);
     if (g.n == 0) continue;
     const bool in_place = c.out == (g.dtype == ZQ_INT4 && !g.out ? (const char*)g.scales : (const char*)g.data);
-    put(c.out, c.n * elem_bytes(c.out_type), i, true);
-    if (!(in_place && g.dtype != ZQ_INT4)) put(n.data, data_bytes(n.n, n.type), i, false);
-    if (g.dtype == ZQ_INT4 && g.out) put(g.scales, 4 * num_scales(g.n, g.block), i, false);
+    put_span(spans, c.out, c.n * elem_bytes(c.out_type), true);
+    if (!(in_place && g.dtype != ZQ_INT4)) put_span(spans, n.data, data_bytes(n.n, n.type), false);
+    if (g.dtype == ZQ_INT4 && g.out) put_span(spans, g.scales, 4 * num_scales(g.n, g.block), false);
   }
-  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
-  // the furthest end of outputs, and of anything, among the spans before
-  uintptr_t out_to = 0, any_to = 0;
-  for (const Span& s : spans) {
-    if (s.from < out_to || (s.out && s.from < any_to)) return ZQ_E_ALIAS;
-    any_to = std::max(any_to, s.to);
-    if (s.out) out_to = std::max(out_to, s.to);
-  }
-  return ZQ_OK;
+  return check_spans(spans);
 }
 
 int plan_table(const zq_grad* grads, int32_t count, zq_grad_plan* plan) {

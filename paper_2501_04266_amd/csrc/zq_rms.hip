@@ -1,0 +1,519 @@
+// zq_rms.hip -- root-mean-square norm of rows after the residual's addition, its output
+// dense or as INT8 blocks, and its gradient, on gfx950.
+//
+//   h = cvt(fl(x + residual))   rstd = fl(1 / sqrt(sum h^2 / D + eps))   y = fl(fl(h rstd) w)
+//   dx = rstd (dy w - xh sum(dy w xh) / D) + dh      dw = sum over rows of dy xh      xh = fl(h rstd)
+//
+// Bound by memory: a row is read once, held in its threads' registers between the sum and
+// the output, and written once.  Squares and their sum are binary64: the sum's order does
+// not show in rstd except by one rounding, so INT8 codes next to a border do not depend on
+// how a row is cut.
+//
+// A row belongs to a group of 64, 256 or 1,024 threads with up to 4 vectors of 8 elements
+// each, by its length; longer rows are read a second time.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <cmath>
+
+#include "zq.h"
+#include "zq_device.h"
+#include "zq_host.h"
+#include "zq_vec.h"
+
+#pragma clang fp contract(off)
+
+namespace zq {
+namespace {
+
+constexpr int kInt8 = 3;  // y's type code beside ZQ_F32 / ZQ_F16 / ZQ_BF16
+constexpr int64_t kMaxWidth = 1 << 24;
+
+// ---------------------------------------------------------------- rows
+
+// 8 elements from element i of n; zeros behind the end
+template <int DT>
+__device__ __forceinline__ void load8(const void* row, int64_t i, int64_t n, float (&v)[8]) {
+  if (i + 8 <= n) {
+    load_elems<DT, 8, true>(row, i, v);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float t[1] = {0.0f};
+    if (i + k < n) load_elems<DT, 1>(row, i + k, t);
+    v[k] = t[0];
+  }
+}
+__device__ __forceinline__ void load8_any(int dt, const void* row, int64_t i, int64_t n, float (&v)[8]) {
+  if (dt == ZQ_F32) load8<ZQ_F32>(row, i, n, v);
+  else if (dt == ZQ_BF16) load8<ZQ_BF16>(row, i, n, v);
+  else load8<ZQ_F16>(row, i, n, v);
+}
+template <int DT>
+__device__ __forceinline__ void store8(void* row, int64_t i, int64_t n, const float (&v)[8]) {
+  if (i + 8 <= n) {
+    store_elems<DT, 8, true>(row, i, v);
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float t[1] = {v[k]};
+    if (i + k < n) store_elems<DT, 1>(row, i + k, t);
+  }
+}
+__device__ __forceinline__ void store8_any(int dt, void* row, int64_t i, int64_t n, const float (&v)[8]) {
+  if (dt == ZQ_F32) store8<ZQ_F32>(row, i, n, v);
+  else if (dt == ZQ_BF16) store8<ZQ_BF16>(row, i, n, v);
+  else store8<ZQ_F16>(row, i, n, v);
+}
+template <int DT>
+__device__ __forceinline__ float as_stored(float v) {
+  if constexpr (DT == ZQ_BF16) return u2f(bf16x2_bits(v, 0.0f) << 16);
+  else if constexpr (DT == ZQ_F16) return h2f(f2h(v));
+  else return v;
+}
+
+// ---------------------------------------------------------------- sums over a row's threads
+
+template <typename F>
+__device__ __forceinline__ F wave_sum(F v) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+// the sum over a row's R threads, in all of them; `slot`: R / 64 values of LDS, written
+// again only after a barrier
+template <int R, typename F>
+__device__ __forceinline__ F row_sum(F v, F* slot) {
+  v = wave_sum(v);
+  if constexpr (R == 64) return v;
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  __syncthreads();
+  F s = slot[0];
+#pragma unroll
+  for (int w = 1; w < R / 64; ++w) s += slot[w];
+  return s;
+}
+
+// The largest of `v` (bits of non-negative numbers) over each group of `lanes` lanes.
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));                    // quad_perm 1,0,3,2
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));                    // quad_perm 2,3,0,1
+  if (lanes >= 8) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));   // row_half_mirror
+  if (lanes >= 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, false));  // row_mirror
+  if (lanes >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+  if (lanes >= 64) v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+  return v;
+}
+
+// ---------------------------------------------------------------- forward
+
+struct Norm {
+  const void* x;
+  const void* residual;
+  const void* weight;
+  void* h;
+  void* y;
+  float* scales;
+  float* rstd;
+  int64_t T, D;
+  double eps;
+  int8_t wt, yt, lgB;
+};
+
+// 8 values of a row as codes of the INT8 format.  All threads of the row's waves call it;
+// a block of 1,024 is two waves', whose halves meet in `half` (LDS, R / 64 values).
+template <int R>
+__device__ __forceinline__ void put_int8(const Norm& a, int64_t at, int64_t i, const float (&v)[8], uint32_t* half) {
+  uint32_t t = 0u;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) t = max(t, f2u(v[k]) & 0x7fffffffu);
+  t = lanes_max(t, a.lgB < 9 ? 1 << (a.lgB - 3) : 64);
+  if (R > 64 && a.lgB == 10) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) half[threadIdx.x >> 6] = t;
+    __syncthreads();
+    t = max(t, half[(threadIdx.x >> 6) ^ 1]);
+  }
+  const float m = u2f(t);
+  const bool fits = m >= 0x1p-119f;
+  const float s = fits ? m / 127.0f : 0.0f, r = fits ? 127.0f / m : 0.0f;
+  if (i >= a.D) return;
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) w[k / 4] |= ((uint32_t)(int)rintf(v[k] * r) & 0xffu) << (8 * (k & 3));
+  store_words_any<true>(static_cast<char*>(a.y) + at + i, w);
+  if ((i & ((1 << a.lgB) - 1)) == 0) a.scales[(at + i) >> a.lgB] = s;
+}
+
+// NV vectors of 8 elements a thread; NV = 0: rows of any length, h read again
+template <int XT, int R, int NV>
+__global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms(unsigned first, Norm a) {
+  constexpr int THREADS = R < 256 ? 256 : R;
+  __shared__ double slot[R / 64];
+  __shared__ uint32_t half[R / 64];
+  const int lane = threadIdx.x % R;
+  int64_t t = (int64_t)(first + blockIdx.x) * (THREADS / R) + threadIdx.x / R;
+  if (R == 64 && t >= a.T) return;  // a wave's own row: the others go on
+  const int64_t at = t * a.D;       // the row's first element
+  const char* x = static_cast<const char*>(a.x) + at * dt_size<XT>();
+  const char* res = a.residual ? static_cast<const char*>(a.residual) + at * dt_size<XT>() : nullptr;
+  char* h = a.residual ? static_cast<char*>(a.h) + at * dt_size<XT>() : nullptr;
+  char* y = static_cast<char*>(a.y) + at * (a.yt == ZQ_F32 ? 4 : 2);
+
+  double sum = 0.0;
+  auto take = [&](int64_t i, float (&v)[8]) {
+    load8<XT>(x, i, a.D, v);
+    if (res) {
+      float b[8];
+      load8<XT>(res, i, a.D, b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = as_stored<XT>(v[k] + b[k]);
+      store8<XT>(h, i, a.D, v);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
+  };
+  auto put = [&](int64_t i, float (&v)[8], float rstd) {
+    float w[8];
+    if (a.weight) {
+      load8_any(a.wt, a.weight, i, a.D, w);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (v[k] * rstd) * w[k];
+    if (a.yt == kInt8) put_int8<R>(a, at, i, v, half);
+    else store8_any(a.yt, y, i, a.D, v);
+  };
+  auto finish = [&]() {
+    sum = row_sum<R>(sum, slot);
+    const float rstd = (float)(1.0 / sqrt(sum / (double)a.D + a.eps));
+    if (a.rstd && lane == 0) a.rstd[t] = rstd;
+    return rstd;
+  };
+
+  if constexpr (NV > 0) {
+    float v[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) take((int64_t)(j * R + lane) * 8, v[j]);
+    const float rstd = finish();
+#pragma unroll
+    for (int j = 0; j < NV; ++j) put((int64_t)(j * R + lane) * 8, v[j], rstd);
+  } else {
+    const int64_t end = (a.D + 8 * R - 1) / (8 * R) * (8 * R);  // all threads take every turn
+    for (int64_t i = lane * 8; i < end; i += 8 * R) {
+      float v[8];
+      take(i, v);
+    }
+    const float rstd = finish();
+    for (int64_t i = lane * 8; i < end; i += 8 * R) {
+      float v[8];
+      load8<XT>(res ? h : x, i, a.D, v);  // this thread's own writes
+      put(i, v, rstd);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- gradient
+
+struct NormGrad {
+  const void* dy;
+  const void* h;
+  const void* weight;
+  const float* rstd;
+  const void* dh;
+  void* dx;
+  float* part;  // [groups][D] sums of dw, or NULL
+  int64_t T, D;
+  int groups;   // of rows: group g has the rows g, g + groups, ...
+  int8_t gt, wt;
+};
+
+template <int XT, int R, int NV, bool SAME>
+__global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms_grad(NormGrad a) {
+  constexpr int THREADS = R < 256 ? 256 : R;
+  __shared__ float slot[2][R / 64];
+  const int lane = threadIdx.x % R;
+  const int g = blockIdx.x * (THREADS / R) + threadIdx.x / R;
+  if (R == 64 && g >= a.groups) return;  // a wave's own rows
+  float w[NV][8], dw[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int64_t i = (int64_t)(j * R + lane) * 8;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dw[j][k] = 0.0f, w[j][k] = 1.0f;
+    if (a.weight) load8_any(a.wt, a.weight, i, a.D, w[j]);
+  }
+  int turn = 0;
+  for (int64_t t = g; t < a.T; t += a.groups, turn ^= 1) {
+    const int64_t at = t * a.D;
+    const char* hr = static_cast<const char*>(a.h) + at * dt_size<XT>();
+    const char* dyr = static_cast<const char*>(a.dy) + at * (SAME ? dt_size<XT>() : a.gt == ZQ_F32 ? 4 : 2);
+    const float rstd = a.rstd[t];
+    float xh[NV][8], gw[NV][8], c = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t i = (int64_t)(j * R + lane) * 8;
+      load8<XT>(hr, i, a.D, xh[j]);
+      if constexpr (SAME) load8<XT>(dyr, i, a.D, gw[j]);
+      else load8_any(a.gt, dyr, i, a.D, gw[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        xh[j][k] = xh[j][k] * rstd;
+        dw[j][k] += gw[j][k] * xh[j][k];
+        gw[j][k] = gw[j][k] * w[j][k];
+        c += gw[j][k] * xh[j][k];
+      }
+    }
+    c = row_sum<R>(c, slot[turn]) / (float)a.D;
+    const char* dhr = a.dh ? static_cast<const char*>(a.dh) + at * dt_size<XT>() : nullptr;
+    char* dxr = static_cast<char*>(a.dx) + at * dt_size<XT>();
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t i = (int64_t)(j * R + lane) * 8;
+      float d[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      if (dhr) load8<XT>(dhr, i, a.D, d);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) d[k] += (gw[j][k] - xh[j][k] * c) * rstd;
+      store8<XT>(dxr, i, a.D, d);
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) store8<ZQ_F32>(a.part + (int64_t)g * a.D, (int64_t)(j * R + lane) * 8, a.D, dw[j]);
+}
+
+// rows of any length: dx, a row a workgroup, read twice
+template <int XT>
+__global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad a) {
+  __shared__ double slot[16];
+  const int64_t t = first + blockIdx.x, at = t * a.D;
+  const char* hr = static_cast<const char*>(a.h) + at * dt_size<XT>();
+  const char* dyr = static_cast<const char*>(a.dy) + at * (a.gt == ZQ_F32 ? 4 : 2);
+  const char* dhr = a.dh ? static_cast<const char*>(a.dh) + at * dt_size<XT>() : nullptr;
+  char* dxr = static_cast<char*>(a.dx) + at * dt_size<XT>();
+  const float rstd = a.rstd[t];
+  auto take = [&](int64_t i, float (&xh)[8], float (&gw)[8]) {
+    float w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+    load8<XT>(hr, i, a.D, xh);
+    load8_any(a.gt, dyr, i, a.D, gw);
+    if (a.weight) load8_any(a.wt, a.weight, i, a.D, w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) xh[k] = xh[k] * rstd, gw[k] = gw[k] * w[k];
+  };
+  double sum = 0.0;
+  for (int64_t i = threadIdx.x * 8; i < a.D; i += 8192) {
+    float xh[8], gw[8], c = 0.0f;
+    take(i, xh, gw);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) c += gw[k] * xh[k];
+    sum += (double)c;
+  }
+  const float c = (float)(row_sum<1024>(sum, slot) / (double)a.D);
+  for (int64_t i = threadIdx.x * 8; i < a.D; i += 8192) {
+    float xh[8], gw[8], d[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    take(i, xh, gw);
+    if (dhr) load8<XT>(dhr, i, a.D, d);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) d[k] += (gw[k] - xh[k] * c) * rstd;
+    store8<XT>(dxr, i, a.D, d);
+  }
+}
+
+// and their part of dw: 256 x 8 columns of a group of rows a workgroup
+template <int XT>
+__global__ void __launch_bounds__(256) k_rms_grad_columns(unsigned first, NormGrad a, unsigned tiles) {
+  const unsigned b = first + blockIdx.x;
+  const int g = (int)(b / tiles);
+  const int64_t i = ((int64_t)(b % tiles) * 256 + threadIdx.x) * 8;
+  if (i >= a.D) return;
+  float dw[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  for (int64_t t = g; t < a.T; t += a.groups) {
+    const int64_t at = t * a.D;
+    float h[8], dy[8];
+    load8<XT>(static_cast<const char*>(a.h) + at * dt_size<XT>(), i, a.D, h);
+    load8_any(a.gt, static_cast<const char*>(a.dy) + at * (a.gt == ZQ_F32 ? 4 : 2), i, a.D, dy);
+    const float rstd = a.rstd[t];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dw[k] += dy[k] * (h[k] * rstd);
+  }
+  store8<ZQ_F32>(a.part + (int64_t)g * a.D, i, a.D, dw);
+}
+
+// dw from the groups' sums: 64 columns a workgroup, 16 slices of the groups, each in its
+// order, and then the slices in theirs, in binary64
+__global__ void __launch_bounds__(1024)
+    k_rms_grad_join(const float* __restrict__ part, int groups, int64_t D, int accumulate, void* dw, int dwt) {
+  __shared__ double slice[16][64];
+  const int64_t d = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int s = threadIdx.x >> 6;
+  double v = 0.0;
+  if (d < D) {
+    const int g0 = (int)((int64_t)groups * s / 16), g1 = (int)((int64_t)groups * (s + 1) / 16);
+    int g = g0;
+    for (; g + 8 <= g1; g += 8) {
+      float t[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) t[k] = part[(int64_t)(g + k) * D + d];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += (double)t[k];
+    }
+    for (; g < g1; ++g) v += (double)part[(int64_t)g * D + d];
+  }
+  slice[s][threadIdx.x & 63] = v;
+  __syncthreads();
+  if (s != 0 || d >= D) return;
+  for (int k = 1; k < 16; ++k) v += slice[k][threadIdx.x];
+  float t[1] = {(float)v};
+  if (dwt == ZQ_F32) {
+    float o[1];
+    if (accumulate) load_elems<ZQ_F32, 1>(dw, d, o), t[0] = o[0] + t[0];
+    store_elems<ZQ_F32, 1>(dw, d, t);
+  } else if (dwt == ZQ_BF16) {
+    float o[1];
+    if (accumulate) load_elems<ZQ_BF16, 1>(dw, d, o), t[0] = o[0] + t[0];
+    store_elems<ZQ_BF16, 1>(dw, d, t);
+  } else {
+    float o[1];
+    if (accumulate) load_elems<ZQ_F16, 1>(dw, d, o), t[0] = o[0] + t[0];
+    store_elems<ZQ_F16, 1>(dw, d, t);
+  }
+}
+
+// ---------------------------------------------------------------- choice of kernel
+
+// Threads of a row and vectors of each, by the row's length.
+template <int XT>
+int forward(const Norm& a, hipStream_t st) {
+  const int64_t waves = (a.T + 3) / 4;
+  if (a.D <= 512) return launch_parts(&k_rms<XT, 64, 1>, waves, 256, st, a);
+  if (a.D <= 2048) return launch_parts(&k_rms<XT, 256, 1>, a.T, 256, st, a);
+  if (a.D <= 4096) return launch_parts(&k_rms<XT, 256, 2>, a.T, 256, st, a);
+  if (a.D <= 6144) return launch_parts(&k_rms<XT, 256, 3>, a.T, 256, st, a);
+  if (a.D <= 8192) return launch_parts(&k_rms<XT, 256, 4>, a.T, 256, st, a);
+  if (a.D <= 16384) return launch_parts(&k_rms<XT, 1024, 2>, a.T, 1024, st, a);
+  return launch_parts(&k_rms<XT, 1024, 0>, a.T, 1024, st, a);
+}
+
+int check_forward(const Norm& a, int xt, const void* weight, int wt, bool int8, int yt, int32_t block) {
+  if (!dtype_ok(xt) || (weight && !dtype_ok(wt)) || (!int8 && !dtype_ok(yt))) return ZQ_E_DTYPE;
+  if (int8 && log2_block(block) < 0) return ZQ_E_BLOCK;
+  if (a.T < 0 || a.D < 1 || a.D > kMaxWidth || a.T > kMaxGrid || !(a.eps >= 0.0)) return ZQ_E_SIZE;
+  if (int8 && a.D % block) return ZQ_E_SIZE;
+  if (a.T == 0) return ZQ_OK;
+  if (!a.x || !a.y || (a.residual && !a.h) || (int8 && !a.scales)) return ZQ_E_NULL;
+  const int64_t e = elem_bytes(xt), n = a.T * a.D;
+  if (!aligned(a.x, e) || !aligned(a.residual, e) || !aligned(a.h, e) || (weight && !aligned(weight, elem_bytes(wt))) ||
+      (!int8 && !aligned(a.y, elem_bytes(yt))) || !aligned(a.scales, 4) || !aligned(a.rstd, 4))
+    return ZQ_E_ALIGN;
+  const Range x = {a.x, n * e}, res = {a.residual, a.residual ? n * e : 0};
+  const Range w = {weight, weight ? a.D * elem_bytes(wt) : 0};
+  const Range y = {a.y, int8 ? n : n * elem_bytes(yt)}, sc = {a.scales, int8 ? 4 * (n / block) : 0};
+  const Range rs = {a.rstd, a.rstd ? 4 * a.T : 0}, h = {a.h, a.residual ? n * e : 0};
+  if (any_overlap({y, sc, rs}, {x, res, w, h})) return ZQ_E_ALIAS;
+  // h in the place of x or of residual, or apart from both
+  if (a.residual && (overlap(h, w) || (a.h != a.x && overlap(h, x)) || (a.h != a.residual && overlap(h, res))))
+    return ZQ_E_ALIAS;
+  return ZQ_OK;
+}
+
+int rms_norm(const void* x, const void* residual, int xt, const void* weight, int wt, int64_t T, int64_t D, double eps,
+             void* h, void* y, int yt, float* scales, int32_t block, float* rstd, void* stream, bool int8) {
+  const Norm a = {x, residual, weight, h, y, scales, rstd, T, D, eps, (int8_t)wt, (int8_t)(int8 ? kInt8 : yt),
+                  (int8_t)(int8 ? log2_block(block) : 0)};
+  const int rc = check_forward(a, xt, weight, wt, int8, yt, block);
+  if (rc != ZQ_OK || T == 0) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return xt == ZQ_F32 ? forward<ZQ_F32>(a, st) : xt == ZQ_F16 ? forward<ZQ_F16>(a, st) : forward<ZQ_BF16>(a, st);
+}
+
+// Rows are dealt to groups whose sums of dw (4 D bytes each) are joined: as many as fill
+// the chip with the threads of a row, as far as the sums stay within 16 MB.
+int row_threads(int64_t D) { return D <= 512 ? 64 : D <= 8192 ? 256 : 1024; }
+int64_t groups_for(int64_t T, int64_t D) {
+  int64_t g = (1 << 22) / D;
+  const int64_t most = 512 * 256 / row_threads(D);
+  g = g < 1 ? 1 : g > most ? most : g;
+  return g < T ? g : T < 1 ? 1 : T;
+}
+
+template <int XT, bool SAME>
+int backward_short(const NormGrad& a, hipStream_t st) {
+  const unsigned g = (unsigned)a.groups;
+  if (a.D <= 512) return launch(&k_rms_grad<XT, 64, 1, SAME>, (g + 3) / 4, 256u, st, a);
+  if (a.D <= 2048) return launch(&k_rms_grad<XT, 256, 1, SAME>, g, 256u, st, a);
+  if (a.D <= 4096) return launch(&k_rms_grad<XT, 256, 2, SAME>, g, 256u, st, a);
+  if (a.D <= 6144) return launch(&k_rms_grad<XT, 256, 3, SAME>, g, 256u, st, a);
+  if (a.D <= 8192) return launch(&k_rms_grad<XT, 256, 4, SAME>, g, 256u, st, a);
+  return launch(&k_rms_grad<XT, 1024, 2, SAME>, g, 1024u, st, a);
+}
+
+template <int XT>
+int backward(const NormGrad& a, hipStream_t st) {
+  if (a.D <= 16384) return a.gt == XT ? backward_short<XT, true>(a, st) : backward_short<XT, false>(a, st);
+  int rc = launch_parts(&k_rms_grad_long<XT>, a.T, 1024, st, a);
+  if (rc != ZQ_OK || !a.part) return rc;
+  const unsigned tiles = (unsigned)((a.D + 2047) / 2048);
+  return launch_parts(&k_rms_grad_columns<XT>, (int64_t)tiles * a.groups, 256, st, a, tiles);
+}
+
+bool grad_sizes_ok(int64_t T, int64_t D) { return T >= 0 && T <= kMaxGrid && D >= 1 && D <= kMaxWidth; }
+
+}  // namespace
+}  // namespace zq
+
+extern "C" {
+
+using namespace zq;
+
+int zq_rms_norm(const void* x, const void* residual, zq_dtype xt, const void* weight, zq_dtype wt, int64_t T,
+                int64_t D, double eps, void* h, void* y, zq_dtype yt, float* rstd, void* stream) {
+  return rms_norm(x, residual, xt, weight, wt, T, D, eps, h, y, yt, nullptr, 0, rstd, stream, false);
+}
+
+int qwz_rms_norm(const void* x, const void* residual, zq_dtype xt, const void* weight, zq_dtype wt, int64_t T,
+                 int64_t D, double eps, void* h, int8_t* codes, float* scales, int32_t block, float* rstd,
+                 void* stream) {
+  return rms_norm(x, residual, xt, weight, wt, T, D, eps, h, codes, 0, scales, block, rstd, stream, true);
+}
+
+int64_t zq_rms_norm_grad_bytes(int64_t T, int64_t D) {
+  return grad_sizes_ok(T, D) ? 4 * groups_for(T, D) * D : -1;
+}
+
+int zq_rms_norm_grad(const void* dy, zq_dtype gt, const void* h, zq_dtype xt, const void* weight, zq_dtype wt,
+                     const float* rstd, const void* dh, int64_t T, int64_t D, void* dx, int accumulate, void* dw,
+                     zq_dtype dwt, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!dtype_ok(gt) || !dtype_ok(xt) || (weight && !dtype_ok(wt)) || (dw && !dtype_ok(dwt))) return ZQ_E_DTYPE;
+  if (!grad_sizes_ok(T, D)) return ZQ_E_SIZE;
+  const int64_t need = dw ? zq_rms_norm_grad_bytes(T, D) : 0;
+  if (workspace_bytes < need) return ZQ_E_SIZE;
+  if (T == 0 && (!dw || accumulate)) return ZQ_OK;
+  if ((need && !workspace) || (T > 0 && (!dy || !h || !rstd || !dx))) return ZQ_E_NULL;
+  const int64_t e = elem_bytes(xt), n = T * D;
+  if (!aligned(dy, elem_bytes(gt)) || !aligned(h, e) || (weight && !aligned(weight, elem_bytes(wt))) ||
+      !aligned(rstd, 4) || !aligned(dh, e) || !aligned(dx, e) || (dw && !aligned(dw, elem_bytes(dwt))) ||
+      (need && !aligned(workspace, 16)))
+    return ZQ_E_ALIGN;
+  const Range rdy = {dy, n * elem_bytes(gt)}, rh = {h, n * e}, rw = {weight, weight ? D * elem_bytes(wt) : 0};
+  const Range rr = {rstd, 4 * T}, rdh = {dh, dh && dh != dx ? n * e : 0}, rdx = {dx, n * e};
+  const Range rdw = {dw, dw ? D * elem_bytes(dwt) : 0}, ws = {need ? workspace : nullptr, need};
+  if (any_overlap({rdx, rdw, ws}, {rdy, rh, rw, rr, rdh})) return ZQ_E_ALIAS;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const NormGrad a = {dy, h, weight, rstd, dh, dx, dw ? static_cast<float*>(workspace) : nullptr, T, D,
+                      (int)groups_for(T, D), (int8_t)gt, (int8_t)wt};
+  if (T > 0) {
+    const int rc = xt == ZQ_F32 ? backward<ZQ_F32>(a, st) : xt == ZQ_F16 ? backward<ZQ_F16>(a, st) : backward<ZQ_BF16>(a, st);
+    if (rc != ZQ_OK) return rc;
+  }
+  if (!dw) return ZQ_OK;
+  return launch(&k_rms_grad_join, (unsigned)((D + 63) / 64), 1024u, st, static_cast<const float*>(workspace),
+                T > 0 ? a.groups : 0, D, accumulate, dw, (int)dwt);
+}
+
+}  // extern "C"
