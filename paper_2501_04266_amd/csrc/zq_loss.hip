@@ -16,6 +16,7 @@
 #include <stdint.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "zq.h"
 #include "zq_device.h"
@@ -54,10 +55,10 @@ constexpr int per_vec() { return 16 / dt_size<DT>(); }
 
 // a 16-byte vector of logits from element i of n; -infinity behind the end
 template <int DT>
-__device__ __forceinline__ void load_vec(const char* row, int64_t i, int64_t n, uint32_t (&w)[4]) {
+__device__ __forceinline__ void load_vec(const char* row, int i, int n, uint32_t (&w)[4]) {
   constexpr int E = per_vec<DT>();
   if (i + E <= n) {
-    load_words_any<true>(row + i * dt_size<DT>(), w);
+    load_words_any<true>(row + (uint32_t)i * dt_size<DT>(), w);
     return;
   }
   constexpr uint32_t none = DT == ZQ_F32 ? 0xff800000u : DT == ZQ_BF16 ? 0xff80ff80u : 0xfc00fc00u;
@@ -75,10 +76,17 @@ __device__ __forceinline__ void load_vec(const char* row, int64_t i, int64_t n, 
   }
 }
 
+// The words are what they were, but the compiler does not know: what it has derived from
+// them (their widened values) is not kept in registers across this point.
+__device__ __forceinline__ void forget(uint32_t (&w)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) asm volatile("" : "+v"(w[k]));
+}
+
 template <int GT, int E>
-__device__ __forceinline__ void store_vec(char* row, int64_t i, int64_t n, const float (&v)[E]) {
+__device__ __forceinline__ void store_vec(char* row, int i, int n, const float (&v)[E]) {
   if (i + E <= n) {
-    store_elems<GT, E, true>(row, i, v);
+    store_elems<GT, E, true>(row + (uint32_t)i * dt_size<GT>(), 0, v);
     return;
   }
 #pragma unroll
@@ -87,11 +95,12 @@ __device__ __forceinline__ void store_vec(char* row, int64_t i, int64_t n, const
     if (i + k < n) store_elems<GT, 1>(row, i + k, t);
   }
 }
-template <int E>
-__device__ __forceinline__ void store_any(int gt, char* row, int64_t i, int64_t n, const float (&v)[E]) {
-  if (gt == ZQ_F32) store_vec<ZQ_F32>(row, i, n, v);
-  else if (gt == ZQ_BF16) store_vec<ZQ_BF16>(row, i, n, v);
-  else store_vec<ZQ_F16>(row, i, n, v);
+// f<type>() for the type that dt names
+template <typename F>
+__device__ __forceinline__ void for_type(int dt, F f) {
+  if (dt == ZQ_F32) f(std::integral_constant<int, ZQ_F32>());
+  else if (dt == ZQ_BF16) f(std::integral_constant<int, ZQ_BF16>());
+  else f(std::integral_constant<int, ZQ_F16>());
 }
 
 template <int R>
@@ -115,6 +124,33 @@ __device__ __forceinline__ double group_sum(double v, double* slot) {
   return s;
 }
 
+// exp and log of a token's few binary64 numbers, as loops over their series with the
+// coefficients in scalar registers: they run while a row waits in the vector registers,
+// and the library's functions take some 40 of those.  Errors below 2^-48 relative.
+__device__ const double kInverse[14] = {1.0, 1.0,       1.0 / 2,  1.0 / 3,  1.0 / 4,  1.0 / 5,  1.0 / 6,
+                                        1.0 / 7, 1.0 / 8, 1.0 / 9, 1.0 / 10, 1.0 / 11, 1.0 / 12, 1.0 / 13};
+__device__ __forceinline__ double exp64(double x) {
+  if (!(fabs(x) <= 700.0)) return x > 0.0 ? (double)kInf : x < 0.0 ? 0.0 : x;
+  // x = k log 2 + r, |r| <= 0.35: the series to r^13 / 13!
+  const double k = rint(x * 1.4426950408889634), r = __builtin_fma(k, -0x1.62e42fefa39efp-1, x);
+  double p = 1.0;
+#pragma unroll 1
+  for (int n = 13; n >= 1; --n) p = __builtin_fma(p, r * kInverse[n], 1.0);
+  return ldexp(p, (int)k);
+}
+// of s from 1 to 2^24 (or NaN)
+__device__ __forceinline__ double log64(double s) {
+  int k;
+  double f = frexp(s, &k);
+  if (f < 0.70710678118654752) f *= 2.0, --k;
+  // log f = 2 (q + q^3 / 3 + ... + q^23 / 23), q = (f - 1) / (f + 1), |q| <= 0.172
+  const double q = (f - 1.0) / (f + 1.0), q2 = q * q;
+  double p = 0.0;
+#pragma unroll 1
+  for (int n = 23; n >= 1; n -= 2) p = __builtin_fma(p, q2, 1.0 / n);
+  return __builtin_fma((double)k, 0x1.62e42fefa39efp-1, 2.0 * q * p);
+}
+
 // The terms of a token, and the factor of its row of gradients.
 __device__ __forceinline__ double token_terms(const Loss& a, int64_t t, double logp, double* rows) {
   const double w = a.weights ? (double)a.weights[t] : 1.0;
@@ -122,13 +158,13 @@ __device__ __forceinline__ double token_terms(const Loss& a, int64_t t, double l
     rows[0] = rows[1] = rows[2] = rows[3] = 0.0;
     return 0.0;
   }
-  const double A = a.advantages[t], r = exp(logp - (double)a.old_logp[t]);
+  const double A = a.advantages[t], r = exp64(logp - (double)a.old_logp[t]);
   const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
   const bool clipped = (A > 0.0 && r > hi) || (A < 0.0 && r < lo);
   const double pg = -(clipped ? (A > 0.0 ? hi : lo) * A : r * A);
   double slope = clipped ? 0.0 : -r * A, kl = 0.0;
   if (a.ref_logp) {
-    const double u = (double)a.ref_logp[t] - logp, e = exp(u);
+    const double u = (double)a.ref_logp[t] - logp, e = exp64(u);
     kl = e - u - 1.0;
     if (a.kl != 0.0f) slope += (double)a.kl * (1.0 - e);
   }
@@ -141,7 +177,7 @@ __device__ __forceinline__ double token_terms(const Loss& a, int64_t t, double l
 
 // R threads a row, NV vectors each; NV = 0: rows of any length, read again
 template <int LT, int R, int NV>
-__global__ void __launch_bounds__(R) k_loss(unsigned first, Loss a) {
+__global__ void __launch_bounds__(R, NV > 8 ? 4 : 8) k_loss(unsigned first, Loss a) {
   constexpr int E = per_vec<LT>();
   __shared__ float top[R / 64];
   __shared__ double total[R / 64];
@@ -151,23 +187,26 @@ __global__ void __launch_bounds__(R) k_loss(unsigned first, Loss a) {
   const char* row = static_cast<const char*>(a.logits) + t * a.ld * dt_size<LT>();
   char* grow = a.grad ? static_cast<char*>(a.grad) + t * a.ldg * (a.gt == ZQ_F32 ? 4 : 2) : nullptr;
   const float k2 = a.scale * 1.44269504088896340736f;  // exp(scale d) = 2^(k2 d)
-  const int64_t step = (int64_t)R * E;
+  const int V = (int)a.V;  // up to 2^24: places in a row are 32-bit numbers
+  constexpr int STEP = R * E;
 
+  auto zeros = [&]() {
+    for_type(a.gt, [&](auto gt) {
+      const float zero[E] = {};
+      for (int i = threadIdx.x * E; i < V; i += STEP) store_vec<gt>(grow, i, V, zero);
+    });
+  };
   auto none = [&]() {  // no token: no loss, a gradient of zeros
     if (threadIdx.x == 0) {
       if (a.logp) a.logp[t] = 0.0f;
       if (a.rows) a.rows[4 * t] = a.rows[4 * t + 1] = a.rows[4 * t + 2] = a.rows[4 * t + 3] = 0.0;
     }
-    if (!grow) return;
-    const float zero[E] = {};
-    for (int64_t i = threadIdx.x * E; i < a.V; i += step) store_any(a.gt, grow, i, a.V, zero);
+    if (grow) zeros();
   };
-  if (id < 0 || id >= a.V) {
+  if (id < 0 || id >= V) {
     none();
     return;
   }
-  float za[1];
-  load_elems<LT, 1>(row, id, za);
 
   uint32_t z[NV > 0 ? NV : 1][4];
   float m = -kInf;
@@ -177,21 +216,27 @@ __global__ void __launch_bounds__(R) k_loss(unsigned first, Loss a) {
 #pragma unroll
     for (int k = 0; k < E; ++k) m = fmaxf(m, v[k]);
   };
+  float za[1];
   if constexpr (NV > 0) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load_vec<LT>(row, (int64_t)(j * R + threadIdx.x) * E, a.V, z[j]);
+    for (int j = 0; j < NV; ++j) load_vec<LT>(row, (j * R + (int)threadIdx.x) * E, V, z[j]);
+    load_elems<LT, 1>(row, id, za);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) max_of(z[j]);
+    for (int j = 0; j < NV; ++j) {
+      max_of(z[j]);
+      forget(z[j]);
+    }
   } else {
-    for (int64_t i = threadIdx.x * E; i < a.V; i += step) {
-      load_vec<LT>(row, i, a.V, z[0]);
+    load_elems<LT, 1>(row, id, za);
+    for (int i = threadIdx.x * E; i < V; i += STEP) {
+      load_vec<LT>(row, i, V, z[0]);
       max_of(z[0]);
     }
   }
   m = group_max<R>(m, top);
   if (m == -kInf) {  // no logit above -infinity, or none but NaNs
     int nan = 0;
-    for (int64_t i = threadIdx.x; i < a.V; i += R) {
+    for (int i = threadIdx.x; i < V; i += R) {
       float v[1];
       load_elems<LT, 1>(row, i, v);
       nan |= v[0] != v[0];
@@ -213,11 +258,14 @@ __global__ void __launch_bounds__(R) k_loss(unsigned first, Loss a) {
   if constexpr (NV > 0) {
     float s = 0.0f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) s += sum_of(z[j]);
+    for (int j = 0; j < NV; ++j) {
+      s += sum_of(z[j]);
+      forget(z[j]);
+    }
     sum = (double)s;
   } else {
-    for (int64_t i = threadIdx.x * E; i < a.V; i += step) {
-      load_vec<LT>(row, i, a.V, z[0]);
+    for (int i = threadIdx.x * E; i < V; i += STEP) {
+      load_vec<LT>(row, i, V, z[0]);
       sum += (double)sum_of(z[0]);
     }
   }
@@ -225,7 +273,7 @@ __global__ void __launch_bounds__(R) k_loss(unsigned first, Loss a) {
 
   // one wave's work, the others wait for it if they have a gradient to write
   if (threadIdx.x < 64) {
-    const double logp = (double)a.scale * ((double)za[0] - (double)m) - log(sum);
+    const double logp = (double)a.scale * ((double)za[0] - (double)m) - log64(sum);
     double rows[4];
     const double g = a.rows ? token_terms(a, t, logp, rows) : 0.0;
     if (threadIdx.x == 0) {
@@ -240,28 +288,38 @@ __global__ void __launch_bounds__(R) k_loss(unsigned first, Loss a) {
   if (!grow) return;
   __syncthreads();
   const float g = (float)factor, c = (float)(-factor / sum);
-  auto put = [&](const uint32_t(&w)[4], int64_t i) {
-    float v[E];
-    widen<LT>(w, v);
-#pragma unroll
-    for (int k = 0; k < E; ++k) {
-      v[k] = g == 0.0f ? 0.0f : __builtin_amdgcn_exp2f((v[k] - m) * k2) * c;
-      if (i + k == id) v[k] += g;
-    }
-    store_any(a.gt, grow, i, a.V, v);
-  };
-  if constexpr (NV > 0) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int64_t i = (int64_t)(j * R + threadIdx.x) * E;
-      if (i < a.V) put(z[j], i);
-    }
-  } else {
-    for (int64_t i = threadIdx.x * E; i < a.V; i += step) {
-      load_vec<LT>(row, i, a.V, z[0]);
-      put(z[0], i);
-    }
+  if (g == 0.0f) {  // masked, or clipped without a KL term
+    zeros();
+    return;
   }
+  int thread = threadIdx.x;
+  asm volatile("" : "+v"(thread));  // places computed anew: those of the loads are not kept
+  for_type(a.gt, [&](auto gt) {
+    auto put = [&](const uint32_t(&w)[4], int i) {
+      float v[E];
+      widen<LT>(w, v);
+#pragma unroll
+      for (int k = 0; k < E; ++k) v[k] = __builtin_amdgcn_exp2f((v[k] - m) * k2) * c;
+      const uint32_t at = (uint32_t)((int)id - i);
+      if (at < (uint32_t)E) {
+#pragma unroll
+        for (int k = 0; k < E; ++k) v[k] = at == (uint32_t)k ? v[k] + g : v[k];
+      }
+      store_vec<gt>(grow, i, V, v);
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int i = (j * R + thread) * E;
+        if (i < V) put(z[j], i);
+      }
+    } else {
+      for (int i = threadIdx.x * E; i < V; i += STEP) {
+        load_vec<LT>(row, i, V, z[0]);
+        put(z[0], i);
+      }
+    }
+  });
 }
 
 // the sums over the rows: each thread its rows in their order, then the threads
@@ -284,19 +342,35 @@ __global__ void __launch_bounds__(1024) k_loss_sums(const double* __restrict__ r
   sums[threadIdx.x] = (float)v;
 }
 
-// Threads of a row and their vectors, by the row's bytes.
+// Threads of a row and their vectors, by the row's vectors of 16 bytes: the fewest
+// threads that hold them in 8 each, then 1,024 with more.
+template <int LT, int R, int NV>
+int rows_in(const Loss& a, hipStream_t st) {
+  return launch_parts(&k_loss<LT, R, NV>, a.T, R, st, a);
+}
 template <int LT>
 int rows_of(const Loss& a, hipStream_t st) {
   const int64_t vecs = (a.V + per_vec<LT>() - 1) / per_vec<LT>();
-  if (vecs <= 256 * 2) return launch_parts(&k_loss<LT, 256, 2>, a.T, 256, st, a);
-  if (vecs <= 256 * 4) return launch_parts(&k_loss<LT, 256, 4>, a.T, 256, st, a);
-  if (vecs <= 256 * 8) return launch_parts(&k_loss<LT, 256, 8>, a.T, 256, st, a);
-  if (vecs <= 512 * 8) return launch_parts(&k_loss<LT, 512, 8>, a.T, 512, st, a);
-  if (vecs <= 512 * 12) return launch_parts(&k_loss<LT, 512, 12>, a.T, 512, st, a);
-  if (vecs <= 512 * 16) return launch_parts(&k_loss<LT, 512, 16>, a.T, 512, st, a);
-  if (vecs <= 1024 * 12) return launch_parts(&k_loss<LT, 1024, 12>, a.T, 1024, st, a);
-  if (vecs <= 1024 * 16) return launch_parts(&k_loss<LT, 1024, 16>, a.T, 1024, st, a);
-  return launch_parts(&k_loss<LT, 1024, 0>, a.T, 1024, st, a);
+  const auto per = [&](int64_t threads) { return (vecs + threads - 1) / threads; };
+  if (per(64) <= 2) return rows_in<LT, 64, 2>(a, st);
+  if (per(64) <= 4) return rows_in<LT, 64, 4>(a, st);
+  if (per(256) <= 2) return rows_in<LT, 256, 2>(a, st);
+  if (per(256) <= 3) return rows_in<LT, 256, 3>(a, st);
+  if (per(256) <= 4) return rows_in<LT, 256, 4>(a, st);
+  if (per(256) <= 6) return rows_in<LT, 256, 6>(a, st);
+  if (per(256) <= 8) return rows_in<LT, 256, 8>(a, st);
+  if (per(512) <= 5) return rows_in<LT, 512, 5>(a, st);
+  if (per(512) <= 6) return rows_in<LT, 512, 6>(a, st);
+  if (per(512) <= 7) return rows_in<LT, 512, 7>(a, st);
+  if (per(512) <= 8) return rows_in<LT, 512, 8>(a, st);
+  if (per(1024) <= 5) return rows_in<LT, 1024, 5>(a, st);
+  if (per(1024) <= 6) return rows_in<LT, 1024, 6>(a, st);
+  if (per(1024) <= 7) return rows_in<LT, 1024, 7>(a, st);
+  if (per(1024) <= 8) return rows_in<LT, 1024, 8>(a, st);
+  if (per(1024) <= 10) return rows_in<LT, 1024, 10>(a, st);
+  if (per(1024) <= 13) return rows_in<LT, 1024, 13>(a, st);
+  if (per(1024) <= 16) return rows_in<LT, 1024, 16>(a, st);
+  return rows_in<LT, 1024, 0>(a, st);
 }
 
 int run(const Loss& a, int lt, hipStream_t st) {

@@ -31,48 +31,81 @@ constexpr int64_t kMaxWidth = 1 << 24;
 
 // ---------------------------------------------------------------- rows
 
-// 8 elements from element i of n; zeros behind the end
-template <int DT>
-__device__ __forceinline__ void load8(const void* row, int64_t i, int64_t n, float (&v)[8]) {
-  if (i + 8 <= n) {
-    load_elems<DT, 8, true>(row, i, v);
+// Places in a row are 32-bit numbers of bytes: rows have up to 2^24 elements.  WHOLE: D is
+// a multiple of 8, so a vector of 8 elements is in the row or behind it.
+
+// the words of 8 elements from element i of n; zeros behind the end
+template <int DT, bool WHOLE>
+__device__ __forceinline__ void load8(const char* row, int i, int n, uint32_t (&w)[2 * dt_size<DT>()]) {
+  constexpr int S = dt_size<DT>();
+#pragma unroll
+  for (int k = 0; k < 2 * S; ++k) w[k] = 0u;
+  if (WHOLE ? i < n : i + 8 <= n) {
+    load_words_any<true>(row + (uint32_t)i * S, w);
+  } else if (!WHOLE && i < n) {
+#pragma unroll
+    for (int k = 0; k < 7; ++k) {
+      if (i + k >= n) continue;
+      if constexpr (S == 4) w[k] = *reinterpret_cast<const uint32_t*>(row + (uint32_t)(i + k) * 4);
+      else w[k / 2] |= (uint32_t) * reinterpret_cast<const uint16_t*>(row + (uint32_t)(i + k) * 2) << (16 * (k & 1));
+    }
+  }
+}
+// of a type that is known when the kernel runs: in the first 4 or in all 8 words
+template <bool WHOLE>
+__device__ __forceinline__ void load8(int dt, const char* row, int i, int n, uint32_t (&w)[8]) {
+  if (dt == ZQ_F32) {
+    load8<ZQ_F32, WHOLE>(row, i, n, w);
     return;
   }
+  uint32_t t[4];
+  load8<ZQ_BF16, WHOLE>(row, i, n, t);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    float t[1] = {0.0f};
-    if (i + k < n) load_elems<DT, 1>(row, i + k, t);
-    v[k] = t[0];
-  }
+  for (int k = 0; k < 4; ++k) w[k] = t[k], w[k + 4] = 0u;
 }
-__device__ __forceinline__ void load8_any(int dt, const void* row, int64_t i, int64_t n, float (&v)[8]) {
-  if (dt == ZQ_F32) load8<ZQ_F32>(row, i, n, v);
-  else if (dt == ZQ_BF16) load8<ZQ_BF16>(row, i, n, v);
-  else load8<ZQ_F16>(row, i, n, v);
+__device__ __forceinline__ void widen8(int dt, const uint32_t (&w)[8], float (&v)[8]) {
+  if (dt == ZQ_F32) widen<ZQ_F32>(w, v);
+  else if (dt == ZQ_BF16) widen<ZQ_BF16>(w, v);
+  else widen<ZQ_F16>(w, v);
 }
-template <int DT>
-__device__ __forceinline__ void store8(void* row, int64_t i, int64_t n, const float (&v)[8]) {
-  if (i + 8 <= n) {
-    store_elems<DT, 8, true>(row, i, v);
-    return;
-  }
+template <int DT, bool WHOLE>
+__device__ __forceinline__ void store8(char* row, int i, int n, const float (&v)[8]) {
+  constexpr int S = dt_size<DT>();
+  if (WHOLE ? i < n : i + 8 <= n) {
+    store_elems<DT, 8, true>(row + (uint32_t)i * S, 0, v);
+  } else if (!WHOLE && i < n) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float t[1] = {v[k]};
-    if (i + k < n) store_elems<DT, 1>(row, i + k, t);
+    for (int k = 0; k < 7; ++k) {
+      const float t[1] = {v[k]};
+      if (i + k < n) store_elems<DT, 1>(row + (uint32_t)(i + k) * S, 0, t);
+    }
   }
 }
-__device__ __forceinline__ void store8_any(int dt, void* row, int64_t i, int64_t n, const float (&v)[8]) {
-  if (dt == ZQ_F32) store8<ZQ_F32>(row, i, n, v);
-  else if (dt == ZQ_BF16) store8<ZQ_BF16>(row, i, n, v);
-  else store8<ZQ_F16>(row, i, n, v);
+template <bool WHOLE>
+__device__ __forceinline__ void store8(int dt, char* row, int i, int n, const float (&v)[8]) {
+  if (dt == ZQ_F32) store8<ZQ_F32, WHOLE>(row, i, n, v);
+  else if (dt == ZQ_BF16) store8<ZQ_BF16, WHOLE>(row, i, n, v);
+  else store8<ZQ_F16, WHOLE>(row, i, n, v);
 }
+// the words of 8 values as a type holds them
 template <int DT>
-__device__ __forceinline__ float as_stored(float v) {
-  if constexpr (DT == ZQ_BF16) return u2f(bf16x2_bits(v, 0.0f) << 16);
-  else if constexpr (DT == ZQ_F16) return h2f(f2h(v));
-  else return v;
+__device__ __forceinline__ void narrow8(const float (&v)[8], uint32_t (&w)[2 * dt_size<DT>()]) {
+#pragma unroll
+  for (int k = 0; k < 2 * dt_size<DT>(); ++k) {
+    if constexpr (DT == ZQ_F32) w[k] = f2u(v[k]);
+    else if constexpr (DT == ZQ_BF16) w[k] = bf16x2_bits(v[2 * k], v[2 * k + 1]);
+    else w[k] = f2h(v[2 * k]) | (f2h(v[2 * k + 1]) << 16);
+  }
 }
+// The words are what they were, but the compiler does not know: what it has derived from
+// them (their widened values) is not kept in registers across this point.
+template <int N>
+__device__ __forceinline__ void forget(uint32_t (&w)[N]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) asm volatile("" : "+v"(w[k]));
+}
+
+constexpr int kind_bytes(int dt) { return dt == ZQ_F32 ? 4 : 2; }
 
 // ---------------------------------------------------------------- sums over a row's threads
 
@@ -124,7 +157,7 @@ struct Norm {
 // 8 values of a row as codes of the INT8 format.  All threads of the row's waves call it;
 // a block of 1,024 is two waves', whose halves meet in `half` (LDS, R / 64 values).
 template <int R>
-__device__ __forceinline__ void put_int8(const Norm& a, int64_t at, int64_t i, const float (&v)[8], uint32_t* half) {
+__device__ __forceinline__ void put_int8(const Norm& a, int64_t at, int i, const float (&v)[8], uint32_t* half) {
   uint32_t t = 0u;
 #pragma unroll
   for (int k = 0; k < 8; ++k) t = max(t, f2u(v[k]) & 0x7fffffffu);
@@ -138,7 +171,7 @@ __device__ __forceinline__ void put_int8(const Norm& a, int64_t at, int64_t i, c
   const float m = u2f(t);
   const bool fits = m >= 0x1p-119f;
   const float s = fits ? m / 127.0f : 0.0f, r = fits ? 127.0f / m : 0.0f;
-  if (i >= a.D) return;
+  if (i >= (int)a.D) return;
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int k = 0; k < 8; ++k) w[k / 4] |= ((uint32_t)(int)rintf(v[k] * r) & 0xffu) << (8 * (k & 3));
@@ -146,46 +179,54 @@ __device__ __forceinline__ void put_int8(const Norm& a, int64_t at, int64_t i, c
   if ((i & ((1 << a.lgB) - 1)) == 0) a.scales[(at + i) >> a.lgB] = s;
 }
 
-// NV vectors of 8 elements a thread; NV = 0: rows of any length, h read again
-template <int XT, int R, int NV>
-__global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms(unsigned first, Norm a) {
-  constexpr int THREADS = R < 256 ? 256 : R;
-  __shared__ double slot[R / 64];
-  __shared__ uint32_t half[R / 64];
-  const int lane = threadIdx.x % R;
-  int64_t t = (int64_t)(first + blockIdx.x) * (THREADS / R) + threadIdx.x / R;
-  if (R == 64 && t >= a.T) return;  // a wave's own row: the others go on
-  const int64_t at = t * a.D;       // the row's first element
+// NV vectors of 8 elements a thread; NV = 0: rows of any length, h read again.
+// Everything a row needs is loaded before the first store: loads would wait behind stores
+// that might be to their memory.
+template <int XT, int R, int NV, bool WHOLE>
+__device__ __forceinline__ void norm_row(const Norm& a, int64_t t, int lane, double* slot, uint32_t* half) {
+  constexpr int W = 2 * dt_size<XT>(), N = NV > 0 ? NV : 1;
+  const int D = (int)a.D;
+  const int64_t at = t * a.D;  // the row's first element
   const char* x = static_cast<const char*>(a.x) + at * dt_size<XT>();
   const char* res = a.residual ? static_cast<const char*>(a.residual) + at * dt_size<XT>() : nullptr;
+  const char* weight = static_cast<const char*>(a.weight);
   char* h = a.residual ? static_cast<char*>(a.h) + at * dt_size<XT>() : nullptr;
-  char* y = static_cast<char*>(a.y) + at * (a.yt == ZQ_F32 ? 4 : 2);
+  char* y = static_cast<char*>(a.y) + at * kind_bytes(a.yt);
 
   double sum = 0.0;
-  auto take = [&](int64_t i, float (&v)[8]) {
-    load8<XT>(x, i, a.D, v);
+  uint32_t xw[N][W], rw[N][W], ww[N][8];
+  auto load = [&](int j, int i) {
+    load8<XT, WHOLE>(x, i, D, xw[j]);
+    if (res) load8<XT, WHOLE>(res, i, D, rw[j]);
+  };
+  auto add = [&](int j, int i) {  // xw becomes h's words
+    float v[8];
+    widen<XT>(xw[j], v);
     if (res) {
       float b[8];
-      load8<XT>(res, i, a.D, b);
+      widen<XT>(rw[j], b);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = as_stored<XT>(v[k] + b[k]);
-      store8<XT>(h, i, a.D, v);
+      for (int k = 0; k < 8; ++k) v[k] = v[k] + b[k];
+      narrow8<XT>(v, xw[j]);
+      widen<XT>(xw[j], v);
+      store8<XT, WHOLE>(h, i, D, v);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
+    forget(xw[j]);
   };
-  auto put = [&](int64_t i, float (&v)[8], float rstd) {
-    float w[8];
-    if (a.weight) {
-      load8_any(a.wt, a.weight, i, a.D, w);
-    } else {
+  auto put = [&](int j, int i, float rstd) {
+    float v[8], w[8];
+    widen<XT>(xw[j], v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+    for (int k = 0; k < 8; ++k) v[k] = v[k] * rstd;
+    if (weight) {
+      widen8(a.wt, ww[j], w);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = v[k] * w[k];
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = (v[k] * rstd) * w[k];
     if (a.yt == kInt8) put_int8<R>(a, at, i, v, half);
-    else store8_any(a.yt, y, i, a.D, v);
+    else store8<WHOLE>(a.yt, y, i, D, v);
   };
   auto finish = [&]() {
     sum = row_sum<R>(sum, slot);
@@ -195,25 +236,42 @@ __global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms(unsigned first, Norm 
   };
 
   if constexpr (NV > 0) {
-    float v[NV][8];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) take((int64_t)(j * R + lane) * 8, v[j]);
+    for (int j = 0; j < NV; ++j) load(j, (j * R + lane) * 8);
+    if (weight) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) load8<WHOLE>(a.wt, weight, (j * R + lane) * 8, D, ww[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) add(j, (j * R + lane) * 8);
     const float rstd = finish();
 #pragma unroll
-    for (int j = 0; j < NV; ++j) put((int64_t)(j * R + lane) * 8, v[j], rstd);
+    for (int j = 0; j < NV; ++j) put(j, (j * R + lane) * 8, rstd);
   } else {
-    const int64_t end = (a.D + 8 * R - 1) / (8 * R) * (8 * R);  // all threads take every turn
-    for (int64_t i = lane * 8; i < end; i += 8 * R) {
-      float v[8];
-      take(i, v);
+    const int end = (D + 8 * R - 1) / (8 * R) * (8 * R);  // all threads take every turn
+    for (int i = lane * 8; i < end; i += 8 * R) {
+      load(0, i);
+      add(0, i);
     }
     const float rstd = finish();
-    for (int64_t i = lane * 8; i < end; i += 8 * R) {
-      float v[8];
-      load8<XT>(res ? h : x, i, a.D, v);  // this thread's own writes
-      put(i, v, rstd);
+    for (int i = lane * 8; i < end; i += 8 * R) {
+      load8<XT, WHOLE>(res ? h : x, i, D, xw[0]);  // h: this thread's own writes
+      if (weight) load8<WHOLE>(a.wt, weight, i, D, ww[0]);
+      put(0, i, rstd);
     }
   }
+}
+
+template <int XT, int R, int NV>
+__global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms(unsigned first, Norm a) {
+  constexpr int THREADS = R < 256 ? 256 : R;
+  __shared__ double slot[R / 64];
+  __shared__ uint32_t half[R / 64];
+  const int lane = threadIdx.x % R;
+  const int64_t t = (int64_t)(first + blockIdx.x) * (THREADS / R) + threadIdx.x / R;
+  if (R == 64 && t >= a.T) return;  // a wave's own row: the others go on
+  if (a.D % 8 == 0) norm_row<XT, R, NV, true>(a, t, lane, slot, half);
+  else norm_row<XT, R, NV, false>(a, t, lane, slot, half);
 }
 
 // ---------------------------------------------------------------- gradient
@@ -231,83 +289,135 @@ struct NormGrad {
   int8_t gt, wt;
 };
 
-template <int XT, int R, int NV, bool SAME>
+// The rows of group g.  A thread keeps its columns' weight and sums of dw; AHEAD: the next
+// row's h and dy are loaded before the present row's sum is taken.
+template <int XT, int R, int NV, bool SAME, bool AHEAD, bool WHOLE>
+__device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, float (*slot)[R / 64]) {
+  constexpr int W = 2 * dt_size<XT>(), WY = SAME ? W : 8;
+  const int D = (int)a.D;
+  const int64_t row_bytes = a.D * dt_size<XT>(), dy_bytes = a.D * (SAME ? dt_size<XT>() : kind_bytes(a.gt));
+  float w[NV][8], dw[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dw[j][k] = 0.0f, w[j][k] = 1.0f;
+    if (a.weight) {
+      uint32_t t[8];
+      load8<WHOLE>(a.wt, static_cast<const char*>(a.weight), (j * R + lane) * 8, D, t);
+      widen8(a.wt, t, w[j]);
+    }
+  }
+  uint32_t hw[NV][W], yw[NV][WY], dhw[NV][W], hn[AHEAD ? NV : 1][W], yn[AHEAD ? NV : 1][WY];
+  auto load = [&](int64_t t, auto& hw_, auto& yw_) {
+    const char* hr = static_cast<const char*>(a.h) + t * row_bytes;
+    const char* yr = static_cast<const char*>(a.dy) + t * dy_bytes;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      load8<XT, WHOLE>(hr, (j * R + lane) * 8, D, hw_[j]);
+      if constexpr (SAME) load8<XT, WHOLE>(yr, (j * R + lane) * 8, D, yw_[j]);
+      else load8<WHOLE>(a.gt, yr, (j * R + lane) * 8, D, yw_[j]);
+    }
+  };
+  auto dy_of = [&](int j, float (&v)[8]) {
+    if constexpr (SAME) widen<XT>(yw[j], v);
+    else widen8(a.gt, yw[j], v);
+  };
+  int turn = 0;
+  if constexpr (AHEAD) load(g, hw, yw);
+  for (int64_t t = g; t < a.T; t += a.groups, turn ^= 1) {
+    const char* dhr = a.dh ? static_cast<const char*>(a.dh) + t * row_bytes : nullptr;
+    char* dxr = static_cast<char*>(a.dx) + t * row_bytes;
+    const float rstd = a.rstd[t];
+    if constexpr (!AHEAD) load(t, hw, yw);
+    if (dhr) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) load8<XT, WHOLE>(dhr, (j * R + lane) * 8, D, dhw[j]);
+    }
+    if constexpr (AHEAD) {
+      if (t + a.groups < a.T) load(t + a.groups, hn, yn);
+    }
+    float c = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float h[8], dy[8];
+      widen<XT>(hw[j], h);
+      dy_of(j, dy);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float xh = h[k] * rstd;
+        dw[j][k] += dy[k] * xh;
+        c += (dy[k] * w[j][k]) * xh;
+      }
+      forget(hw[j]);
+      forget(yw[j]);
+    }
+    c = row_sum<R>(c, slot[turn]) / (float)a.D;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float h[8], dy[8], d[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      widen<XT>(hw[j], h);
+      dy_of(j, dy);
+      if (dhr) widen<XT>(dhw[j], d);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) d[k] += (dy[k] * w[j][k] - (h[k] * rstd) * c) * rstd;
+      store8<XT, WHOLE>(dxr, (j * R + lane) * 8, D, d);
+    }
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) hw[j][k] = hn[j][k];
+#pragma unroll
+        for (int k = 0; k < WY; ++k) yw[j][k] = yn[j][k];
+      }
+    }
+  }
+  if (!a.part) return;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    store8<ZQ_F32, WHOLE>(reinterpret_cast<char*>(a.part + (int64_t)g * a.D), (j * R + lane) * 8, D, dw[j]);
+}
+
+template <int XT, int R, int NV, bool SAME, bool AHEAD>
 __global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms_grad(NormGrad a) {
   constexpr int THREADS = R < 256 ? 256 : R;
   __shared__ float slot[2][R / 64];
   const int lane = threadIdx.x % R;
   const int g = blockIdx.x * (THREADS / R) + threadIdx.x / R;
   if (R == 64 && g >= a.groups) return;  // a wave's own rows
-  float w[NV][8], dw[NV][8];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int64_t i = (int64_t)(j * R + lane) * 8;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) dw[j][k] = 0.0f, w[j][k] = 1.0f;
-    if (a.weight) load8_any(a.wt, a.weight, i, a.D, w[j]);
-  }
-  int turn = 0;
-  for (int64_t t = g; t < a.T; t += a.groups, turn ^= 1) {
-    const int64_t at = t * a.D;
-    const char* hr = static_cast<const char*>(a.h) + at * dt_size<XT>();
-    const char* dyr = static_cast<const char*>(a.dy) + at * (SAME ? dt_size<XT>() : a.gt == ZQ_F32 ? 4 : 2);
-    const float rstd = a.rstd[t];
-    float xh[NV][8], gw[NV][8], c = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int64_t i = (int64_t)(j * R + lane) * 8;
-      load8<XT>(hr, i, a.D, xh[j]);
-      if constexpr (SAME) load8<XT>(dyr, i, a.D, gw[j]);
-      else load8_any(a.gt, dyr, i, a.D, gw[j]);
-    }
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        xh[j][k] = xh[j][k] * rstd;
-        dw[j][k] += gw[j][k] * xh[j][k];
-        gw[j][k] = gw[j][k] * w[j][k];
-        c += gw[j][k] * xh[j][k];
-      }
-    }
-    c = row_sum<R>(c, slot[turn]) / (float)a.D;
-    const char* dhr = a.dh ? static_cast<const char*>(a.dh) + at * dt_size<XT>() : nullptr;
-    char* dxr = static_cast<char*>(a.dx) + at * dt_size<XT>();
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int64_t i = (int64_t)(j * R + lane) * 8;
-      float d[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-      if (dhr) load8<XT>(dhr, i, a.D, d);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) d[k] += (gw[j][k] - xh[j][k] * c) * rstd;
-      store8<XT>(dxr, i, a.D, d);
-    }
-  }
-  if (!a.part) return;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) store8<ZQ_F32>(a.part + (int64_t)g * a.D, (int64_t)(j * R + lane) * 8, a.D, dw[j]);
+  if (a.D % 8 == 0) grad_rows<XT, R, NV, SAME, AHEAD, true>(a, g, lane, slot);
+  else grad_rows<XT, R, NV, SAME, AHEAD, false>(a, g, lane, slot);
 }
 
 // rows of any length: dx, a row a workgroup, read twice
 template <int XT>
 __global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad a) {
   __shared__ double slot[16];
+  const int D = (int)a.D;
   const int64_t t = first + blockIdx.x, at = t * a.D;
   const char* hr = static_cast<const char*>(a.h) + at * dt_size<XT>();
-  const char* dyr = static_cast<const char*>(a.dy) + at * (a.gt == ZQ_F32 ? 4 : 2);
+  const char* dyr = static_cast<const char*>(a.dy) + at * kind_bytes(a.gt);
   const char* dhr = a.dh ? static_cast<const char*>(a.dh) + at * dt_size<XT>() : nullptr;
   char* dxr = static_cast<char*>(a.dx) + at * dt_size<XT>();
   const float rstd = a.rstd[t];
-  auto take = [&](int64_t i, float (&xh)[8], float (&gw)[8]) {
-    float w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
-    load8<XT>(hr, i, a.D, xh);
-    load8_any(a.gt, dyr, i, a.D, gw);
-    if (a.weight) load8_any(a.wt, a.weight, i, a.D, w);
+  auto take = [&](int i, float (&xh)[8], float (&gw)[8]) {
+    uint32_t hw[2 * dt_size<XT>()], yw[8], ww[8];
+    load8<XT, false>(hr, i, D, hw);
+    load8<false>(a.gt, dyr, i, D, yw);
+    widen<XT>(hw, xh);
+    widen8(a.gt, yw, gw);
+    if (a.weight) {
+      float w[8];
+      load8<false>(a.wt, static_cast<const char*>(a.weight), i, D, ww);
+      widen8(a.wt, ww, w);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) xh[k] = xh[k] * rstd, gw[k] = gw[k] * w[k];
+      for (int k = 0; k < 8; ++k) gw[k] = gw[k] * w[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) xh[k] = xh[k] * rstd;
   };
   double sum = 0.0;
-  for (int64_t i = threadIdx.x * 8; i < a.D; i += 8192) {
+  for (int i = threadIdx.x * 8; i < D; i += 8192) {
     float xh[8], gw[8], c = 0.0f;
     take(i, xh, gw);
 #pragma unroll
@@ -315,13 +425,17 @@ __global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad
     sum += (double)c;
   }
   const float c = (float)(row_sum<1024>(sum, slot) / (double)a.D);
-  for (int64_t i = threadIdx.x * 8; i < a.D; i += 8192) {
+  for (int i = threadIdx.x * 8; i < D; i += 8192) {
     float xh[8], gw[8], d[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     take(i, xh, gw);
-    if (dhr) load8<XT>(dhr, i, a.D, d);
+    if (dhr) {
+      uint32_t dw[2 * dt_size<XT>()];
+      load8<XT, false>(dhr, i, D, dw);
+      widen<XT>(dw, d);
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) d[k] += (gw[k] - xh[k] * c) * rstd;
-    store8<XT>(dxr, i, a.D, d);
+    store8<XT, false>(dxr, i, D, d);
   }
 }
 
@@ -329,20 +443,22 @@ __global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad
 template <int XT>
 __global__ void __launch_bounds__(256) k_rms_grad_columns(unsigned first, NormGrad a, unsigned tiles) {
   const unsigned b = first + blockIdx.x;
-  const int g = (int)(b / tiles);
-  const int64_t i = ((int64_t)(b % tiles) * 256 + threadIdx.x) * 8;
-  if (i >= a.D) return;
+  const int g = (int)(b / tiles), D = (int)a.D, i = (int)((b % tiles) * 256 + threadIdx.x) * 8;
+  if (i >= D) return;
   float dw[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   for (int64_t t = g; t < a.T; t += a.groups) {
     const int64_t at = t * a.D;
+    uint32_t hw[2 * dt_size<XT>()], yw[8];
     float h[8], dy[8];
-    load8<XT>(static_cast<const char*>(a.h) + at * dt_size<XT>(), i, a.D, h);
-    load8_any(a.gt, static_cast<const char*>(a.dy) + at * (a.gt == ZQ_F32 ? 4 : 2), i, a.D, dy);
+    load8<XT, false>(static_cast<const char*>(a.h) + at * dt_size<XT>(), i, D, hw);
+    load8<false>(a.gt, static_cast<const char*>(a.dy) + at * kind_bytes(a.gt), i, D, yw);
+    widen<XT>(hw, h);
+    widen8(a.gt, yw, dy);
     const float rstd = a.rstd[t];
 #pragma unroll
     for (int k = 0; k < 8; ++k) dw[k] += dy[k] * (h[k] * rstd);
   }
-  store8<ZQ_F32>(a.part + (int64_t)g * a.D, i, a.D, dw);
+  store8<ZQ_F32, false>(reinterpret_cast<char*>(a.part + (int64_t)g * a.D), i, D, dw);
 }
 
 // dw from the groups' sums: 64 columns a workgroup, 16 slices of the groups, each in its
@@ -442,15 +558,22 @@ int64_t groups_for(int64_t T, int64_t D) {
   return g < T ? g : T < 1 ? 1 : T;
 }
 
+// 16-bit rows: up to 4 vectors a thread, the next row ahead (3 vectors 140 registers); wider
+// words: half as many vectors.
 template <int XT, bool SAME>
 int backward_short(const NormGrad& a, hipStream_t st) {
+  constexpr bool WIDE = XT == ZQ_F32 || !SAME;
   const unsigned g = (unsigned)a.groups;
-  if (a.D <= 512) return launch(&k_rms_grad<XT, 64, 1, SAME>, (g + 3) / 4, 256u, st, a);
-  if (a.D <= 2048) return launch(&k_rms_grad<XT, 256, 1, SAME>, g, 256u, st, a);
-  if (a.D <= 4096) return launch(&k_rms_grad<XT, 256, 2, SAME>, g, 256u, st, a);
-  if (a.D <= 6144) return launch(&k_rms_grad<XT, 256, 3, SAME>, g, 256u, st, a);
-  if (a.D <= 8192) return launch(&k_rms_grad<XT, 256, 4, SAME>, g, 256u, st, a);
-  return launch(&k_rms_grad<XT, 1024, 2, SAME>, g, 1024u, st, a);
+  if (a.D <= 512) return launch(&k_rms_grad<XT, 64, 1, SAME, true>, (g + 3) / 4, 256u, st, a);
+  if (a.D <= 2048) return launch(&k_rms_grad<XT, 256, 1, SAME, true>, g, 256u, st, a);
+  if (a.D <= 4096) return launch(&k_rms_grad<XT, 256, 2, SAME, true>, g, 256u, st, a);
+  if constexpr (WIDE) {
+    if (a.D <= 8192) return launch(&k_rms_grad<XT, 512, 2, SAME, true>, g, 512u, st, a);
+  } else {
+    if (a.D <= 6144) return launch(&k_rms_grad<XT, 256, 3, SAME, true>, g, 256u, st, a);
+    if (a.D <= 8192) return launch(&k_rms_grad<XT, 256, 4, SAME, true>, g, 256u, st, a);
+  }
+  return launch(&k_rms_grad<XT, 1024, 2, SAME, !WIDE>, g, 1024u, st, a);
 }
 
 template <int XT>
