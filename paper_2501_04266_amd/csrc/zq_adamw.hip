@@ -59,7 +59,7 @@ static_assert(sizeof(Entry) == 112, "table layout");
 
 // The step's numbers.
 struct Coef {
-  double lr, bias1;  // bias1 = 1 - b1^t
+  double lr, rate;  // rate = lr / (1 - b1^t)
   float b1, om1, b2, om2, root, eps, max_norm, scale;
   uint32_t key, pad;
 };
@@ -86,7 +86,7 @@ __host__ __device__ inline Coef coef_of(const zq_adamw_args& a, int64_t step, do
   Coef c = {};
   if (step < 1) step = 1;
   c.lr = lr;
-  c.bias1 = 1.0 - pow(a.beta1, (double)step);
+  c.rate = lr / (1.0 - pow(a.beta1, (double)step));
   c.b1 = (float)a.beta1;
   c.om1 = (float)(1.0 - a.beta1);
   c.b2 = (float)a.beta2;
@@ -106,60 +106,120 @@ __global__ void k_adamw_numbers(char* __restrict__ table, zq_adamw_args a, const
 
 // ---------------------------------------------------------------- 8-bit floats and blocks
 
-// e4m3 with a sign (bias 7) or e5m2 without (bias 15): a code's bits are the top of a
-// binary32 number's exponent and mantissa, times a power of two.
+// A code's bits are the top of a binary32 number's exponent and mantissa, times a power of
+// two: value = number(code << shift) / unit.
 template <bool SIGNED>
 struct F8 {
   static constexpr int shift = SIGNED ? 20 : 21;
   static constexpr float top = SIGNED ? 448.0f : 57344.0f;
-  static constexpr float unit = SIGNED ? 0x1p-120f : 0x1p-112f;  // code = bits(value * unit) >> shift
-  static constexpr float back = SIGNED ? 0x1p120f : 0x1p112f;
-  static constexpr uint32_t last = SIGNED ? 126u : 123u;         // the code of top
-  static __device__ __forceinline__ float value(uint32_t code) {
-    const uint32_t mag = (code & 0x7fu) << shift;
-    return u2f(SIGNED ? mag | (code & 0x80u) << 24 : mag) * back;
-  }
-  // drawn: 16 random bits
-  static __device__ __forceinline__ uint32_t code(float x, float r, uint32_t drawn) {
-    const float y = (fabsf(x) * r) * unit;
-    uint32_t c = (f2u(y) + (drawn << (shift - 16)) + (1u << (shift - 17))) >> shift;
-    c = c < last ? c : last;
-    return SIGNED && x < 0.0f ? c | 0x80u : c;
-  }
+  static constexpr float unit = SIGNED ? 0x1p-120f : 0x1p-112f;
+  static constexpr uint32_t last = SIGNED ? 126u : 123u;  // the code of top
 };
 
-// The largest of `v` (bits of non-negative numbers, which order as they do) over each
-// group of `lanes` lanes, 1 to 64, the same in all lanes of the wave.
-__device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes) {
-  if (lanes >= 2) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));    // quad_perm 1,0,3,2
-  if (lanes >= 4) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));    // quad_perm 2,3,0,1
-  if (lanes >= 8) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));   // row_half_mirror
-  if (lanes >= 16) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, false));  // row_mirror
-  if (lanes >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-  if (lanes >= 64) v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
-  return v;
+// 4 codes, exactly
+template <bool SIGNED>
+__device__ __forceinline__ void decode8(uint32_t w, float (&v)[4]) {
+  f32x2_t lo, hi;
+  if constexpr (SIGNED) {
+    lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false);
+    hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  } else {
+    lo = __builtin_amdgcn_cvt_pk_f32_bf8((int)w, false);
+    hi = __builtin_amdgcn_cvt_pk_f32_bf8((int)w, true);
+  }
+  v[0] = lo.x, v[1] = lo.y, v[2] = hi.x, v[3] = hi.y;
 }
 
-// The largest magnitude of each step's block (2^lgB elements, 32 to 1,024).
-__device__ __forceinline__ void block_max(const float (&x)[kSteps][4], int lgB, float (&a)[kSteps]) {
-  uint32_t w[kSteps];
+// The code of x * r in the top byte of the result.  drawn: 16 bits of m's in the low half of
+// a word, of v's in the high half; they are scaled and added below the code in one instruction.
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t code_on_top(float x, float r, uint32_t drawn) {
+  const uint32_t y = f2u((fabsf(x) * r) * F8<SIGNED>::unit);
+  uint32_t t;
+  if constexpr (SIGNED) asm("v_mad_u32_u16 %0, %1, 16, %2" : "=v"(t) : "v"(drawn), "v"(y));
+  else asm("v_mad_u32_u16 %0, %1, 32, %2 op_sel:[1,0,0,0]" : "=v"(t) : "v"(drawn), "v"(y));
+  t = (t + (1u << (F8<SIGNED>::shift - 17))) << (24 - F8<SIGNED>::shift);
+  t = min(t, F8<SIGNED>::last << 24 | 0xffffffu);
+  return SIGNED ? (t & 0x7fffffffu) | (f2u(x) & 0x80000000u) : t;
+}
+// the top bytes of 4 words, or their lowest
+__device__ __forceinline__ uint32_t pack_top(const uint32_t (&t)[4]) {
+  return __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0703u) | __builtin_amdgcn_perm(t[3], t[2], 0x07030c0cu);
+}
+__device__ __forceinline__ uint32_t pack_low(const uint32_t (&t)[4]) {
+  return __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0400u) | __builtin_amdgcn_perm(t[3], t[2], 0x04000c0cu);
+}
+
+// 32 drawn bits of each of 4 elements from element i on, a multiple of 4: mix(key ^ (i + k)).
+// The first product's factors differ in their two lowest bits alone, so 3 of the 4 are the
+// first plus or minus the constant and its double (a 32-bit product takes 4 cycles of any other).
+__device__ __forceinline__ void draw4(uint32_t key, uint32_t i, uint32_t (&w)[4]) {
+  constexpr uint32_t C = 0x6A09E667u;
+  uint32_t x = key ^ i;
+  x ^= x >> 16;
+  const uint32_t d1 = x & 1u ? 0u - C : C, d2 = x & 2u ? 0u - 2u * C : 2u * C;
+  w[0] = x * C;
+  w[1] = w[0] + d1;
+  w[2] = w[0] + d2;
+  w[3] = w[1] + d2;
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
-    uint32_t t = 0u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) t = max(t, f2u(x[u][k]) & 0x7fffffffu);
-    w[u] = lanes_max(t, lgB < 8 ? 1 << (lgB - 2) : 64);
+  for (int k = 0; k < 4; ++k) {
+    w[k] ^= w[k] >> 15;
+    w[k] *= 0x3B67AE85u;
+    w[k] ^= w[k] >> 16;
   }
-  if (lgB >= 9) {
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kRor4 = 0x124, kRor8 = 0x128;  // lanes of a quad, of 16
+
+// The largest magnitude of the blocks (2^lgB elements, 32 to 1,024) that a lane's elements
+// of the 4 steps are in: lane l gets that of step l % 4.  The 4 maxima are reduced side by
+// side: each exchange between lanes halves what a lane still has to carry.
+__device__ __forceinline__ float block_max(const float (&x)[kSteps][4], int lgB) {
+  static_assert(kSteps == 4, "a step for each lane of a quad");
+  uint32_t w[4];
 #pragma unroll
-    for (int u = 0; u < kSteps; u += 2) w[u] = w[u + 1] = max(w[u], w[u + 1]);
+  for (int u = 0; u < 4; ++u)
+    w[u] = f2u(fmaxf(fmaxf(fabsf(x[u][0]), fabsf(x[u][1])), fmaxf(fabsf(x[u][2]), fabsf(x[u][3]))));
+  const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+  const uint32_t a = max(odd ? w[1] : w[0], dpp<kSwap1>(odd ? w[0] : w[1]));
+  const uint32_t b = max(odd ? w[3] : w[2], dpp<kSwap1>(odd ? w[2] : w[3]));
+  uint32_t v = max(high ? b : a, dpp<kSwap2>(high ? a : b));
+  if (lgB == 5) return u2f(max(v, (uint32_t)__shfl_xor((int)v, 4, 64)));  // 8 lanes
+  v = max(v, dpp<kRor4>(v));
+  v = max(v, dpp<kRor8>(v));
+  if (lgB >= 7) {
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(s[0], s[1]);
   }
-  if (lgB >= 10) {
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) w[u] = max(w[0], w[2]);
+  if (lgB >= 8) {
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = max(s[0], s[1]);
   }
-#pragma unroll
-  for (int u = 0; u < kSteps; ++u) a[u] = u2f(w[u]);
+  if (lgB >= 9) v = max(v, dpp<kSwap1>(v));
+  if (lgB >= 10) v = max(v, dpp<kSwap2>(v));
+  return u2f(v);
+}
+// what lane l has of step l % 4, for each step
+__device__ __forceinline__ void of_steps(float v, float (&all)[4]) {
+  all[0] = u2f(dpp<0x00>(f2u(v)));
+  all[1] = u2f(dpp<0x55>(f2u(v)));
+  all[2] = u2f(dpp<0xAA>(f2u(v)));
+  all[3] = u2f(dpp<0xFF>(f2u(v)));
+}
+// The scales of a wave's blocks, from lanes that have them as block_max does.  e0: the
+// wave's first element.
+template <bool FULL>
+__device__ __forceinline__ void store_scales(float* scales, float s, int lgB, int64_t e0, int64_t n) {
+  const int lane = threadIdx.x & 63, lanes = lgB < 8 ? 1 << (lgB - 2) : 64;
+  const int step = lane & 3;
+  if ((lane & (lanes - 1)) >= 4 || (lgB > 8 && (step & ((1 << (lgB - 8)) - 1)) != 0)) return;
+  const int64_t block = (e0 + step * 256 + lane * 4) >> lgB;
+  if (FULL || block << lgB < n) scales[block] = s;
 }
 
 // ---------------------------------------------------------------- loads and stores of 4 elements
@@ -234,42 +294,43 @@ __device__ __forceinline__ uint32_t load_int4(const char* base, int64_t i, int64
   return n > i && ((n - i) & 1) ? w & ((1u << (4 * (n - i))) - 1u) : w;
 }
 
-// writes x as 8-bit floats and their blocks' scales
+// Writes x as 8-bit floats and their blocks' scales.  a / top is a / 7 times a power of two,
+// which is a binary32 number or further than 2^-29 of it from the middle of two, so its
+// product with 1 / top in binary64, rounded, is the rounded quotient.
 template <bool SIGNED, bool FULL>
 __device__ __forceinline__ void store_state8(const float (&x)[kSteps][4], const uint32_t (&drawn)[kSteps][4], char* codes,
                                              float* scales, int lgB, int64_t i0, int64_t n) {
-  float a[kSteps];
-  block_max(x, lgB, a);
+  const float a = block_max(x, lgB);
+  const bool fits = a >= 0x1p-110f;
+  store_scales<FULL>(scales, fits ? (float)((double)a * (1.0 / F8<SIGNED>::top)) : 0.0f, lgB,
+                     i0 - (threadIdx.x & 63) * 4, n);
+  float r[kSteps];
+  of_steps(fits ? F8<SIGNED>::top / a : 0.0f, r);
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
-    const int64_t i = i0 + u * 256;
-    const bool fits = a[u] >= 0x1p-110f;
-    const float s = fits ? a[u] / F8<SIGNED>::top : 0.0f, r = fits ? F8<SIGNED>::top / a[u] : 0.0f;
-    uint32_t w = 0u;
+    uint32_t t[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      w |= F8<SIGNED>::code(x[u][k], r, SIGNED ? drawn[u][k] & 0xffffu : drawn[u][k] >> 16) << (8 * k);
-    store4b<FULL>(codes, i, n, w);
-    if ((i & ((1 << lgB) - 1)) == 0 && (FULL || i < n)) scales[i >> lgB] = s;
+    for (int k = 0; k < 4; ++k) t[k] = code_on_top<SIGNED>(x[u][k], r[u], drawn[u][k]);
+    store4b<FULL>(codes, i0 + u * 256, n, pack_top(t));
   }
 }
 
-// writes x as INT8 codes and scales, as the weights' quantiser does
+// Writes x as INT8 codes and scales, as the weights' quantiser does: a code is in the low
+// byte of x r + 1.5 * 2^23, a / 127 as above.
 template <bool FULL>
 __device__ __forceinline__ void store_int8(const float (&x)[kSteps][4], char* codes, float* scales, int lgB, int64_t i0,
                                            int64_t n) {
-  float a[kSteps];
-  block_max(x, lgB, a);
+  const float a = block_max(x, lgB);
+  const bool fits = a >= 0x1p-119f;
+  store_scales<FULL>(scales, fits ? (float)((double)a * (1.0 / 127.0)) : 0.0f, lgB, i0 - (threadIdx.x & 63) * 4, n);
+  float r[kSteps];
+  of_steps(fits ? 127.0f / a : 0.0f, r);
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
-    const int64_t i = i0 + u * 256;
-    const bool fits = a[u] >= 0x1p-119f;
-    const float s = fits ? a[u] / 127.0f : 0.0f, r = fits ? 127.0f / a[u] : 0.0f;
-    uint32_t w = 0u;
+    uint32_t t[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w |= ((uint32_t)(int)rintf(x[u][k] * r) & 0xffu) << (8 * k);
-    store4b<FULL>(codes, i, n, w);
-    if ((i & ((1 << lgB) - 1)) == 0 && (FULL || i < n)) scales[i >> lgB] = s;
+    for (int k = 0; k < 4; ++k) t[k] = f2u(x[u][k] * r[u] + 12582912.0f);
+    store4b<FULL>(codes, i0 + u * 256, n, pack_low(t));
   }
 }
 
@@ -301,8 +362,7 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
       load4<ZQ_F32, FULL>(en.v, i, n, vw[u]);
     }
   }
-  const double lr = c.lr * en.lr_scale;
-  const float alpha = (float)(lr / c.bias1), decay = (float)(1.0 - lr * en.decay);
+  const float alpha = (float)(c.rate * en.lr_scale), decay = (float)(1.0 - c.lr * en.lr_scale * en.decay);
 
   float p[kSteps][4], m[kSteps][4], v[kSteps][4];
 #pragma unroll
@@ -318,18 +378,20 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
 #pragma unroll
       for (int k = 0; k < 4; ++k) g[k] = g[k] * clip;
     }
+    float m0[4], v0[4];
+    if constexpr (S8) {
+      decode8<true>(mw[u][0], m0);
+      decode8<false>(vw[u][0], v0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m0[k] = m0[k] * ms[u], v0[k] = v0[k] * vs[u];
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m0[k] = u2f(mw[u][k]), v0[k] = u2f(vw[u][k]);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      float m0, v0;
-      if constexpr (S8) {
-        m0 = F8<true>::value(mw[u][0] >> (8 * k) & 0xffu) * ms[u];
-        v0 = F8<false>::value(vw[u][0] >> (8 * k) & 0xffu) * vs[u];
-      } else {
-        m0 = u2f(mw[u][k]);
-        v0 = u2f(vw[u][k]);
-      }
-      m[u][k] = m0 * c.b1 + g[k] * c.om1;
-      v[u][k] = v0 * c.b2 + (g[k] * g[k]) * c.om2;
+      m[u][k] = m0[k] * c.b1 + g[k] * c.om1;
+      v[u][k] = v0[k] * c.b2 + (g[k] * g[k]) * c.om2;
       const float d = sqrtf(v[u][k]) * c.root + c.eps;
       p[u][k] = p[u][k] * decay - (m[u][k] / d) * alpha;
     }
@@ -349,10 +411,7 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
     if ((i0 >> 32) != 0) key = mix(key + (uint32_t)(i0 >> 32));  // the same for a piece
     uint32_t drawn[kSteps][4];
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) drawn[u][k] = mix(key ^ ((uint32_t)i0 + (uint32_t)(u * 256 + k)));
-    }
+    for (int u = 0; u < kSteps; ++u) draw4(key, (uint32_t)i0 + (uint32_t)(u * 256), drawn[u]);
     store_state8<true, FULL>(m, drawn, en.m, en.ms, en.lgS, i0, n);
     store_state8<false, FULL>(v, drawn, en.v, en.vs, en.lgS, i0, n);
   }

@@ -58,7 +58,7 @@ template <int DT>
 __device__ __forceinline__ void load_vec(const char* row, int i, int n, uint32_t (&w)[4]) {
   constexpr int E = per_vec<DT>();
   if (i + E <= n) {
-    load_words_any<true>(row + (uint32_t)i * dt_size<DT>(), w);
+    load_words_any<false>(row + (uint32_t)i * dt_size<DT>(), w);
     return;
   }
   constexpr uint32_t none = DT == ZQ_F32 ? 0xff800000u : DT == ZQ_BF16 ? 0xff80ff80u : 0xfc00fc00u;
@@ -326,7 +326,21 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : 8) k_loss(unsigned first, Loss
 __global__ void __launch_bounds__(1024) k_loss_sums(const double* __restrict__ rows, int64_t T, float* __restrict__ sums) {
   __shared__ double part[16][4];
   double s[4] = {0.0, 0.0, 0.0, 0.0};
-  for (int64_t t = threadIdx.x; t < T; t += 1024) {
+  int64_t t = threadIdx.x;
+  for (; t + 3 * 1024 < T; t += 4 * 1024) {  // 4 rows' loads in flight
+    double v[4][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[u][k] = rows[4 * (t + 1024 * u) + k];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k] += v[u][k];
+    }
+  }
+  for (; t < T; t += 1024) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) s[k] += rows[4 * t + k];
   }
