@@ -762,6 +762,13 @@ def _here(**tensors):
             raise ValueError(f"{name} is on {t.device}, the current device is cuda:{now}")
 
 
+def _elements(dtype, name):
+    """A type of elements that a call is to allocate."""
+    if dtype not in _TORCH_DT:
+        raise TypeError(f"{name} is {dtype}; expected one of {[str(d) for d in _ELEM]}")
+    return dtype
+
+
 def _rows(x, name="x"):
     """(rows, row length) of a tensor whose last dimension is normed."""
     if x.dim() < 1 or x.shape[-1] < 1:
@@ -789,22 +796,29 @@ def _weight(weight, D):
     return at or _dev(weight, "weight"), _TORCH_DT[weight.dtype]
 
 
-def _rms_args(x, weight, residual, hidden, rstd, stream):
+def _rms_args(x, weight, residual, hidden, rstd, out, stream):
+    """What both kinds of norm take, checked; what the call allocates itself is not."""
     T, D = _rows(x)
     x_at = _ptr(x, "x", T * D, _ELEM) or _dev(x, "x")
     w_at, wt = _weight(weight, D)
-    res_at = _like(residual, "residual", x, (x.dtype,))
+    _here(x=x, weight=weight, residual=residual, hidden=hidden, rstd=rstd, out=out)
+    res_at = h_at = None
     if residual is None:
         if hidden is not None:
             raise ValueError("hidden receives x + residual: give the residual")
         hidden = x
-    elif hidden is None:
-        hidden = _output(stream, x.device, x.dtype, *x.shape)
-    h_at = _like(hidden, "hidden", x, (x.dtype,)) if residual is not None else None
+    else:
+        res_at = _like(residual, "residual", x, (x.dtype,))
+        if hidden is None:
+            hidden = _output(stream, x.device, x.dtype, *x.shape)
+            h_at = hidden.data_ptr()
+        else:
+            h_at = _like(hidden, "hidden", x, (x.dtype,))
     if rstd is None:
         rstd = _output(stream, x.device, torch.float32, T)
-    r_at = _ptr(rstd, "rstd", T, _F32) or _dev(rstd, "rstd")
-    _here(x=x, weight=weight, residual=residual, hidden=hidden, rstd=rstd)
+        r_at = rstd.data_ptr()
+    else:
+        r_at = _ptr(rstd, "rstd", T, _F32) or _dev(rstd, "rstd")
     return T, D, x_at, w_at, wt, res_at, hidden, h_at, rstd, r_at
 
 
@@ -815,11 +829,12 @@ def rms_norm(x, weight, residual=None, eps=1e-6, out_dtype=None, out=None, hidde
     bf16 [..., D], residual of its type and shape, weight f32 / f16 / bf16 [D] or None
     (ones); y of out_dtype (x's if not given).  out, hidden, rstd: where y, h and rstd go;
     hidden may be residual or x itself.  h and rstd are what rms_norm_grad takes."""
-    T, D, x_at, w_at, wt, res_at, h, h_at, rstd, r_at = _rms_args(x, weight, residual, hidden, rstd, stream)
+    T, D, x_at, w_at, wt, res_at, h, h_at, rstd, r_at = _rms_args(x, weight, residual, hidden, rstd, out, stream)
     if out is None:
-        out = _output(stream, x.device, out_dtype or x.dtype, *x.shape)
-    y_at = _like(out, "out", x, _ELEM)
-    _here(out=out)
+        out = _output(stream, x.device, _elements(out_dtype or x.dtype, "out_dtype"), *x.shape)
+        y_at = out.data_ptr()
+    else:
+        y_at = _like(out, "out", x, _ELEM)
     _check(lib().zq_rms_norm(x_at, res_at, _TORCH_DT[x.dtype], w_at, wt, T, D, eps, h_at, y_at, _TORCH_DT[out.dtype],
                              r_at, _stream(stream)), "rms_norm")
     return out, h, rstd
@@ -830,15 +845,18 @@ def qwz_rms_norm(x, weight, residual=None, eps=1e-6, block=256, codes=None, scal
     """rms_norm with its output in the INT8 format: (codes, scales, h, rstd), codes int8 of
     x's shape and scales [numel / block], what qwz_quantize gives for the unrounded y.  D
     must be a multiple of block."""
-    T, D, x_at, w_at, wt, res_at, h, h_at, rstd, r_at = _rms_args(x, weight, residual, hidden, rstd, stream)
+    T, D, x_at, w_at, wt, res_at, h, h_at, rstd, r_at = _rms_args(x, weight, residual, hidden, rstd, codes, stream)
     if codes is None:
         codes = _output(stream, x.device, torch.int8, *x.shape)
+        c_at = codes.data_ptr()
+    else:
+        c_at = _ptr(codes, "codes", T * D, _I8) or _dev(codes, "codes")
     if scales is None:
         scales = _output(stream, x.device, torch.float32, _alloc_nsc(T * D, block))
-    c_at = _ptr(codes, "codes", T * D, _I8)
-    s_at = _ptr(scales, "scales", _nsc(T * D, block), _F32)
-    c_at, s_at = c_at or _dev(codes, "codes"), s_at or _dev(scales, "scales")
-    _here(codes=codes, scales=scales)
+        s_at = scales.data_ptr()
+    else:
+        s_at = _ptr(scales, "scales", _nsc(T * D, block), _F32) or _dev(scales, "scales")
+        _here(scales=scales)
     _check(lib().qwz_rms_norm(x_at, res_at, _TORCH_DT[x.dtype], w_at, wt, T, D, eps, h_at, c_at, s_at, block, r_at,
                               _stream(stream)), "qwz_rms_norm")
     return codes, scales, h, rstd
@@ -865,18 +883,22 @@ def rms_norm_grad(dy, h, weight, rstd, dh=None, out=None, dweight=None, accumula
     w_at, wt = _weight(weight, D)
     r_at = _ptr(rstd, "rstd", T, _F32)
     dh_at = _like(dh, "dh", h, (h.dtype,))
+    h_at, r_at = h_at or _dev(h, "h"), r_at or _dev(rstd, "rstd")
+    _here(h=h, dy=dy, weight=weight, rstd=rstd, dh=dh, out=out, dweight=dweight, workspace=workspace)
     if out is None:
         out = _output(stream, h.device, h.dtype, *h.shape)
-    out_at = _like(out, "out", h, (h.dtype,))
+        out_at = out.data_ptr()
+    else:
+        out_at = _like(out, "out", h, (h.dtype,))
     if dweight is None:
         if accumulate:
             raise ValueError("accumulate adds to dweight: give it")
         dweight = _output(stream, h.device, torch.float32, D)
-    dw_at = _ptr(dweight, "dweight", D, _ELEM)
-    if dweight.numel() != D:
-        raise ValueError(f"dweight holds {dweight.numel()} elements; rows have {D}")
-    h_at, r_at, dw_at = h_at or _dev(h, "h"), r_at or _dev(rstd, "rstd"), dw_at or _dev(dweight, "dweight")
-    _here(h=h, dy=dy, weight=weight, rstd=rstd, dh=dh, out=out, dweight=dweight, workspace=workspace)
+        dw_at = dweight.data_ptr()
+    else:
+        dw_at = _ptr(dweight, "dweight", D, _ELEM) or _dev(dweight, "dweight")
+        if dweight.numel() != D:
+            raise ValueError(f"dweight holds {dweight.numel()} elements; rows have {D}")
     ws_at, ws_size = _given_workspace(workspace, rms_norm_grad_bytes(T, D), h.device, stream)
     _check(lib().zq_rms_norm_grad(dy_at, _TORCH_DT[dy.dtype], h_at, _TORCH_DT[h.dtype], w_at, wt, r_at, dh_at, T, D,
                                   out_at, int(bool(accumulate)), dw_at, _TORCH_DT[dweight.dtype], ws_at, ws_size,
@@ -926,10 +948,12 @@ def token_logp(logits, ids, scale=1.0, out=None, stream=None):
     [0, V) gives 0."""
     l_at, T, V, ld = _logits(logits, "logits", _ELEM)
     ids_at = _token_ids(ids, T)
+    _here(logits=logits, ids=ids, out=out)
     if out is None:
         out = _output(stream, logits.device, torch.float32, *ids.shape)
-    out_at = _per_row(out, "out", T)
-    _here(logits=logits, ids=ids, out=out)
+        out_at = out.data_ptr()
+    else:
+        out_at = _per_row(out, "out", T)
     _check(lib().zq_token_logp(l_at, _TORCH_DT[logits.dtype], T, V, ld, ids_at, _ID_DT[ids.dtype], scale, out_at,
                                _stream(stream)), "token_logp")
     return out
@@ -964,23 +988,27 @@ def policy_loss(logits, ids, old_logp, advantages, weights=None, ref_logp=None, 
                 _per_row(weights, "weights", T), _per_row(ref_logp, "ref_logp", T), clip[0], clip[1], kl, scale,
                 grad_scale, 0)
     g_at, gt, ldg = None, ZQ_F32, V
-    if grad is True:
-        grad = _output(stream, logits.device, grad_dtype or logits.dtype, *logits.shape)
-    if grad is False or grad is None:
-        grad = None
-    else:
+    given = grad if isinstance(grad, torch.Tensor) else None
+    _here(logits=logits, ids=ids, old_logp=old_logp, advantages=advantages, weights=weights, ref_logp=ref_logp,
+          grad=given, logp=logp, workspace=workspace)
+    if given is not None:
         g_at, _, gV, ldg = _logits(grad, "grad", _ELEM, T)
         if gV != V:
             raise ValueError(f"grad has rows of {gV}; logits of {V}")
         gt = _TORCH_DT[grad.dtype]
+    elif grad:
+        grad = _output(stream, logits.device, _elements(grad_dtype or logits.dtype, "grad_dtype"), *logits.shape)
+        g_at, gt = grad.data_ptr(), _TORCH_DT[grad.dtype]
+    else:
+        grad = None
     sums = _output(stream, logits.device, torch.float32, 4)
     if logp is None:
         logp = _output(stream, logits.device, torch.float32, *ids.shape)
-    logp_at = _per_row(logp, "logp", T)
-    _here(logits=logits, ids=ids, old_logp=old_logp, advantages=advantages, weights=weights, ref_logp=ref_logp,
-          grad=grad, logp=logp, workspace=workspace)
+        logp_at = logp.data_ptr()
+    else:
+        logp_at = _per_row(logp, "logp", T)
     ws_at, ws_size = _given_workspace(workspace, policy_loss_bytes(T), logits.device, stream)
     _check(lib().zq_policy_loss(l_at, _TORCH_DT[logits.dtype], T, V, ld, ids_at, _ID_DT[ids.dtype], ctypes.byref(p),
-                                _dev(sums, "sums"), logp_at, g_at, gt, ldg, ws_at, ws_size,
+                                sums.data_ptr(), logp_at, g_at, gt, ldg, ws_at, ws_size,
                                 _stream(stream)), "policy_loss")
     return sums, logp, grad

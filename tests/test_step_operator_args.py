@@ -271,6 +271,8 @@ def test_binding_of_the_norm(monkeypatch):
             call(residual=gpu(torch.zeros(64, 4)))
         with pytest.raises(ValueError, match="rstd"):
             call(rstd=gpu(torch.zeros(3)))
+    with pytest.raises(TypeError, match="out_dtype"):
+        zq.rms_norm(x, w, out_dtype=torch.float64, rstd=gpu(torch.zeros(4)))
     with pytest.raises(ValueError, match="weight"):
         zq.rms_norm(x, gpu(torch.ones(65)))
     with pytest.raises(ValueError, match="shape"):
@@ -373,6 +375,8 @@ def test_binding_of_rows(monkeypatch):
         zq.policy_loss(z, ids, row, row, gpu(torch.zeros(3)))
     with pytest.raises(TypeError, match="ref_logp"):
         zq.policy_loss(z, ids, row, row, None, row.double(), kl=0.1)
+    with pytest.raises(TypeError, match="grad_dtype"):
+        zq.policy_loss(z, ids, row, row, grad_dtype=torch.int8)
     with pytest.raises(ValueError, match="grad"):
         zq.policy_loss(z, ids, row, row, grad=gpu(torch.zeros(4, 8)))
     with pytest.raises(ValueError, match="grad"):
