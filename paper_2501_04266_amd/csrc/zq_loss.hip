@@ -53,17 +53,30 @@ struct Loss {
 template <int DT>
 constexpr int per_vec() { return 16 / dt_size<DT>(); }
 
-// a 16-byte vector of logits from element i of n; -infinity behind the end
+// A 16-byte vector of logits from element i of n; -infinity behind the end.  A row's last,
+// partial vector is read as the 16 bytes up to its end and moved down.
 template <int DT>
 __device__ __forceinline__ void load_vec(const char* row, int i, int n, uint32_t (&w)[4]) {
-  constexpr int E = per_vec<DT>();
-  if (i + E <= n) {
-    load_words_any<false>(row + (uint32_t)i * dt_size<DT>(), w);
-    return;
-  }
+  constexpr int E = per_vec<DT>(), S = dt_size<DT>();
   constexpr uint32_t none = DT == ZQ_F32 ? 0xff800000u : DT == ZQ_BF16 ? 0xff80ff80u : 0xfc00fc00u;
 #pragma unroll
   for (int k = 0; k < 4; ++k) w[k] = none;
+  if (n >= E) {
+    const int at = min(i, n - E);
+    if (i < n) load_words_any<false>(row + (uint32_t)at * S, w);
+    if (i == at || i >= n) return;
+    const int words = (i - at) * S / 4;
+#pragma unroll
+    for (int b = 2; b >= 1; b /= 2) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = words & b ? (k + b < 4 ? w[k + b] : none) : w[k];
+    }
+    if (S == 2 && (i - at) & 1) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = w[k] >> 16 | (k + 1 < 4 ? w[k + 1] : none) << 16;
+    }
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < E - 1; ++k) {
     if (i + k >= n) continue;

@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "zq.h"
@@ -28,70 +29,81 @@ namespace {
 
 constexpr int kInt8 = 3;  // y's type code beside ZQ_F32 / ZQ_F16 / ZQ_BF16
 constexpr int64_t kMaxWidth = 1 << 24;
+constexpr int64_t kUnits = 256;  // CUs of the chip
 
 // ---------------------------------------------------------------- rows
 
-// Places in a row are 32-bit numbers of bytes: rows have up to 2^24 elements.  WHOLE: D is
-// a multiple of 8, so a vector of 8 elements is in the row or behind it.
+// Places in a row are 32-bit numbers of bytes: rows have up to 2^24 elements.  Threads hold
+// vectors of 8 elements of the first D - D % 8; the row's last D % 8 are held one each by its
+// first threads, so that no vector needs moving or splitting (a partial vector's words moved
+// into place cost the gradient of 16,384 x 2,056 twice its time: the wave waited for them).
 
 // Which accesses pass the caches by, measured in turns on 16,384 x 6,144 of bf16: the norm
 // 143 us with its stores past them, 156 with its loads too, 151 with neither; its gradient
-// 134 with its loads past them, 143 with its stores too, 158 with neither.
-constexpr bool kNormLoadsPast = false, kNormStoresPast = true;
-constexpr bool kGradLoadsPast = true, kGradStoresPast = false;
+// 134 with its loads past them, 143 with its stores too, 158 with neither.  The gradient's
+// loads pass them by only where rows are whole cache lines: else two rows share a line
+// (5,003 rows of 2,051 of fp16: 39 and 32 us).
+constexpr bool kNormLoadsPast = false, kNormStoresPast = true, kGradStoresPast = false;
 
-// the words of 8 elements from element i of n; zeros behind the end
-template <int DT, bool WHOLE, bool PAST>
+// the words of 8 elements from element i on; zeros from element n on, a multiple of 8
+template <int DT, bool PAST>
 __device__ __forceinline__ void load8(const char* row, int i, int n, uint32_t (&w)[2 * dt_size<DT>()]) {
-  constexpr int S = dt_size<DT>();
 #pragma unroll
-  for (int k = 0; k < 2 * S; ++k) w[k] = 0u;
-  if (WHOLE ? i < n : i + 8 <= n) {
-    load_words_any<PAST>(row + (uint32_t)i * S, w);
-  } else if (!WHOLE && i < n) {
-#pragma unroll
-    for (int k = 0; k < 7; ++k) {
-      if (i + k >= n) continue;
-      if constexpr (S == 4) w[k] = *reinterpret_cast<const uint32_t*>(row + (uint32_t)(i + k) * 4);
-      else w[k / 2] |= (uint32_t) * reinterpret_cast<const uint16_t*>(row + (uint32_t)(i + k) * 2) << (16 * (k & 1));
-    }
-  }
+  for (int k = 0; k < 2 * dt_size<DT>(); ++k) w[k] = 0u;
+  if (i < n) load_words_any<PAST>(row + (uint32_t)i * dt_size<DT>(), w);
 }
 // of a type that is known when the kernel runs: in the first 4 or in all 8 words
-template <bool WHOLE, bool PAST>
+template <bool PAST>
 __device__ __forceinline__ void load8(int dt, const char* row, int i, int n, uint32_t (&w)[8]) {
   if (dt == ZQ_F32) {
-    load8<ZQ_F32, WHOLE, PAST>(row, i, n, w);
+    load8<ZQ_F32, PAST>(row, i, n, w);
     return;
   }
   uint32_t t[4];
-  load8<ZQ_BF16, WHOLE, PAST>(row, i, n, t);
+  load8<ZQ_BF16, PAST>(row, i, n, t);
 #pragma unroll
   for (int k = 0; k < 4; ++k) w[k] = t[k], w[k + 4] = 0u;
+}
+// one element
+template <int DT>
+__device__ __forceinline__ float load1(const char* row, int i) {
+  float v[1];
+  load_elems<DT, 1>(row + (uint32_t)i * dt_size<DT>(), 0, v);
+  return v[0];
+}
+__device__ __forceinline__ float load1(int dt, const char* row, int i) {
+  return dt == ZQ_F32 ? load1<ZQ_F32>(row, i) : dt == ZQ_BF16 ? load1<ZQ_BF16>(row, i) : load1<ZQ_F16>(row, i);
+}
+template <int DT>
+__device__ __forceinline__ void store1(char* row, int i, float v) {
+  const float t[1] = {v};
+  store_elems<DT, 1>(row + (uint32_t)i * dt_size<DT>(), 0, t);
+}
+__device__ __forceinline__ void store1(int dt, char* row, int i, float v) {
+  if (dt == ZQ_F32) store1<ZQ_F32>(row, i, v);
+  else if (dt == ZQ_BF16) store1<ZQ_BF16>(row, i, v);
+  else store1<ZQ_F16>(row, i, v);
 }
 __device__ __forceinline__ void widen8(int dt, const uint32_t (&w)[8], float (&v)[8]) {
   if (dt == ZQ_F32) widen<ZQ_F32>(w, v);
   else if (dt == ZQ_BF16) widen<ZQ_BF16>(w, v);
   else widen<ZQ_F16>(w, v);
 }
-template <int DT, bool WHOLE, bool PAST>
+template <int DT, bool PAST>
 __device__ __forceinline__ void store8(char* row, int i, int n, const float (&v)[8]) {
-  constexpr int S = dt_size<DT>();
-  if (WHOLE ? i < n : i + 8 <= n) {
-    store_elems<DT, 8, PAST>(row + (uint32_t)i * S, 0, v);
-  } else if (!WHOLE && i < n) {
-#pragma unroll
-    for (int k = 0; k < 7; ++k) {
-      const float t[1] = {v[k]};
-      if (i + k < n) store_elems<DT, 1>(row + (uint32_t)(i + k) * S, 0, t);
-    }
-  }
+  if (i < n) store_elems<DT, 8, PAST>(row + (uint32_t)i * dt_size<DT>(), 0, v);
 }
-template <bool WHOLE, bool PAST>
+template <bool PAST>
 __device__ __forceinline__ void store8(int dt, char* row, int i, int n, const float (&v)[8]) {
-  if (dt == ZQ_F32) store8<ZQ_F32, WHOLE, PAST>(row, i, n, v);
-  else if (dt == ZQ_BF16) store8<ZQ_BF16, WHOLE, PAST>(row, i, n, v);
-  else store8<ZQ_F16, WHOLE, PAST>(row, i, n, v);
+  if (dt == ZQ_F32) store8<ZQ_F32, PAST>(row, i, n, v);
+  else if (dt == ZQ_BF16) store8<ZQ_BF16, PAST>(row, i, n, v);
+  else store8<ZQ_F16, PAST>(row, i, n, v);
+}
+template <int DT>
+__device__ __forceinline__ float as_stored(float v) {
+  if constexpr (DT == ZQ_BF16) return u2f(bf16x2_bits(v, 0.0f) << 16);
+  else if constexpr (DT == ZQ_F16) return h2f(f2h(v));
+  else return v;
 }
 // the words of 8 values as a type holds them
 template <int DT>
@@ -115,17 +127,35 @@ constexpr int kind_bytes(int dt) { return dt == ZQ_F32 ? 4 : 2; }
 
 // ---------------------------------------------------------------- sums over a row's threads
 
-template <typename F>
-__device__ __forceinline__ F wave_sum(F v) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) {
+  return u2f((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f2u(v), CTRL, 0xF, 0xF, false));
+}
+template <int CTRL>
+__device__ __forceinline__ double from_lane(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// the sum over R lanes, 16 to 64, in all of them: within rows of 16 lanes through the ALUs
+// (a shuffle through LDS takes ten times as long), each lane from its mirror image
+template <int R, typename F>
+__device__ __forceinline__ F lanes_sum(F v) {
+  v += from_lane<0xB1>(v);   // quad_perm 1,0,3,2
+  v += from_lane<0x4E>(v);   // quad_perm 2,3,0,1
+  v += from_lane<0x141>(v);  // row_half_mirror
+  v += from_lane<0x140>(v);  // row_mirror
+  if constexpr (R >= 32) v += __shfl_xor(v, 16);
+  if constexpr (R >= 64) v += __shfl_xor(v, 32);
   return v;
 }
 // the sum over a row's R threads, in all of them; `slot`: R / 64 values of LDS, written
 // again only after a barrier
 template <int R, typename F>
 __device__ __forceinline__ F row_sum(F v, F* slot) {
-  v = wave_sum(v);
-  if constexpr (R == 64) return v;
+  if constexpr (R <= 64) return lanes_sum<R>(v);
+  v = lanes_sum<64>(v);
   if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
   __syncthreads();
   F s = slot[0];
@@ -188,10 +218,11 @@ __device__ __forceinline__ void put_int8(const Norm& a, int64_t at, int i, const
 // NV vectors of 8 elements a thread; NV = 0: rows of any length, h read again.
 // Everything a row needs is loaded before the first store: loads would wait behind stores
 // that might be to their memory.
-template <int XT, int R, int NV, bool WHOLE>
+template <int XT, int R, int NV>
 __device__ __forceinline__ void norm_row(const Norm& a, int64_t t, int lane, double* slot, uint32_t* half) {
   constexpr int W = 2 * dt_size<XT>(), N = NV > 0 ? NV : 1;
-  const int D = (int)a.D;
+  const int D = (int)a.D & ~7, last = D + lane;  // vectors up to D, then one element a thread
+  const bool has_last = last < (int)a.D;
   const int64_t at = t * a.D;  // the row's first element
   const char* x = static_cast<const char*>(a.x) + at * dt_size<XT>();
   const char* res = a.residual ? static_cast<const char*>(a.residual) + at * dt_size<XT>() : nullptr;
@@ -201,9 +232,16 @@ __device__ __forceinline__ void norm_row(const Norm& a, int64_t t, int lane, dou
 
   double sum = 0.0;
   uint32_t xw[N][W], rw[N][W], ww[N][8];
+  float x1 = 0.0f, r1 = 0.0f, w1 = 1.0f;
   auto load = [&](int j, int i) {
-    load8<XT, WHOLE, kNormLoadsPast>(x, i, D, xw[j]);
-    if (res) load8<XT, WHOLE, kNormLoadsPast>(res, i, D, rw[j]);
+    load8<XT, kNormLoadsPast>(x, i, D, xw[j]);
+    if (res) load8<XT, kNormLoadsPast>(res, i, D, rw[j]);
+  };
+  auto load_last = [&]() {
+    if (!has_last) return;
+    x1 = load1<XT>(x, last);
+    if (res) r1 = load1<XT>(res, last);
+    if (weight) w1 = load1(a.wt, weight, last);
   };
   auto add = [&](int j, int i) {  // xw becomes h's words
     float v[8];
@@ -215,11 +253,19 @@ __device__ __forceinline__ void norm_row(const Norm& a, int64_t t, int lane, dou
       for (int k = 0; k < 8; ++k) v[k] = v[k] + b[k];
       narrow8<XT>(v, xw[j]);
       widen<XT>(xw[j], v);
-      store8<XT, WHOLE, kNormStoresPast>(h, i, D, v);
+      store8<XT, kNormStoresPast>(h, i, D, v);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum = __builtin_fma((double)v[k], (double)v[k], sum);
     forget(xw[j]);
+  };
+  auto add_last = [&]() {  // x1 becomes h's element
+    if (!has_last) return;
+    if (res) {
+      x1 = as_stored<XT>(x1 + r1);
+      store1<XT>(h, last, x1);
+    }
+    sum = __builtin_fma((double)x1, (double)x1, sum);
   };
   auto put = [&](int j, int i, float rstd) {
     float v[8], w[8];
@@ -232,12 +278,13 @@ __device__ __forceinline__ void norm_row(const Norm& a, int64_t t, int lane, dou
       for (int k = 0; k < 8; ++k) v[k] = v[k] * w[k];
     }
     if (a.yt == kInt8) put_int8<R>(a, at, i, v, half);
-    else store8<WHOLE, kNormStoresPast>(a.yt, y, i, D, v);
+    else store8<kNormStoresPast>(a.yt, y, i, D, v);
   };
   auto finish = [&]() {
     sum = row_sum<R>(sum, slot);
     const float rstd = (float)(1.0 / sqrt(sum / (double)a.D + a.eps));
     if (a.rstd && lane == 0) a.rstd[t] = rstd;
+    if (has_last) store1(a.yt, y, last, weight ? (x1 * rstd) * w1 : x1 * rstd);
     return rstd;
   };
 
@@ -246,38 +293,41 @@ __device__ __forceinline__ void norm_row(const Norm& a, int64_t t, int lane, dou
     for (int j = 0; j < NV; ++j) load(j, (j * R + lane) * 8);
     if (weight) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) load8<WHOLE, false>(a.wt, weight, (j * R + lane) * 8, D, ww[j]);
+      for (int j = 0; j < NV; ++j) load8<false>(a.wt, weight, (j * R + lane) * 8, D, ww[j]);
     }
+    load_last();
 #pragma unroll
     for (int j = 0; j < NV; ++j) add(j, (j * R + lane) * 8);
+    add_last();
     const float rstd = finish();
 #pragma unroll
     for (int j = 0; j < NV; ++j) put(j, (j * R + lane) * 8, rstd);
   } else {
     const int end = (D + 8 * R - 1) / (8 * R) * (8 * R);  // all threads take every turn
+    load_last();
     for (int i = lane * 8; i < end; i += 8 * R) {
       load(0, i);
       add(0, i);
     }
+    add_last();
     const float rstd = finish();
     for (int i = lane * 8; i < end; i += 8 * R) {
-      load8<XT, WHOLE, kNormLoadsPast>(res ? h : x, i, D, xw[0]);  // h: this thread's own writes
-      if (weight) load8<WHOLE, false>(a.wt, weight, i, D, ww[0]);
+      load8<XT, kNormLoadsPast>(res ? h : x, i, D, xw[0]);  // h: this thread's own writes
+      if (weight) load8<false>(a.wt, weight, i, D, ww[0]);
       put(0, i, rstd);
     }
   }
 }
 
 template <int XT, int R, int NV>
-__global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms(unsigned first, Norm a) {
-  constexpr int THREADS = R < 256 ? 256 : R;
-  __shared__ double slot[R / 64];
-  __shared__ uint32_t half[R / 64];
+__global__ void __launch_bounds__(R <= 64 ? 256 : R) k_rms(unsigned first, Norm a) {
+  constexpr int THREADS = R <= 64 ? 256 : R;
+  __shared__ double slot[(R + 63) / 64];
+  __shared__ uint32_t half[(R + 63) / 64];
   const int lane = threadIdx.x % R;
   const int64_t t = (int64_t)(first + blockIdx.x) * (THREADS / R) + threadIdx.x / R;
-  if (R == 64 && t >= a.T) return;  // a wave's own row: the others go on
-  if (a.D % 8 == 0) norm_row<XT, R, NV, true>(a, t, lane, slot, half);
-  else norm_row<XT, R, NV, false>(a, t, lane, slot, half);
+  if (R <= 64 && t >= a.T) return;  // rows within a wave: the others go on
+  norm_row<XT, R, NV>(a, t, lane, slot, half);
 }
 
 // ---------------------------------------------------------------- gradient
@@ -293,35 +343,44 @@ struct NormGrad {
   int64_t T, D;
   int groups;   // of rows: group g has the rows g, g + groups, ...
   int8_t gt, wt;
+  bool lines;   // rows of whole cache lines, from the first byte of one
 };
 
 // The rows of group g.  A thread keeps its columns' weight and sums of dw; AHEAD: the next
-// row's h and dy are loaded before the present row's sum is taken.
-template <int XT, int R, int NV, bool SAME, bool AHEAD, bool WHOLE>
-__device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, float (*slot)[R / 64]) {
+// row's h and dy are loaded before the present row's sum is taken.  LINES: rows are whole
+// cache lines.
+template <int XT, int R, int NV, bool SAME, bool AHEAD, bool LINES>
+__device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, float (*slot)[(R + 63) / 64]) {
   constexpr int W = 2 * dt_size<XT>(), WY = SAME ? W : 8;
-  const int D = (int)a.D;
+  const int D = (int)a.D & ~7, last = D + lane;  // vectors up to D, then one element a thread
+  const bool has_last = !LINES && last < (int)a.D;
   const int64_t row_bytes = a.D * dt_size<XT>(), dy_bytes = a.D * (SAME ? dt_size<XT>() : kind_bytes(a.gt));
-  float w[NV][8], dw[NV][8];
+  float w[NV][8], dw[NV][8], w1 = 1.0f, dw1 = 0.0f;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) dw[j][k] = 0.0f, w[j][k] = 1.0f;
     if (a.weight) {
       uint32_t t[8];
-      load8<WHOLE, false>(a.wt, static_cast<const char*>(a.weight), (j * R + lane) * 8, D, t);
+      load8<false>(a.wt, static_cast<const char*>(a.weight), (j * R + lane) * 8, D, t);
       widen8(a.wt, t, w[j]);
     }
   }
+  if (has_last && a.weight) w1 = load1(a.wt, static_cast<const char*>(a.weight), last);
   uint32_t hw[NV][W], yw[NV][WY], dhw[NV][W], hn[AHEAD ? NV : 1][W], yn[AHEAD ? NV : 1][WY];
-  auto load = [&](int64_t t, auto& hw_, auto& yw_) {
+  float h1 = 0.0f, y1 = 0.0f, hn1 = 0.0f, yn1 = 0.0f;
+  auto load = [&](int64_t t, auto& hw_, auto& yw_, float& h1_, float& y1_) {
     const char* hr = static_cast<const char*>(a.h) + t * row_bytes;
     const char* yr = static_cast<const char*>(a.dy) + t * dy_bytes;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      load8<XT, WHOLE, kGradLoadsPast>(hr, (j * R + lane) * 8, D, hw_[j]);
-      if constexpr (SAME) load8<XT, WHOLE, kGradLoadsPast>(yr, (j * R + lane) * 8, D, yw_[j]);
-      else load8<WHOLE, kGradLoadsPast>(a.gt, yr, (j * R + lane) * 8, D, yw_[j]);
+      load8<XT, LINES>(hr, (j * R + lane) * 8, D, hw_[j]);
+      if constexpr (SAME) load8<XT, LINES>(yr, (j * R + lane) * 8, D, yw_[j]);
+      else load8<LINES>(a.gt, yr, (j * R + lane) * 8, D, yw_[j]);
+    }
+    if (has_last) {
+      h1_ = load1<XT>(hr, last);
+      y1_ = SAME ? load1<XT>(yr, last) : load1(a.gt, yr, last);
     }
   };
   auto dy_of = [&](int j, float (&v)[8]) {
@@ -329,20 +388,26 @@ __device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, fl
     else widen8(a.gt, yw[j], v);
   };
   int turn = 0;
-  if constexpr (AHEAD) load(g, hw, yw);
+  if constexpr (AHEAD) load(g, hw, yw, h1, y1);
+  float rstd_next = a.rstd[g];
   for (int64_t t = g; t < a.T; t += a.groups, turn ^= 1) {
     const char* dhr = a.dh ? static_cast<const char*>(a.dh) + t * row_bytes : nullptr;
     char* dxr = static_cast<char*>(a.dx) + t * row_bytes;
-    const float rstd = a.rstd[t];
-    if constexpr (!AHEAD) load(t, hw, yw);
+    const float rstd = rstd_next;
+    float d1 = 0.0f;
+    if constexpr (!AHEAD) load(t, hw, yw, h1, y1);
     if (dhr) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) load8<XT, WHOLE, kGradLoadsPast>(dhr, (j * R + lane) * 8, D, dhw[j]);
+      for (int j = 0; j < NV; ++j) load8<XT, LINES>(dhr, (j * R + lane) * 8, D, dhw[j]);
+      if (has_last) d1 = load1<XT>(dhr, last);
     }
-    if constexpr (AHEAD) {
-      if (t + a.groups < a.T) load(t + a.groups, hn, yn);
+    if (t + a.groups < a.T) {
+      rstd_next = a.rstd[t + a.groups];
+      if constexpr (AHEAD) load(t + a.groups, hn, yn, hn1, yn1);
     }
-    float c = 0.0f;
+    const float xh1 = h1 * rstd, gw1 = y1 * w1;
+    float c = gw1 * xh1;
+    dw1 += y1 * xh1;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float h[8], dy[8];
@@ -366,8 +431,9 @@ __device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, fl
       if (dhr) widen<XT>(dhw[j], d);
 #pragma unroll
       for (int k = 0; k < 8; ++k) d[k] += (dy[k] * w[j][k] - (h[k] * rstd) * c) * rstd;
-      store8<XT, WHOLE, kGradStoresPast>(dxr, (j * R + lane) * 8, D, d);
+      store8<XT, kGradStoresPast>(dxr, (j * R + lane) * 8, D, d);
     }
+    if (has_last) store1<XT>(dxr, last, d1 + (gw1 - xh1 * c) * rstd);
     if constexpr (AHEAD) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
@@ -376,22 +442,24 @@ __device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, fl
 #pragma unroll
         for (int k = 0; k < WY; ++k) yw[j][k] = yn[j][k];
       }
+      h1 = hn1, y1 = yn1;
     }
   }
   if (!a.part) return;
+  char* part = reinterpret_cast<char*>(a.part + (int64_t)g * a.D);
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-    store8<ZQ_F32, WHOLE, kGradStoresPast>(reinterpret_cast<char*>(a.part + (int64_t)g * a.D), (j * R + lane) * 8, D, dw[j]);
+  for (int j = 0; j < NV; ++j) store8<ZQ_F32, kGradStoresPast>(part, (j * R + lane) * 8, D, dw[j]);
+  if (has_last) store1<ZQ_F32>(part, last, dw1);
 }
 
 template <int XT, int R, int NV, bool SAME, bool AHEAD>
-__global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms_grad(NormGrad a) {
-  constexpr int THREADS = R < 256 ? 256 : R;
-  __shared__ float slot[2][R / 64];
+__global__ void __launch_bounds__(R <= 64 ? 256 : R) k_rms_grad(NormGrad a) {
+  constexpr int THREADS = R <= 64 ? 256 : R;
+  __shared__ float slot[2][(R + 63) / 64];
   const int lane = threadIdx.x % R;
   const int g = blockIdx.x * (THREADS / R) + threadIdx.x / R;
-  if (R == 64 && g >= a.groups) return;  // a wave's own rows
-  if (a.D % 8 == 0) grad_rows<XT, R, NV, SAME, AHEAD, true>(a, g, lane, slot);
+  if (R <= 64 && g >= a.groups) return;  // rows within a wave
+  if (a.lines) grad_rows<XT, R, NV, SAME, AHEAD, true>(a, g, lane, slot);
   else grad_rows<XT, R, NV, SAME, AHEAD, false>(a, g, lane, slot);
 }
 
@@ -399,22 +467,24 @@ __global__ void __launch_bounds__(R < 256 ? 256 : R) k_rms_grad(NormGrad a) {
 template <int XT>
 __global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad a) {
   __shared__ double slot[16];
-  const int D = (int)a.D;
+  const int D = (int)a.D & ~7, last = D + (int)threadIdx.x;
+  const bool has_last = last < (int)a.D;
   const int64_t t = first + blockIdx.x, at = t * a.D;
   const char* hr = static_cast<const char*>(a.h) + at * dt_size<XT>();
   const char* dyr = static_cast<const char*>(a.dy) + at * kind_bytes(a.gt);
   const char* dhr = a.dh ? static_cast<const char*>(a.dh) + at * dt_size<XT>() : nullptr;
+  const char* weight = static_cast<const char*>(a.weight);
   char* dxr = static_cast<char*>(a.dx) + at * dt_size<XT>();
   const float rstd = a.rstd[t];
   auto take = [&](int i, float (&xh)[8], float (&gw)[8]) {
     uint32_t hw[2 * dt_size<XT>()], yw[8], ww[8];
-    load8<XT, false, kGradLoadsPast>(hr, i, D, hw);
-    load8<false, kGradLoadsPast>(a.gt, dyr, i, D, yw);
+    load8<XT, false>(hr, i, D, hw);
+    load8<false>(a.gt, dyr, i, D, yw);
     widen<XT>(hw, xh);
     widen8(a.gt, yw, gw);
-    if (a.weight) {
+    if (weight) {
       float w[8];
-      load8<false, false>(a.wt, static_cast<const char*>(a.weight), i, D, ww);
+      load8<false>(a.wt, weight, i, D, ww);
       widen8(a.wt, ww, w);
 #pragma unroll
       for (int k = 0; k < 8; ++k) gw[k] = gw[k] * w[k];
@@ -422,7 +492,9 @@ __global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad
 #pragma unroll
     for (int k = 0; k < 8; ++k) xh[k] = xh[k] * rstd;
   };
-  double sum = 0.0;
+  const float xh1 = has_last ? load1<XT>(hr, last) * rstd : 0.0f;
+  const float gw1 = has_last ? load1(a.gt, dyr, last) * (weight ? load1(a.wt, weight, last) : 1.0f) : 0.0f;
+  double sum = (double)(gw1 * xh1);
   for (int i = threadIdx.x * 8; i < D; i += 8192) {
     float xh[8], gw[8], c = 0.0f;
     take(i, xh, gw);
@@ -436,35 +508,42 @@ __global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad
     take(i, xh, gw);
     if (dhr) {
       uint32_t dw[2 * dt_size<XT>()];
-      load8<XT, false, kGradLoadsPast>(dhr, i, D, dw);
+      load8<XT, false>(dhr, i, D, dw);
       widen<XT>(dw, d);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) d[k] += (gw[k] - xh[k] * c) * rstd;
-    store8<XT, false, kGradStoresPast>(dxr, i, D, d);
+    store8<XT, kGradStoresPast>(dxr, i, D, d);
   }
+  if (has_last) store1<XT>(dxr, last, (dhr ? load1<XT>(dhr, last) : 0.0f) + (gw1 - xh1 * c) * rstd);
 }
 
-// and their part of dw: 256 x 8 columns of a group of rows a workgroup
+// and their part of dw: 256 x 8 columns of a group of rows a workgroup, the row's last
+// D % 8 columns with the first 8's
 template <int XT>
 __global__ void __launch_bounds__(256) k_rms_grad_columns(unsigned first, NormGrad a, unsigned tiles) {
   const unsigned b = first + blockIdx.x;
-  const int g = (int)(b / tiles), D = (int)a.D, i = (int)((b % tiles) * 256 + threadIdx.x) * 8;
-  if (i >= D) return;
-  float dw[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  const int g = (int)(b / tiles), D = (int)a.D & ~7, i = (int)((b % tiles) * 256 + threadIdx.x) * 8, last = D + i / 8;
+  const bool has_last = last < (int)a.D;
+  if (i >= D && !has_last) return;
+  float dw[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}, dw1 = 0.0f;
   for (int64_t t = g; t < a.T; t += a.groups) {
-    const int64_t at = t * a.D;
+    const char* hr = static_cast<const char*>(a.h) + t * a.D * dt_size<XT>();
+    const char* yr = static_cast<const char*>(a.dy) + t * a.D * kind_bytes(a.gt);
     uint32_t hw[2 * dt_size<XT>()], yw[8];
     float h[8], dy[8];
-    load8<XT, false, kGradLoadsPast>(static_cast<const char*>(a.h) + at * dt_size<XT>(), i, D, hw);
-    load8<false, kGradLoadsPast>(a.gt, static_cast<const char*>(a.dy) + at * kind_bytes(a.gt), i, D, yw);
+    load8<XT, false>(hr, i, D, hw);
+    load8<false>(a.gt, yr, i, D, yw);
+    const float rstd = a.rstd[t];
+    if (has_last) dw1 += load1(a.gt, yr, last) * (load1<XT>(hr, last) * rstd);
     widen<XT>(hw, h);
     widen8(a.gt, yw, dy);
-    const float rstd = a.rstd[t];
 #pragma unroll
     for (int k = 0; k < 8; ++k) dw[k] += dy[k] * (h[k] * rstd);
   }
-  store8<ZQ_F32, false, kGradStoresPast>(reinterpret_cast<char*>(a.part + (int64_t)g * a.D), i, D, dw);
+  char* part = reinterpret_cast<char*>(a.part + (int64_t)g * a.D);
+  store8<ZQ_F32, kGradStoresPast>(part, i, D, dw);
+  if (has_last) store1<ZQ_F32>(part, last, dw1);
 }
 
 // dw from the groups' sums: 64 columns a workgroup, 16 slices of the groups, each in its
@@ -509,18 +588,28 @@ __global__ void __launch_bounds__(1024)
 
 // ---------------------------------------------------------------- choice of kernel
 
-// Threads of a row and vectors of each, by the row's length.
+// Threads of a row and vectors of each, by the row's length.  A block of 1,024 elements is
+// two waves of one turn of a row's threads: where D can be a multiple of 1,024, R is one of 128.
+template <int XT, int R, int NV>
+int norm_in(const Norm& a, hipStream_t st) {
+  return launch_parts(&k_rms<XT, R, NV>, a.T, R, st, a);
+}
 template <int XT>
 int forward(const Norm& a, hipStream_t st) {
-  const int64_t waves = (a.T + 3) / 4;
-  if (a.D <= 512) return launch_parts(&k_rms<XT, 64, 1>, waves, 256, st, a);
-  if (a.D <= 2048) return launch_parts(&k_rms<XT, 256, 1>, a.T, 256, st, a);
-  if (a.D <= 4096) return launch_parts(&k_rms<XT, 256, 2>, a.T, 256, st, a);
+  if (a.D <= 128) return launch_parts(&k_rms<XT, 16, 1>, (a.T + 15) / 16, 256, st, a);
+  if (a.D <= 256) return launch_parts(&k_rms<XT, 32, 1>, (a.T + 7) / 8, 256, st, a);
+  if (a.D <= 512) return launch_parts(&k_rms<XT, 64, 1>, (a.T + 3) / 4, 256, st, a);
+  if (a.D <= 1024) return norm_in<XT, 128, 1>(a, st);
+  if (a.D <= 1536) return norm_in<XT, 192, 1>(a, st);
+  if (a.D <= 2048) return norm_in<XT, 256, 1>(a, st);
+  if (a.D <= 2560) return norm_in<XT, 320, 1>(a, st);
+  if (a.D <= 4096) return norm_in<XT, 512, 1>(a, st);
   // 16,384 rows of 6,144: 140 us so, 145 with 256 threads of 3 vectors
-  if (a.D <= 6144) return launch_parts(&k_rms<XT, 384, 2>, a.T, 384, st, a);
-  if (a.D <= 8192) return launch_parts(&k_rms<XT, 256, 4>, a.T, 256, st, a);
-  if (a.D <= 16384) return launch_parts(&k_rms<XT, 1024, 2>, a.T, 1024, st, a);
-  return launch_parts(&k_rms<XT, 1024, 0>, a.T, 1024, st, a);
+  if (a.D <= 6144) return norm_in<XT, 384, 2>(a, st);
+  if (a.D <= 8192) return norm_in<XT, 512, 2>(a, st);
+  if (a.D <= 12288) return norm_in<XT, 768, 2>(a, st);
+  if (a.D <= 16384) return norm_in<XT, 1024, 2>(a, st);
+  return norm_in<XT, 1024, 0>(a, st);
 }
 
 int check_forward(const Norm& a, int xt, const void* weight, int wt, bool int8, int yt, int32_t block) {
@@ -555,32 +644,44 @@ int rms_norm(const void* x, const void* residual, int xt, const void* weight, in
   return xt == ZQ_F32 ? forward<ZQ_F32>(a, st) : xt == ZQ_F16 ? forward<ZQ_F16>(a, st) : forward<ZQ_BF16>(a, st);
 }
 
-// Rows are dealt to groups whose sums of dw (4 D bytes each) are joined: as many as fill
-// the chip with the threads of a row, as far as the sums stay within 16 MB.
-int row_threads(int64_t D) { return D <= 512 ? 64 : D <= 8192 ? 256 : 1024; }
+// Threads of a row in the gradient's kernels; 256 with up to 4 vectors each, as far as that
+// goes, are better than more with fewer: 16,384 rows of 6,144 take 134 us with 256 threads of
+// 3 vectors, 155 with 768 of one, 165 with 384 of 2.
+int row_threads(int64_t D) {
+  for (int r : {16, 32, 64, 128, 192, 256})
+    if (D <= 8 * r) return r;
+  return D <= 8192 ? 256 : 1024;
+}
+// Rows are dealt to groups, whose sums of dw (4 D bytes each) are joined: the same number of
+// groups on each CU, as many as its registers hold (16 waves of one vector a thread, 12 of
+// two, 8 of more), as far as the sums stay within 16 MB.
 int64_t groups_for(int64_t T, int64_t D) {
-  int64_t g = (1 << 22) / D;
-  const int64_t most = 512 * 256 / row_threads(D);
-  g = g < 1 ? 1 : g > most ? most : g;
-  return g < T ? g : T < 1 ? 1 : T;
+  const int waves = D <= 2048 ? 16 : D <= 4096 ? 12 : 8;
+  const int64_t g = kUnits * std::max(1, waves * 64 / row_threads(D));
+  const int64_t most = std::max<int64_t>(1, (1 << 22) / D);
+  return std::max<int64_t>(1, std::min(std::min(g, most), T));
 }
 
-// 16-bit rows: up to 4 vectors a thread, the next row ahead (3 vectors 140 registers); wider
-// words: half as many vectors.
+template <int XT, int R, int NV, bool SAME, bool AHEAD = true>
+int grad_in(const NormGrad& a, hipStream_t st) {
+  return launch(&k_rms_grad<XT, R, NV, SAME, AHEAD>, (unsigned)a.groups, R, st, a);
+}
 template <int XT, bool SAME>
 int backward_short(const NormGrad& a, hipStream_t st) {
-  constexpr bool WIDE = XT == ZQ_F32 || !SAME;
-  const unsigned g = (unsigned)a.groups;
-  if (a.D <= 512) return launch(&k_rms_grad<XT, 64, 1, SAME, true>, (g + 3) / 4, 256u, st, a);
-  if (a.D <= 2048) return launch(&k_rms_grad<XT, 256, 1, SAME, true>, g, 256u, st, a);
-  if (a.D <= 4096) return launch(&k_rms_grad<XT, 256, 2, SAME, true>, g, 256u, st, a);
-  if constexpr (WIDE) {
-    if (a.D <= 8192) return launch(&k_rms_grad<XT, 512, 2, SAME, true>, g, 512u, st, a);
-  } else {
-    if (a.D <= 6144) return launch(&k_rms_grad<XT, 256, 3, SAME, true>, g, 256u, st, a);
-    if (a.D <= 8192) return launch(&k_rms_grad<XT, 256, 4, SAME, true>, g, 256u, st, a);
+  constexpr bool WIDE = XT == ZQ_F32 || !SAME;  // vectors of up to 8 words: not more than 2 a thread
+  switch (row_threads(a.D)) {
+    case 16: return launch(&k_rms_grad<XT, 16, 1, SAME, true>, (unsigned)(a.groups + 15) / 16, 256u, st, a);
+    case 32: return launch(&k_rms_grad<XT, 32, 1, SAME, true>, (unsigned)(a.groups + 7) / 8, 256u, st, a);
+    case 64: return launch(&k_rms_grad<XT, 64, 1, SAME, true>, (unsigned)(a.groups + 3) / 4, 256u, st, a);
+    case 128: return grad_in<XT, 128, 1, SAME>(a, st);
+    case 192: return grad_in<XT, 192, 1, SAME>(a, st);
+    case 1024: return grad_in<XT, 1024, 2, SAME, false>(a, st);
+    default: break;
   }
-  return launch(&k_rms_grad<XT, 1024, 2, SAME, !WIDE>, g, 1024u, st, a);
+  if (a.D <= 2048) return grad_in<XT, 256, 1, SAME>(a, st);
+  if (a.D <= 4096) return grad_in<XT, 256, 2, SAME>(a, st);
+  if constexpr (WIDE) return grad_in<XT, 512, 2, SAME>(a, st);
+  else return a.D <= 6144 ? grad_in<XT, 256, 3, SAME>(a, st) : grad_in<XT, 256, 4, SAME>(a, st);
 }
 
 template <int XT>
@@ -636,7 +737,9 @@ int zq_rms_norm_grad(const void* dy, zq_dtype gt, const void* h, zq_dtype xt, co
   if (any_overlap({rdx, rdw, ws}, {rdy, rh, rw, rr, rdh})) return ZQ_E_ALIAS;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const NormGrad a = {dy, h, weight, rstd, dh, dx, dw ? static_cast<float*>(workspace) : nullptr, T, D,
-                      (int)groups_for(T, D), (int8_t)gt, (int8_t)wt};
+                      (int)groups_for(T, D), (int8_t)gt, (int8_t)wt,
+                      D * e % 64 == 0 && D * elem_bytes(gt) % 64 == 0 && aligned(h, 64) && aligned(dy, 64) &&
+                          aligned(dh, 64)};
   if (T > 0) {
     const int rc = xt == ZQ_F32 ? backward<ZQ_F32>(a, st) : xt == ZQ_F16 ? backward<ZQ_F16>(a, st) : backward<ZQ_BF16>(a, st);
     if (rc != ZQ_OK) return rc;
