@@ -38,12 +38,13 @@ constexpr int64_t kUnits = 256;  // CUs of the chip
 // first threads, so that no vector needs moving or splitting (a partial vector's words moved
 // into place cost the gradient of 16,384 x 2,056 twice its time: the wave waited for them).
 
-// Which accesses pass the caches by, measured in turns on 16,384 x 6,144 of bf16: the norm
-// 143 us with its stores past them, 156 with its loads too, 151 with neither; its gradient
-// 134 with its loads past them, 143 with its stores too, 158 with neither.  The gradient's
-// loads pass them by only where rows are whole cache lines: else two rows share a line
-// (5,003 rows of 2,051 of fp16: 39 and 32 us).
-constexpr bool kNormLoadsPast = false, kNormStoresPast = true, kGradStoresPast = false;
+// Which accesses pass the caches by, measured in turns on 16,384 x 6,144 of bf16, outputs in
+// new memory each time: the norm 140 us with its stores past them, 137 with its loads too
+// (but 37 and 35 us on 8,192 x 2,048 into INT8), 147 with neither; its gradient 137 with
+// both, 148 with its loads alone, 153 with neither.  The gradient's do so only where rows are
+// whole cache lines: else two rows share a line (5,003 rows of 2,051 of fp16: loads past them
+// 39 us, through them 32, with stores past them 4% more).
+constexpr bool kNormLoadsPast = false, kNormStoresPast = true;
 
 // the words of 8 elements from element i on; zeros from element n on, a multiple of 8
 template <int DT, bool PAST>
@@ -431,7 +432,7 @@ __device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, fl
       if (dhr) widen<XT>(dhw[j], d);
 #pragma unroll
       for (int k = 0; k < 8; ++k) d[k] += (dy[k] * w[j][k] - (h[k] * rstd) * c) * rstd;
-      store8<XT, kGradStoresPast>(dxr, (j * R + lane) * 8, D, d);
+      store8<XT, LINES>(dxr, (j * R + lane) * 8, D, d);
     }
     if (has_last) store1<XT>(dxr, last, d1 + (gw1 - xh1 * c) * rstd);
     if constexpr (AHEAD) {
@@ -448,7 +449,7 @@ __device__ __forceinline__ void grad_rows(const NormGrad& a, int g, int lane, fl
   if (!a.part) return;
   char* part = reinterpret_cast<char*>(a.part + (int64_t)g * a.D);
 #pragma unroll
-  for (int j = 0; j < NV; ++j) store8<ZQ_F32, kGradStoresPast>(part, (j * R + lane) * 8, D, dw[j]);
+  for (int j = 0; j < NV; ++j) store8<ZQ_F32, false>(part, (j * R + lane) * 8, D, dw[j]);
   if (has_last) store1<ZQ_F32>(part, last, dw1);
 }
 
@@ -513,7 +514,7 @@ __global__ void __launch_bounds__(1024) k_rms_grad_long(unsigned first, NormGrad
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) d[k] += (gw[k] - xh[k] * c) * rstd;
-    store8<XT, kGradStoresPast>(dxr, i, D, d);
+    store8<XT, false>(dxr, i, D, d);
   }
   if (has_last) store1<XT>(dxr, last, (dhr ? load1<XT>(dhr, last) : 0.0f) + (gw1 - xh1 * c) * rstd);
 }
@@ -542,7 +543,7 @@ __global__ void __launch_bounds__(256) k_rms_grad_columns(unsigned first, NormGr
     for (int k = 0; k < 8; ++k) dw[k] += dy[k] * (h[k] * rstd);
   }
   char* part = reinterpret_cast<char*>(a.part + (int64_t)g * a.D);
-  store8<ZQ_F32, kGradStoresPast>(part, i, D, dw);
+  store8<ZQ_F32, false>(part, i, D, dw);
   if (has_last) store1<ZQ_F32>(part, last, dw1);
 }
 
@@ -645,7 +646,7 @@ int rms_norm(const void* x, const void* residual, int xt, const void* weight, in
 }
 
 // Threads of a row in the gradient's kernels; 256 with up to 4 vectors each, as far as that
-// goes, are better than more with fewer: 16,384 rows of 6,144 take 134 us with 256 threads of
+// goes, are better than more with fewer: 16,384 rows of 6,144 took 134 us with 256 threads of
 // 3 vectors, 155 with 768 of one, 165 with 384 of 2.
 int row_threads(int64_t D) {
   for (int r : {16, 32, 64, 128, 192, 256})
