@@ -358,7 +358,7 @@ int64_t zq_int4_dequant_gemm_bytes(int64_t M, int64_t N, int64_t K); /* -1 for s
  * 2^-110: scale 0 and codes 0; else scale = fl(a / top), and fl(|x| * fl(top / a)) is
  * rounded to a neighbouring code, up with the chance of the part cut off (16 bits of it),
  * so that changes smaller than a step are kept on average: nearest rounding would lose
- * every change of v by less than an eighth.  The bits drawn for element i of tensor k are
+ * every change of v by less than an eighth.  (m's sign is kept, that of a zero too.)  The bits drawn for element i of tensor k are
  * a function of (t, k, i) alone: the same step gives the same result.  With w = mix(key ^
  * (i mod 2^32)), key = mix(mix(mix(t) + k * 0x9E3779B9) + i / 2^32) (the outer mix only
  * where i / 2^32 > 0), mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *=
@@ -460,8 +460,9 @@ int64_t zq_rms_norm_grad_bytes(int64_t T, int64_t D); /* -1 for sizes outside th
 /* ---- The loss at the output head ------------------------------------------------
  * Log-probabilities of given tokens, and the clipped policy loss with a KL term and its
  * gradient, from rows of V logits.  Row t of logits starts at element t * ld (ld >= V:
- * heads padded to a wider row).  A logit of -infinity names a token that cannot occur:
- * probability and gradient 0.  An id outside [0, V), or a row without any logit above
+ * heads padded to a wider row), T * ld at most 2^59.  A logit of -infinity names a token
+ * that cannot occur: probability and gradient 0 (as the row's own token: logp -infinity and
+ * a ratio of 0; a KL term is then infinite).  An id outside [0, V), or a row without any logit above
  * -infinity, names no token: logp 0, no loss, a gradient of zeros.
  *
  * zq_token_logp: logp[t] = scale * (z[a] - max z) - log(sum_v exp(scale * (z[v] - max z))),

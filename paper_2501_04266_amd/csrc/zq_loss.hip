@@ -29,6 +29,7 @@ namespace zq {
 namespace {
 
 constexpr int64_t kMaxVocab = 1 << 24;
+constexpr int64_t kMaxPlaces = (int64_t)1 << 59;  // T * ld: bytes of all rows within 63 bits
 constexpr float kInf = __builtin_inff();
 
 struct Loss {
@@ -409,7 +410,7 @@ int64_t span(int64_t T, int64_t V, int64_t ld, int64_t e) { return T > 0 ? ((T -
 
 int check_logits(const void* logits, int lt, int64_t T, int64_t V, int64_t ld, const void* ids, int it, float scale) {
   if (!dtype_ok(lt) || (it != ZQ_I32 && it != ZQ_I64)) return ZQ_E_DTYPE;
-  if (T < 0 || T > (1 << 30) || V < 1 || V > kMaxVocab || ld < V || ld > ((int64_t)1 << 32)) return ZQ_E_SIZE;
+  if (T < 0 || T > (1 << 30) || V < 1 || V > kMaxVocab || ld < V || (T > 0 && ld > kMaxPlaces / T)) return ZQ_E_SIZE;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return ZQ_E_SIZE;
   if (T == 0) return ZQ_OK;
   if (!logits || !ids) return ZQ_E_NULL;
@@ -450,7 +451,7 @@ int zq_policy_loss(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_
   if (!(p.clip_low >= 0.0f && p.clip_low <= 1.0f) || !(p.clip_high >= 0.0f) || !(p.kl >= 0.0f) ||
       !std::isfinite(p.clip_high) || !std::isfinite(p.kl) || !std::isfinite(p.grad_scale))
     return ZQ_E_SIZE;
-  if (grad && (ldg < V || ldg > ((int64_t)1 << 32))) return ZQ_E_SIZE;
+  if (grad && (ldg < V || (T > 0 && ldg > kMaxPlaces / T))) return ZQ_E_SIZE;
   const int64_t need = zq_policy_loss_bytes(T);
   if (workspace_bytes < need) return ZQ_E_SIZE;
   if (!sums || (T > 0 && (!workspace || !p.old_logp || !p.advantages || (p.kl != 0.0f && !p.ref_logp)))) return ZQ_E_NULL;

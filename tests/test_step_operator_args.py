@@ -308,7 +308,7 @@ def loss(L, policy=None, **other):
 @pytest.mark.parametrize("other,policy,status", [
     (dict(lt=3), {}, DTYPE), (dict(it=0), {}, DTYPE), (dict(gt=INT8), {}, DTYPE),
     (dict(T=-1), {}, SIZE), (dict(T=(1 << 30) + 1), {}, SIZE), (dict(V=0), {}, SIZE), (dict(V=(1 << 24) + 1, ld=1 << 25), {}, SIZE),
-    (dict(ld=99), {}, SIZE), (dict(ldg=99), {}, SIZE), (dict(ld=(1 << 32) + 1), {}, SIZE), (dict(bytes=319), {}, SIZE),
+    (dict(ld=99), {}, SIZE), (dict(ldg=99), {}, SIZE), (dict(ld=(1 << 59) // 10 + 1), {}, SIZE), (dict(ldg=(1 << 59) // 10 + 1), {}, SIZE), (dict(bytes=319), {}, SIZE),
     ({}, dict(scale=0.0), SIZE), ({}, dict(scale=-1.0), SIZE), ({}, dict(scale=math.inf), SIZE), ({}, dict(scale=math.nan), SIZE),
     ({}, dict(clip_low=-0.1), SIZE), ({}, dict(clip_low=1.1), SIZE), ({}, dict(clip_high=-0.1), SIZE), ({}, dict(clip_high=math.nan), SIZE),
     ({}, dict(kl=-1.0), SIZE), ({}, dict(kl=math.inf), SIZE), ({}, dict(grad_scale=math.nan), SIZE),
