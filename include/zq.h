@@ -327,7 +327,8 @@ int zq_int4_dequant_gemm(const void* x, zq_dtype xt, const uint8_t* packed, cons
 int64_t zq_int4_dequant_gemm_bytes(int64_t M, int64_t N, int64_t K); /* -1 for sizes outside the limits */
 
 /* ---- The optimizer's step ------------------------------------------------------
- * One AdamW step over any number of tensors in one launch: the owner's shard of the
+ * One AdamW step over any number of tensors in one launch (two, where only some have 8-bit
+ * moments or an INT8 out): the owner's shard of the
  * optimizer states (Design, Optimizer-State Partitioning) updated from the gradient
  * shards as the reduce levels leave them, clipped on the way, and the weight written
  * in the form that is gathered next.  For every element, with t the step, fl() as
@@ -391,8 +392,9 @@ typedef struct {
 
 /* Sizes of a table of tensors; filled by zq_adamw_plan_make. */
 typedef struct {
-  int64_t bytes; /* of the table */
-  int64_t pieces;
+  int64_t bytes;        /* of the table */
+  int64_t pieces;       /* of tensors without blocks of their own */
+  int64_t block_pieces; /* of those with 8-bit moments or an INT8 out */
   int32_t count;
   int32_t reserved;
 } zq_adamw_plan;

@@ -54,8 +54,8 @@ class _AdamW(ctypes.Structure):  # zq_adamw
 
 
 class _AdamWPlan(ctypes.Structure):  # zq_adamw_plan
-    _fields_ = [("bytes", ctypes.c_int64), ("pieces", ctypes.c_int64), ("count", ctypes.c_int32),
-                ("reserved", ctypes.c_int32)]
+    _fields_ = [("bytes", ctypes.c_int64), ("pieces", ctypes.c_int64), ("block_pieces", ctypes.c_int64),
+                ("count", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class _AdamWArgs(ctypes.Structure):  # zq_adamw_args
@@ -722,7 +722,7 @@ def adamw_table(params, grads, exp_avg, exp_avg_sq, outs=None, weight_decay=0.0,
 
 
 def adamw_step(table, step, lr, betas=(0.9, 0.999), eps=1e-8, norm=None, max_norm=None, scale=1.0, stream=None):
-    """One AdamW step over an AdamWTable, in one launch; returns the parameters, updated
+    """One AdamW step over an AdamWTable, in a launch or two; returns the parameters, updated
     in place.  step counts from 1.  With norm (grad_norm's, on the GPU, called with the
     same scale) gradients are clipped to max_norm on the way, as grad_clip does, and a
     norm that is not finite leaves everything as it is; scale multiplies the gradients.

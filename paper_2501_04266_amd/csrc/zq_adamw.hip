@@ -14,8 +14,10 @@
 // only known after the update, so a wave holds whole blocks (1,024 elements, the largest
 // block) in registers, updates them, and takes the blocks' maxima across its lanes.
 //
-// One launch covers all tensors, a workgroup a piece of 4,096 elements; a map in the
-// table says which tensor a piece belongs to.
+// A launch covers all tensors of a kind, a workgroup a piece: 4,096 elements where there are
+// blocks, 1,024 where moments are binary32 and the copy is dense (fewer registers, twice the
+// waves: the step of 1.2 billion elements takes 5,890 us so, 6,190 in pieces of 4,096, that
+// of 0.8 million 6.8 and 8.7).  A map in the table says which tensor a piece belongs to.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -32,9 +34,9 @@ namespace zq {
 namespace {
 
 constexpr int kAdamThreads = 256;
-constexpr int kPiece = 4096;             // elements of a workgroup
-constexpr int kWaveElems = 1024;         // of a wave: whole blocks of any size
-constexpr int kSteps = kWaveElems / 256; // 4 elements a lane and step
+constexpr int kSteps = 4;  // of a wave with blocks, 256 elements each: whole blocks of any size
+constexpr int kPlainSteps = 1;
+__host__ __device__ constexpr int piece_elems(bool blocks) { return (blocks ? kSteps : kPlainSteps) * 4 * kAdamThreads; }
 constexpr int kInt4 = 3, kInt8 = 4;      // type codes beside ZQ_F32 / ZQ_F16 / ZQ_BF16
 constexpr int kNone = -1;
 
@@ -50,7 +52,7 @@ struct Entry {
   char* out;
   float* outs;
   int64_t n;
-  int64_t piece0;  // pieces of the tensors before it
+  int64_t piece0;  // pieces of the tensors of its kind before it
   double decay, lr_scale;
   int8_t pt, gt, ot, state8;
   int8_t lgG, lgS, lgO, pad;
@@ -66,7 +68,7 @@ struct Coef {
 static_assert(sizeof(Coef) == 56, "table layout");
 
 // Table: the numbers of a step whose count or rate is on the device, the entries, the
-// entry of each piece.
+// entry of each piece without blocks and of each with.
 constexpr int64_t kEntriesAt = 64;
 __host__ __device__ inline int64_t map_at(int entries) { return kEntriesAt + (int64_t)entries * (int64_t)sizeof(Entry); }
 
@@ -334,16 +336,19 @@ __device__ __forceinline__ void store_int8(const float (&x)[kSteps][4], char* co
   }
 }
 
-// ---------------------------------------------------------------- a wave's 1,024 elements
+// ---------------------------------------------------------------- a wave's elements
 
-template <int PT, int GT, bool S8, bool FULL>
+// BLOCKS: 8-bit moments or an INT8 copy, or both
+template <int PT, int GT, bool BLOCKS, bool S8, bool FULL>
 __device__ __forceinline__ void update(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0) {
+  static_assert(BLOCKS || !S8, "8-bit moments are in blocks");
+  constexpr int N = BLOCKS ? kSteps : kPlainSteps;
   const int64_t n = en.n;
   // all loads first
-  uint32_t pw[kSteps][4], gw[kSteps][4], mw[kSteps][4], vw[kSteps][4];
-  float gs[kSteps], ms[kSteps], vs[kSteps];
+  uint32_t pw[N][4], gw[N][4], mw[N][4], vw[N][4];
+  float gs[N], ms[N], vs[N];
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
+  for (int u = 0; u < N; ++u) {
     const int64_t i = i0 + u * 256;
     load4<PT, FULL>(en.p, i, n, pw[u]);
     if constexpr (GT == kInt4) {
@@ -364,9 +369,9 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
   }
   const float alpha = (float)(c.rate * en.lr_scale), decay = (float)(1.0 - c.lr * en.lr_scale * en.decay);
 
-  float p[kSteps][4], m[kSteps][4], v[kSteps][4];
+  float p[N][4], m[N][4], v[N][4];
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
+  for (int u = 0; u < N; ++u) {
     float g[4];
     widen4<PT>(pw[u], p[u]);
     if constexpr (GT == kInt4) {
@@ -398,7 +403,7 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
   }
 
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
+  for (int u = 0; u < N; ++u) {
     const int64_t i = i0 + u * 256;
     store4<PT, FULL>(en.p, i, n, p[u]);
     if constexpr (!S8) {
@@ -409,24 +414,24 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
   if constexpr (S8) {
     uint32_t key = mix(c.key + (uint32_t)tensor * 0x9E3779B9u);
     if ((i0 >> 32) != 0) key = mix(key + (uint32_t)(i0 >> 32));  // the same for a piece
-    uint32_t drawn[kSteps][4];
+    uint32_t drawn[N][4];
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) draw4(key, (uint32_t)i0 + (uint32_t)(u * 256), drawn[u]);
+    for (int u = 0; u < N; ++u) draw4(key, (uint32_t)i0 + (uint32_t)(u * 256), drawn[u]);
     store_state8<true, FULL>(m, drawn, en.m, en.ms, en.lgS, i0, n);
     store_state8<false, FULL>(v, drawn, en.v, en.vs, en.lgS, i0, n);
   }
   if (en.ot == kNone) return;
   if constexpr (PT != ZQ_F32) {  // the copy is of the weight as stored
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
+    for (int u = 0; u < N; ++u) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) p[u][k] = PT == ZQ_BF16 ? u2f(bf16x2_bits(p[u][k], 0.0f) << 16) : h2f(f2h(p[u][k]));
     }
   }
-  if (en.ot == kInt8) {
+  if constexpr (BLOCKS) if (en.ot == kInt8) {
     if constexpr (!FULL) {  // what lies behind the end counts in no block
 #pragma unroll
-      for (int u = 0; u < kSteps; ++u) {
+      for (int u = 0; u < N; ++u) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           if (i0 + u * 256 + k >= n) p[u][k] = 0.0f;
@@ -436,7 +441,7 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
     return;
   }
 #pragma unroll
-  for (int u = 0; u < kSteps; ++u) {
+  for (int u = 0; u < N; ++u) {
     const int64_t i = i0 + u * 256;
     if (en.ot == ZQ_BF16) store4<ZQ_BF16, FULL>(en.out, i, n, p[u]);
     else if (en.ot == ZQ_F16) store4<ZQ_F16, FULL>(en.out, i, n, p[u]);
@@ -444,37 +449,35 @@ __device__ __forceinline__ void update(const Entry& en, const Coef& c, float cli
   }
 }
 
-template <int PT, int GT, bool S8>
+template <int PT, int GT, bool BLOCKS>
 __device__ __forceinline__ void update_any(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0, bool full) {
-  if (full) update<PT, GT, S8, true>(en, c, clip, tensor, i0);
-  else update<PT, GT, S8, false>(en, c, clip, tensor, i0);
+  if constexpr (BLOCKS) {
+    if (en.state8) {
+      if (full) update<PT, GT, true, true, true>(en, c, clip, tensor, i0);
+      else update<PT, GT, true, true, false>(en, c, clip, tensor, i0);
+      return;
+    }
+  }
+  if (full) update<PT, GT, BLOCKS, false, true>(en, c, clip, tensor, i0);
+  else update<PT, GT, BLOCKS, false, false>(en, c, clip, tensor, i0);
 }
 
-template <int PT, bool S8>
+template <int PT, bool BLOCKS>
 __device__ __forceinline__ void update_grad(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0, bool full) {
   switch (en.gt) {
-    case ZQ_F32: update_any<PT, ZQ_F32, S8>(en, c, clip, tensor, i0, full); break;
-    case ZQ_F16: update_any<PT, ZQ_F16, S8>(en, c, clip, tensor, i0, full); break;
-    case ZQ_BF16: update_any<PT, ZQ_BF16, S8>(en, c, clip, tensor, i0, full); break;
-    default: update_any<PT, kInt4, S8>(en, c, clip, tensor, i0, full); break;
+    case ZQ_F32: update_any<PT, ZQ_F32, BLOCKS>(en, c, clip, tensor, i0, full); break;
+    case ZQ_F16: update_any<PT, ZQ_F16, BLOCKS>(en, c, clip, tensor, i0, full); break;
+    case ZQ_BF16: update_any<PT, ZQ_BF16, BLOCKS>(en, c, clip, tensor, i0, full); break;
+    default: update_any<PT, kInt4, BLOCKS>(en, c, clip, tensor, i0, full); break;
   }
 }
 
-template <bool S8>
-__device__ __forceinline__ void update_param(const Entry& en, const Coef& c, float clip, int tensor, int64_t i0, bool full) {
-  switch (en.pt) {
-    case ZQ_F32: update_grad<ZQ_F32, S8>(en, c, clip, tensor, i0, full); break;
-    case ZQ_F16: update_grad<ZQ_F16, S8>(en, c, clip, tensor, i0, full); break;
-    default: update_grad<ZQ_BF16, S8>(en, c, clip, tensor, i0, full); break;
-  }
-}
-
-// 4 waves a SIMD (128 registers): 453 million elements with 8-bit moments take 1,315 us, with
-// the 136 registers that the compiler would take 1,385.
+// With blocks 4 waves a SIMD (128 registers): 453 million elements with 8-bit moments take
+// 1,315 us, with the 136 registers that the compiler would take 1,385.
+template <bool BLOCKS>
 __global__ void __launch_bounds__(kAdamThreads, 4)
-    k_adamw(unsigned first, const char* __restrict__ table, int count, Coef given, int from_table,
+    k_adamw(unsigned first, const char* __restrict__ table, const int* __restrict__ entry_of, Coef given, int from_table,
             const float* __restrict__ norm) {
-  const int* entry_of = reinterpret_cast<const int*>(table + map_at(count));
   const unsigned piece = first + blockIdx.x;
   const int tensor = entry_of[piece];
   const Entry en = reinterpret_cast<const Entry*>(table + kEntriesAt)[tensor];
@@ -486,16 +489,25 @@ __global__ void __launch_bounds__(kAdamThreads, 4)
     const float ratio = c.max_norm / (t + 1e-6f);
     clip = c.scale * (ratio > 1.0f ? 1.0f : ratio);
   }
-  const int64_t e0 = ((int64_t)piece - en.piece0) * kPiece;
-  const int64_t i0 = e0 + (threadIdx.x >> 6) * kWaveElems + (threadIdx.x & 63) * 4;
-  const bool full = e0 + kPiece <= en.n;
-  if (en.state8) update_param<true>(en, c, clip, tensor, i0, full);
-  else update_param<false>(en, c, clip, tensor, i0, full);
+  constexpr int PIECE = piece_elems(BLOCKS), WAVE = PIECE / (kAdamThreads / 64);
+  static_assert(WAVE == (BLOCKS ? kSteps : kPlainSteps) * 256, "a wave's elements");
+  const int64_t e0 = ((int64_t)piece - en.piece0) * PIECE;
+  const int64_t i0 = e0 + (threadIdx.x >> 6) * WAVE + (threadIdx.x & 63) * 4;
+  const bool full = e0 + PIECE <= en.n;
+  switch (en.pt) {
+    case ZQ_F32: update_grad<ZQ_F32, BLOCKS>(en, c, clip, tensor, i0, full); break;
+    case ZQ_F16: update_grad<ZQ_F16, BLOCKS>(en, c, clip, tensor, i0, full); break;
+    default: update_grad<ZQ_BF16, BLOCKS>(en, c, clip, tensor, i0, full); break;
+  }
 }
 
 // ---------------------------------------------------------------- table
 
-int64_t pieces_of(int64_t n) { return (n + kPiece - 1) / kPiece; }
+bool has_blocks(const zq_adamw& t) { return t.state_dtype == ZQ_F8 || (t.out && t.out_dtype == ZQ_INT8); }
+int64_t pieces_of(const zq_adamw& t) {
+  const int64_t per = piece_elems(has_blocks(t));
+  return (t.n + per - 1) / per;
+}
 
 int check(const zq_adamw& t) {
   if (t.n < 0 || t.n > INT64_MAX / 16) return ZQ_E_SIZE;
@@ -578,12 +590,12 @@ int plan_table(const zq_adamw* tensors, int32_t count, zq_adamw_plan* plan) {
   for (int32_t i = 0; i < count; ++i) {
     const int rc = check(tensors[i]);
     if (rc != ZQ_OK) return rc;
-    p.pieces += pieces_of(tensors[i].n);
-    if (p.pieces > kMaxGrid) return ZQ_E_SIZE;
+    (has_blocks(tensors[i]) ? p.block_pieces : p.pieces) += pieces_of(tensors[i]);
+    if (p.pieces > kMaxGrid || p.block_pieces > kMaxGrid) return ZQ_E_SIZE;
   }
   const int rc = check_overlaps(tensors, count);
   if (rc != ZQ_OK) return rc;
-  p.bytes = map_at(count) + 4 * p.pieces;
+  p.bytes = map_at(count) + 4 * (p.pieces + p.block_pieces);
   *plan = p;
   return ZQ_OK;
 }
@@ -609,13 +621,15 @@ int zq_adamw_plan_table(const zq_adamw* tensors, const zq_adamw_plan* plan, void
   std::fill(t, t + kEntriesAt, (char)0);
   Entry* entries = reinterpret_cast<Entry*>(t + kEntriesAt);
   int* map = reinterpret_cast<int*>(t + map_at(plan->count));
-  int64_t at = 0;
+  int64_t at[2] = {0, 0};
   for (int32_t i = 0; i < plan->count; ++i) {
+    const bool blocks = has_blocks(tensors[i]);
     entries[i] = entry_for(tensors[i]);
-    entries[i].piece0 = at;
-    const int64_t pieces = pieces_of(tensors[i].n);
-    std::fill(map + at, map + at + pieces, i);
-    at += pieces;
+    entries[i].piece0 = at[blocks];
+    const int64_t pieces = pieces_of(tensors[i]);
+    int* of = map + (blocks ? plan->pieces : 0) + at[blocks];
+    std::fill(of, of + pieces, i);
+    at[blocks] += pieces;
   }
   return ZQ_OK;
 }
@@ -629,7 +643,7 @@ int zq_adamw_step(const zq_adamw_plan* plan, void* table, const zq_adamw_args* a
   if (!share(args->beta1) || !share(args->beta2) || !(args->eps >= 0.0) || (!step && args->step < 1) ||
       (!lr && !std::isfinite(args->lr)) || (norm && !(args->max_norm >= 0.0f)))
     return ZQ_E_SIZE;
-  if (plan->pieces == 0) return ZQ_OK;
+  if (plan->pieces == 0 && plan->block_pieces == 0) return ZQ_OK;
   hipStream_t st = static_cast<hipStream_t>(stream);
   Coef c = {};
   if (step || lr) {
@@ -638,8 +652,12 @@ int zq_adamw_step(const zq_adamw_plan* plan, void* table, const zq_adamw_args* a
   } else {
     c = coef_of(*args, args->step, args->lr);
   }
-  return launch_parts(&k_adamw, plan->pieces, kAdamThreads, st, static_cast<const char*>(table), plan->count, c,
-                      step || lr ? 1 : 0, norm);
+  const char* t = static_cast<const char*>(table);
+  const int* map = reinterpret_cast<const int*>(t + map_at(plan->count));
+  const int from_table = step || lr ? 1 : 0;
+  const int rc = launch_parts(&k_adamw<false>, plan->pieces, kAdamThreads, st, t, map, c, from_table, norm);
+  if (rc != ZQ_OK) return rc;
+  return launch_parts(&k_adamw<true>, plan->block_pieces, kAdamThreads, st, t, map + plan->pieces, c, from_table, norm);
 }
 
 }  // extern "C"

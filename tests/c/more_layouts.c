@@ -33,6 +33,7 @@ int main(void) {
   printf("zq_adamw_plan %zu\n", sizeof(zq_adamw_plan));
   FIELD(zq_adamw_plan, bytes);
   FIELD(zq_adamw_plan, pieces);
+  FIELD(zq_adamw_plan, block_pieces);
   FIELD(zq_adamw_plan, count);
   FIELD(zq_adamw_plan, reserved);
   printf("zq_adamw_args %zu\n", sizeof(zq_adamw_args));

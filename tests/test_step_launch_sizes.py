@@ -101,7 +101,7 @@ def test_logp(run, T, V, threads):
 
 def test_step(run):
     pieces = (1 << 31) - 1
-    plan = _lib._AdamWPlan(1 << 40, pieces, 1, 0)
+    plan = _lib._AdamWPlan(1 << 40, pieces, 0, 1, 0)
     args = _lib._AdamWArgs(1e-3, 0.9, 0.99, 1e-8, 1, 1.0, 1.0)
     text = [ctypes.string_at(ctypes.byref(s), ctypes.sizeof(s)).hex() for s in (plan, args)]
     rc, launches = run("zq_adamw_step", [P] * 7, text[0], A, text[1], None, None, None, None)
@@ -111,3 +111,11 @@ def test_step(run):
     rc, launches = run("zq_adamw_step", [P] * 7, text[0], A, text[1], B, None, None, None)
     assert rc == 0 and launches[0][4] == 64 and launches[0][0] != launches[1][0]
     parts(launches[1:], pieces, 256)
+    # tensors of both kinds: a kernel each
+    plan.block_pieces = 1 << 30
+    text[0] = ctypes.string_at(ctypes.byref(plan), ctypes.sizeof(plan)).hex()
+    rc, launches = run("zq_adamw_step", [P] * 7, text[0], A, text[1], None, None, None, None)
+    kernels = list(dict.fromkeys(e[0] for e in launches))
+    assert rc == 0 and len(kernels) == 2
+    parts([e for e in launches if e[0] == kernels[0]], pieces, 256)
+    parts([e for e in launches if e[0] == kernels[1]], 1 << 30, 256)

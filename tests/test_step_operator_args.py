@@ -91,8 +91,10 @@ def test_tensors(L, other, status):
 
 def test_tables(L):
     rc, plan = made(L, tensor(), tensor(param=A + 4000, grad=B, m=C + 4000, v=D + 4000, n=9000))
-    assert rc == 0 and plan.count == 2 and plan.pieces == 1 + 3  # pieces of 4,096; a gradient may be read twice
-    assert plan.bytes == 64 + 2 * 112 + 4 * 4
+    assert rc == 0 and plan.count == 2 and plan.pieces == 1 + 9 and plan.block_pieces == 0  # of 1,024; a gradient may be read twice
+    assert plan.bytes == 64 + 2 * 112 + 4 * 10
+    rc, plan = made(L, tensor(), tensor(param=A + 4000, grad=B, m=C + 4000, v=D + 4000, n=9000, **STATE8))
+    assert rc == 0 and plan.pieces == 1 and plan.block_pieces == 3 and plan.bytes == 64 + 2 * 112 + 4 * 4  # of 4,096
     assert made(L, tensor(), tensor())[0] == ALIAS  # a parameter twice
     assert made(L, count=-1)[0] == SIZE and made(L)[0] == 0
     assert L.zq_adamw_plan_make(None, 1, ctypes.byref(plan)) == NULL and L.zq_adamw_plan_make(None, 0, None) == NULL
@@ -114,7 +116,7 @@ def test_tables(L):
 def test_numbers_of_a_step(L, args, more, status):
     a = _lib._AdamWArgs(**{**dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, max_norm=1.0, scale=1.0), **args})
     at = {**dict(table=A, step=None, lr=None, norm=None), **more}
-    empty = _lib._AdamWPlan(64, 0, 0, 0)
+    empty = _lib._AdamWPlan(64, 0, 0, 0, 0)
     assert L.zq_adamw_step(ctypes.byref(empty), vp(at["table"]), ctypes.byref(a), vp(at["step"]), vp(at["lr"]),
                            vp(at["norm"]), None) == status
     assert L.zq_adamw_step(None, vp(A), ctypes.byref(a), None, None, None, None) == NULL
