@@ -6,11 +6,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <algorithm>
 #include <initializer_list>
 #include <tuple>
 #include <utility>
-#include <vector>
 
 #include "zq.h"
 #include "zq_limits.h"
@@ -83,27 +81,6 @@ inline bool any_overlap(std::initializer_list<Range> outs, std::initializer_list
     for (auto o2 = o1 + 1; o2 != outs.end(); ++o2)
       if (overlap(*o1, *o2)) return true;
   return false;
-}
-
-// Memory of a table of tensors: what is written must not overlap anything else.  The
-// ranges in the order of their addresses, each output against what starts before its end.
-struct Span {
-  uintptr_t from, to;
-  bool out;
-};
-inline void put_span(std::vector<Span>& spans, const void* p, int64_t bytes, bool out) {
-  if (p && bytes > 0) spans.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, out});
-}
-inline int check_spans(std::vector<Span>& spans) {
-  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
-  // the furthest end of outputs, and of anything, among the spans before
-  uintptr_t out_to = 0, any_to = 0;
-  for (const Span& s : spans) {
-    if (s.from < out_to || (s.out && s.from < any_to)) return ZQ_E_ALIAS;
-    any_to = std::max(any_to, s.to);
-    if (s.out) out_to = std::max(out_to, s.to);
-  }
-  return ZQ_OK;
 }
 
 inline int64_t num_scales(int64_t n, int32_t block) { return (n + block - 1) / block; }

@@ -32,6 +32,7 @@
 #include "zq.h"
 #include "zq_device.h"
 #include "zq_host.h"
+#include "zq_spans.h"
 #include "zq_vec.h"
 
 #pragma clang fp contract(off)
