@@ -7,7 +7,7 @@
 //
 // Bound by memory: a row of logits is read once, kept in the registers of one workgroup
 // (64 to 1,024 threads, up to 16 vectors of 16 bytes each), and its gradient written
-// once (8,192 rows of 50,000 of bf16: 306 us, 5.1 TB/s; without any exp 294).  exp is v_exp_f32 of a binary32 difference; it is taken twice, for the sum and for
+// once (8,192 rows of 50,000 of bf16: 285 us, 5.5 TB/s).  exp is v_exp_f32 of a binary32 difference; it is taken twice, for the sum and for
 // the gradient, since a row's exponentials in binary32 would need twice the registers of
 // 16-bit logits.  A thread's sum is binary32 (up to 128 terms), sums over threads and what
 // follows binary64: whether a token is clipped is decided at 1 +- clip, and its logarithm
@@ -138,18 +138,20 @@ __device__ __forceinline__ double group_sum(double v, double* slot) {
   return s;
 }
 
-// exp and log of a token's few binary64 numbers, as loops over their series with the
-// coefficients in scalar registers: they run while a row waits in the vector registers,
-// and the library's functions take some 40 of those.  Errors below 2^-48 relative.
-__device__ const double kInverse[14] = {1.0, 1.0,       1.0 / 2,  1.0 / 3,  1.0 / 4,  1.0 / 5,  1.0 / 6,
-                                        1.0 / 7, 1.0 / 8, 1.0 / 9, 1.0 / 10, 1.0 / 11, 1.0 / 12, 1.0 / 13};
+// exp and log of a token's few binary64 numbers, by their series: they run while a row
+// waits in the vector registers, and the library's functions take some 40 of those.  Errors
+// below 2^-48 relative.  (As loops with the coefficients read in turn they held a row of 50,000
+// up for 6% of its time; a token's own values loaded when wanted, for 2%.)
 __device__ __forceinline__ double exp64(double x) {
   if (!(fabs(x) <= 700.0)) return x > 0.0 ? (double)kInf : x < 0.0 ? 0.0 : x;
   // x = k log 2 + r, |r| <= 0.35: the series to r^13 / 13!
+  constexpr double c[14] = {1.0,         1.0,          1.0 / 2,       1.0 / 6,        1.0 / 24,        1.0 / 120,       1.0 / 720,
+                            1.0 / 5040., 1.0 / 40320., 1.0 / 362880., 1.0 / 3628800., 1.0 / 39916800., 1.0 / 479001600.,
+                            1.0 / 6227020800.};
   const double k = rint(x * 1.4426950408889634), r = __builtin_fma(k, -0x1.62e42fefa39efp-1, x);
-  double p = 1.0;
-#pragma unroll 1
-  for (int n = 13; n >= 1; --n) p = __builtin_fma(p, r * kInverse[n], 1.0);
+  double p = c[13];
+#pragma unroll
+  for (int n = 12; n >= 0; --n) p = __builtin_fma(p, r, c[n]);
   return ldexp(p, (int)k);
 }
 // of s from 1 to 2^24 (or NaN)
@@ -159,26 +161,40 @@ __device__ __forceinline__ double log64(double s) {
   if (f < 0.70710678118654752) f *= 2.0, --k;
   // log f = 2 (q + q^3 / 3 + ... + q^23 / 23), q = (f - 1) / (f + 1), |q| <= 0.172
   const double q = (f - 1.0) / (f + 1.0), q2 = q * q;
-  double p = 0.0;
-#pragma unroll 1
-  for (int n = 23; n >= 1; n -= 2) p = __builtin_fma(p, q2, 1.0 / n);
+  double p = 1.0 / 23;
+#pragma unroll
+  for (int n = 21; n >= 1; n -= 2) p = __builtin_fma(p, q2, 1.0 / n);
   return __builtin_fma((double)k, 0x1.62e42fefa39efp-1, 2.0 * q * p);
 }
 
+// What a token brings beside its logits; loaded with them, not when it is wanted.
+struct Token {
+  float weight, advantage, old_logp, ref_logp;
+};
+__device__ __forceinline__ Token token_of(const Loss& a, int64_t t) {
+  Token k = {1.0f, 0.0f, 0.0f, 0.0f};
+  if (!a.rows) return k;
+  if (a.weights) k.weight = a.weights[t];
+  k.advantage = a.advantages[t];
+  k.old_logp = a.old_logp[t];
+  if (a.ref_logp) k.ref_logp = a.ref_logp[t];
+  return k;
+}
+
 // The terms of a token, and the factor of its row of gradients.
-__device__ __forceinline__ double token_terms(const Loss& a, int64_t t, double logp, double* rows) {
-  const double w = a.weights ? (double)a.weights[t] : 1.0;
+__device__ __forceinline__ double token_terms(const Loss& a, const Token& k, double logp, double* rows) {
+  const double w = k.weight;
   if (w == 0.0) {
     rows[0] = rows[1] = rows[2] = rows[3] = 0.0;
     return 0.0;
   }
-  const double A = a.advantages[t], r = exp64(logp - (double)a.old_logp[t]);
+  const double A = k.advantage, r = exp64(logp - (double)k.old_logp);
   const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
   const bool clipped = (A > 0.0 && r > hi) || (A < 0.0 && r < lo);
   const double pg = -(clipped ? (A > 0.0 ? hi : lo) * A : r * A);
   double slope = clipped ? 0.0 : -r * A, kl = 0.0;
   if (a.ref_logp) {
-    const double u = (double)a.ref_logp[t] - logp, e = exp64(u);
+    const double u = (double)k.ref_logp - logp, e = exp64(u);
     kl = e - u - 1.0;
     if (a.kl != 0.0f) slope += (double)a.kl * (1.0 - e);
   }
@@ -191,7 +207,7 @@ __device__ __forceinline__ double token_terms(const Loss& a, int64_t t, double l
 
 // R threads a row, NV vectors each; NV = 0: rows of any length, read again
 template <int LT, int R, int NV>
-__global__ void __launch_bounds__(R, NV > 8 ? 4 : 8) k_loss(unsigned first, Loss a) {
+__global__ void __launch_bounds__(R, NV > 8 ? 4 : NV == 8 && R < 1024 ? 7 : 8) k_loss(unsigned first, Loss a) {
   constexpr int E = per_vec<LT>();
   __shared__ float top[R / 64];
   __shared__ double total[R / 64];
@@ -231,6 +247,7 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : 8) k_loss(unsigned first, Loss
     for (int k = 0; k < E; ++k) m = fmaxf(m, v[k]);
   };
   float za[1];
+  const Token token = token_of(a, t);  // not beside the id, which the row's loads wait for
   if constexpr (NV > 0) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) load_vec<LT>(row, (j * R + (int)threadIdx.x) * E, V, z[j]);
@@ -289,7 +306,7 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : 8) k_loss(unsigned first, Loss
   if (threadIdx.x < 64) {
     const double logp = (double)a.scale * ((double)za[0] - (double)m) - log64(sum);
     double rows[4];
-    const double g = a.rows ? token_terms(a, t, logp, rows) : 0.0;
+    const double g = a.rows ? token_terms(a, token, logp, rows) : 0.0;
     if (threadIdx.x == 0) {
       if (a.logp) a.logp[t] = (float)logp;
       if (a.rows) {
@@ -336,44 +353,34 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : 8) k_loss(unsigned first, Loss
   });
 }
 
-// the sums over the rows: each thread its rows in their order, then the threads
+// A sum over the rows a workgroup: each thread its rows in their order, 8 loads in flight,
+// then the threads in theirs.
 __global__ void __launch_bounds__(1024) k_loss_sums(const double* __restrict__ rows, int64_t T, float* __restrict__ sums) {
-  __shared__ double part[16][4];
-  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  __shared__ double part[16];
+  const int k = blockIdx.x;
+  double s = 0.0;
   int64_t t = threadIdx.x;
-  for (; t + 3 * 1024 < T; t += 4 * 1024) {  // 4 rows' loads in flight
-    double v[4][4];
+  for (; t + 7 * 1024 < T; t += 8 * 1024) {
+    double v[8];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < 8; ++u) v[u] = rows[4 * (t + 1024 * u) + k];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[u][k] = rows[4 * (t + 1024 * u) + k];
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s[k] += v[u][k];
-    }
+    for (int u = 0; u < 8; ++u) s += v[u];
   }
-  for (; t < T; t += 1024) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s[k] += rows[4 * t + k];
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    for (int o = 32; o; o >>= 1) s[k] += __shfl_xor(s[k], o);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][k] = s[k];
-  }
+  for (; t < T; t += 1024) s += rows[4 * t + k];
+  for (int o = 32; o; o >>= 1) s += __shfl_xor(s, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x >= 4) return;
+  if (threadIdx.x != 0) return;
   double v = 0.0;
-  for (int w = 0; w < 16; ++w) v += part[w][threadIdx.x];
-  sums[threadIdx.x] = (float)v;
+  for (int w = 0; w < 16; ++w) v += part[w];
+  sums[k] = (float)v;
 }
 
 // Threads of a row and their vectors, by the row's vectors of 16 bytes: the fewest
 // threads that hold them in 8 each (64 registers: 8 waves a SIMD), then 1,024 with more.
-// Rows of 50,000 of bf16: 306 us with 1,024 threads of 7 vectors, 313 with 512 of 13 and 315
-// with 256 of 25; of 16,411 of binary32 80, 84 and 87 with 1,024 of 5, 512 of 9, 256 of 17.
+// Against 1,024 threads of 7 vectors, rows of 50,000 of bf16 took 1% longer with 512 of 13 and
+// with 256 of 25; of 16,411 of binary32, against 1,024 of 5, 4% with 512 of 9, 7% with 256 of 17.
 template <int LT, int R, int NV>
 int rows_in(const Loss& a, hipStream_t st) {
   return launch_parts(&k_loss<LT, R, NV>, a.T, R, st, a);
@@ -480,7 +487,7 @@ int zq_policy_loss(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_
     const int rc2 = run(a, lt, st);
     if (rc2 != ZQ_OK) return rc2;
   }
-  return launch(&k_loss_sums, 1u, 1024u, st, static_cast<const double*>(workspace), T, sums);
+  return launch(&k_loss_sums, 4u, 1024u, st, static_cast<const double*>(workspace), T, sums);
 }
 
 }  // extern "C"

@@ -559,12 +559,12 @@ __global__ void __launch_bounds__(1024)
   if (d < D) {
     const int g0 = (int)((int64_t)groups * s / 16), g1 = (int)((int64_t)groups * (s + 1) / 16);
     int g = g0;
-    for (; g + 8 <= g1; g += 8) {
-      float t[8];
+    for (; g + 16 <= g1; g += 16) {
+      float t[16];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) t[k] = part[(int64_t)(g + k) * D + d];
+      for (int k = 0; k < 16; ++k) t[k] = part[(int64_t)(g + k) * D + d];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v += (double)t[k];
+      for (int k = 0; k < 16; ++k) v += (double)t[k];
     }
     for (; g < g1; ++g) v += (double)part[(int64_t)g * D + d];
   }
