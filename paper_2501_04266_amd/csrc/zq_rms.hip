@@ -177,6 +177,16 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes) {
   return v;
 }
 
+// 1 / sqrt(x) to the last bits of binary64: v_rsq_f64 (good to some 2^-26) and one step of
+// third order, y + y e (1/2 + 3/8 e) with e = 1 - x y^2, whose error is about e^3.  Every thread
+// of a row computes it: with a division and a square root in its place, 8,192 rows of 2,048
+// into INT8 (and dequantised) take 34.6 us and not 33.2.
+__device__ __forceinline__ double inverse_root(double x) {
+  if (!(x > 0.0 && x < (double)__builtin_inff())) return 1.0 / sqrt(x);
+  const double y = __builtin_amdgcn_rsq(x), e = __builtin_fma(-x * y, y, 1.0);
+  return __builtin_fma(y * e, __builtin_fma(0.375, e, 0.5), y);
+}
+
 // ---------------------------------------------------------------- forward
 
 struct Norm {
@@ -188,7 +198,7 @@ struct Norm {
   float* scales;
   float* rstd;
   int64_t T, D;
-  double eps;
+  double eps, share;  // share = 1 / D
   int8_t wt, yt, lgB;
 };
 
@@ -208,7 +218,9 @@ __device__ __forceinline__ void put_int8(const Norm& a, int64_t at, int i, const
   }
   const float m = u2f(t);
   const bool fits = m >= 0x1p-119f;
-  const float s = fits ? m / 127.0f : 0.0f, r = fits ? 127.0f / m : 0.0f;
+  // m / 127 is a binary32 number or further than 2^-32 of it from the middle of two: its product
+  // with 1 / 127 in binary64, rounded, is the rounded quotient
+  const float s = fits ? (float)((double)m * (1.0 / 127.0)) : 0.0f, r = fits ? 127.0f / m : 0.0f;
   if (i >= (int)a.D) return;
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
@@ -284,7 +296,7 @@ __device__ __forceinline__ void norm_row(const Norm& a, int64_t t, int lane, dou
   };
   auto finish = [&]() {
     sum = row_sum<R>(sum, slot);
-    const float rstd = (float)(1.0 / sqrt(sum / (double)a.D + a.eps));
+    const float rstd = (float)inverse_root(sum * a.share + a.eps);
     if (a.rstd && lane == 0) a.rstd[t] = rstd;
     if (has_last) store1(a.yt, y, last, weight ? (x1 * rstd) * w1 : x1 * rstd);
     return rstd;
@@ -638,7 +650,7 @@ int check_forward(const Norm& a, int xt, const void* weight, int wt, bool int8, 
 
 int rms_norm(const void* x, const void* residual, int xt, const void* weight, int wt, int64_t T, int64_t D, double eps,
              void* h, void* y, int yt, float* scales, int32_t block, float* rstd, void* stream, bool int8) {
-  const Norm a = {x, residual, weight, h, y, scales, rstd, T, D, eps, (int8_t)wt, (int8_t)(int8 ? kInt8 : yt),
+  const Norm a = {x, residual, weight, h, y, scales, rstd, T, D, eps, 1.0 / (double)(D > 0 ? D : 1), (int8_t)wt, (int8_t)(int8 ? kInt8 : yt),
                   (int8_t)(int8 ? log2_block(block) : 0)};
   const int rc = check_forward(a, xt, weight, wt, int8, yt, block);
   if (rc != ZQ_OK || T == 0) return rc;
