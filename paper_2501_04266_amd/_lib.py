@@ -158,14 +158,15 @@ def _output(stream, device, dtype, *shape):
     an object, the allocator keeps the tensor until that stream has passed the call.  (A
     raw handle may be gone by the time the tensor is freed: its owner keeps the tensor
     until the call has run.)"""
-    t = torch.empty(*shape, dtype=dtype, device=device)  # plain sizes: 0.6 us less than a tuple
+    # plain sizes: 0.6 us less than a tuple
+    t = torch.empty(*shape or (1,), dtype=dtype, device=device)
     if stream is not None and t.is_cuda:
         st, current = _stream_object(stream, device), torch.cuda.current_stream(device)
         if st.cuda_stream != current.cuda_stream:
             st.wait_stream(current)
             if st is stream:
                 t.record_stream(st)
-    return t
+    return t if shape else t.view(())
 
 
 def _dev(t, name):

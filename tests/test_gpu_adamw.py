@@ -343,3 +343,22 @@ def test_elements_beyond_2_32():
         assert np.array_equal(bits_of(keep[0].view(torch.uint8)[at:]), codes)
         assert np.array_equal(bits_of(keep[1][at // block:]), bits_of(torch.from_numpy(scales)))
     assert not bool(p[:first].any())
+
+
+def test_step_or_rate_alone_on_the_device():
+    count, rate = torch.full((1,), 4, dtype=torch.int64, device=DEV), torch.full((1,), 1e-3, device=DEV)
+    lr = float(rate)
+    for step_arg, lr_arg in ((4, lr), (count, lr), (4, rate), (count, rate)):
+        ts = [Tensor(np.random.default_rng(6), n, state=s) for n, s in ((3000, 32), (700, 8))]
+        before = [x.host() for x in ts]
+        zq.adamw_step(table_of(ts), step_arg, lr_arg, (STEP["b1"], STEP["b2"]), STEP["eps"])
+        check_step(ts, before, 4, lr=lr)
+
+
+def test_one_gradient_for_two_weights():
+    """A gradient is only read, so two weights may share it."""
+    a, b = (Tensor(np.random.default_rng(s), 5000, state=32) for s in (1, 2))
+    b.grad = a.grad
+    before = [a.host(), b.host()]
+    step([a, b], 2)
+    check_step([a, b], before, 2)

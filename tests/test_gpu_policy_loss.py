@@ -120,6 +120,7 @@ def test_types(dt, gt):
         sums, logp, grad = c.call(grad_dtype=DT[gt], grad_scale=1024.0)
         assert grad.dtype == DT[gt]
         c.check(sums, logp, grad, 1024.0)
+        assert torch.equal(zq.token_logp(c.logits, c.ids, c.scale), logp)
 
 
 @pytest.mark.parametrize("scale,kl,clip", [(0.5, 0.0, (0.2, 0.2)), (2.0, 0.3, (0.1, 0.28)), (1.0, 0.0, (1.0, 3.0)), (1.0, 0.01, (0.0, 0.0))])
@@ -286,3 +287,33 @@ def test_rows_beyond_2_32_elements():
     sums, logp, grad = zq.policy_loss(logits, ids, zeros, adv, clip=(1.0, 100.0), grad=logits)
     assert torch.equal(logp[-2:], want[1]) and torch.equal(grad[-2:], want[2])
     assert bool(((logp[:-2] + math.log(V)).abs() <= 2.0**-20).all())
+
+
+@pytest.mark.parametrize("V", [1000, 50001, 140001])
+def test_gradient_in_place_of_a_padded_head(V):
+    c = Case(5, V, "bf16", ld=V + 15)
+    sums, logp, grad = c.call()
+    s2, l2, g2 = c.call(grad=c.logits)
+    assert g2 is c.logits and torch.equal(g2, grad) and torch.equal(sums, s2) and torch.equal(logp, l2)
+    assert bool(c.base.view(5, V + 15)[:, V:].isnan().all())
+
+
+def test_shapes_of_rows():
+    """One row alone, and rows in more dimensions."""
+    c = Case(12, 70, kl=0.0)
+    sums, logp, grad = c.call()
+    s2, l2, g2 = zq.policy_loss(c.logits.view(3, 4, 70), c.ids.view(3, 4), c.old.view(3, 4), c.adv.view(3, 4), c.w.view(3, 4),
+                                clip=c.clip)
+    assert torch.equal(s2, sums) and torch.equal(l2.view(-1), logp) and torch.equal(g2.view(12, 70), grad)
+    one = zq.token_logp(c.logits[5], c.ids[5])
+    assert one.shape == () and float(one) == float(logp[5])
+
+
+def test_no_slope():
+    """A loss scale of 0, and clipped tokens without a KL term: gradients of zeros."""
+    c = Case(40, 300, kl=0.0)
+    assert not bool(c.call(grad_scale=0.0)[2].any())
+    c.old -= 5.0  # ratios far beyond the clip
+    c.adv.abs_()
+    sums, logp, grad = c.call()
+    assert not bool(grad.any()) and float(sums[3]) > 0

@@ -304,3 +304,33 @@ def test_rows_beyond_2_32_elements():
     sdx, sdw = zq.rms_norm_grad(small, x[-2:].clone(), w, small_r)
     assert torch.equal(dx[-2:], sdx) and not bool(dx[:-2].any())
     assert bool(((dw - sdw).abs() <= 2.0**-22 * sdw.abs() + 1e-30).all())
+
+
+@pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
+def test_weight_gradient_added_in_its_type(out):
+    T, D = 50, 520
+    h, dy, w = rand((T, D), torch.float32, 1), rand((T, D), torch.float32, 2), rand((D,), torch.float32, 3)
+    rstd = rstd_of(h)
+    held = rand((D,), DT[out], 4, 10.0)
+    start = held.double()
+    zq.rms_norm_grad(dy, h, w, rstd, dweight=held, accumulate=True)
+    (_, want), (_, off) = reference(dy, h, w, rstd, None)
+    assert bool(((held.double() - start - want).abs() <= off + 2 * U * (start + want).abs() + 1.01 * half_step(DT[out]) * (start + want).abs() + 1e-7).all())
+
+
+@pytest.mark.parametrize("D", [64, 1000, 6144, 20000])
+def test_x_as_its_own_residual(D):
+    x, w = rand((3, D), torch.bfloat16, 1), rand((D,), torch.float32, 2)
+    y, h, rstd = zq.rms_norm(x, w, x)
+    check_forward(x, x, w, 1e-6, y, h, rstd)
+    keep = x.clone()
+    y2, h2, _ = zq.rms_norm(keep, w, keep, hidden=keep)
+    assert torch.equal(h2, h) and torch.equal(y2, y)
+
+
+def test_one_row():
+    x, w = rand((700,), torch.float32, 1), rand((700,), torch.float32, 2)
+    y, h, rstd = zq.rms_norm(x, w)
+    want = x.double() * torch.rsqrt(x.double().square().mean() + 1e-6) * w.double()
+    assert y.shape == (700,) and h is x and rstd.shape == (1,)
+    assert bool(((y.double() - want).abs() <= 4.1 * U * want.abs()).all())
