@@ -165,6 +165,19 @@ def test_gradient_widths(D):
         check_grad(dy, h, w, rstd, dh, dx, dw, f"{dt} {gt} {T} x {D}")
 
 
+@pytest.mark.parametrize("D", [1, 7, 16, 125, 136, 250, 256, 499, 512])
+def test_gradient_narrow_rows(D):
+    """Several groups of rows a workgroup: the last with all of them, with one and without
+    one; the sums' memory behind its bytes stays as it was."""
+    for T in (3, 4, 5, 15, 16, 17, 4097, 20001):
+        h, dy, w = rand((T, D), torch.bfloat16, D, 1.0), rand((T, D), torch.bfloat16, D + 1, 0.01), rand((D,), torch.float32, 3, 1.0)
+        rstd, need = rstd_of(h), zq.rms_norm_grad_bytes(T, D)
+        ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+        dx, dw = zq.rms_norm_grad(dy, h, w, rstd, workspace=ws)
+        check_grad(dy, h, w, rstd, None, dx, dw, f"{T} x {D}")
+        assert bool((ws[need:] == 0xFF).all())
+
+
 @pytest.mark.parametrize("dt,gt", itertools.product(DT, DT))
 def test_gradient_types(dt, gt):
     for D in (328, 6000, 17000):
