@@ -463,8 +463,10 @@ int64_t zq_rms_norm_grad_bytes(int64_t T, int64_t D); /* -1 for sizes outside th
  * Log-probabilities of given tokens, and the clipped policy loss with a KL term and its
  * gradient, from rows of V logits.  Row t of logits starts at element t * ld (ld >= V:
  * heads padded to a wider row), T * ld at most 2^59.  A logit of -infinity names a token
- * that cannot occur: probability and gradient 0 (as the row's own token: logp -infinity and
- * a ratio of 0; a KL term is then infinite).  An id outside [0, V), or a row without any logit above
+ * that cannot occur: probability and gradient 0.  As the row's own token it has logp
+ * -infinity, a ratio of 0 and an infinite KL term, whatever old_logp and ref_logp hold; a
+ * loss with that term is infinite, and so is its gradient in the logits whose exponential
+ * is above 0 (at least 2^-126).  An id outside [0, V), or a row without any logit above
  * -infinity, names no token: logp 0, no loss, a gradient of zeros.
  *
  * zq_token_logp: logp[t] = scale * (z[a] - max z) - log(sum_v exp(scale * (z[v] - max z))),

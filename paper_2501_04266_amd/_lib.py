@@ -977,6 +977,8 @@ def policy_loss(logits, ids, old_logp, advantages, weights=None, ref_logp=None, 
     4) holds the sums over tokens, by weight, of the loss, its first term, the KL, and of
     the tokens whose ratio is clipped.
     ids as token_logp takes them (outside [0, V): no loss, a gradient of zeros);
+    a logit of -infinity masks its token: a gradient of 0; chosen all the same, a ratio of
+    0 and an infinite KL term;
     old_logp, advantages, weights (None: 1 each; 0: masked), ref_logp (needed for kl)
     float32, one a row; scale > 0 is 1 / temperature.
     grad: True (a tensor of logits' shape and of grad_dtype, logits' if not given), a

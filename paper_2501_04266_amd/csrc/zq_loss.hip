@@ -128,14 +128,18 @@ __device__ __forceinline__ float group_max(float v, float* slot) {
   return m;
 }
 template <int R>
-__device__ __forceinline__ double group_sum(double v, double* slot) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
-  __syncthreads();
+__device__ __forceinline__ double slots_sum(const double* slot) {
   double s = slot[0];
 #pragma unroll
   for (int w = 1; w < R / 64; ++w) s += slot[w];
   return s;
+}
+template <int R>
+__device__ __forceinline__ double group_sum(double v, double* slot) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return slots_sum<R>(slot);
 }
 
 // exp and log of a token's few binary64 numbers, by their series: they run while a row
@@ -188,14 +192,15 @@ __device__ __forceinline__ double token_terms(const Loss& a, const Token& k, dou
     rows[0] = rows[1] = rows[2] = rows[3] = 0.0;
     return 0.0;
   }
-  const double A = k.advantage, r = exp64(logp - (double)k.old_logp);
+  const bool never = logp == -(double)kInf;  // a token that cannot occur, whatever the other policies say of it
+  const double A = k.advantage, r = never ? 0.0 : exp64(logp - (double)k.old_logp);
   const double lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
   const bool clipped = (A > 0.0 && r > hi) || (A < 0.0 && r < lo);
   const double pg = -(clipped ? (A > 0.0 ? hi : lo) * A : r * A);
   double slope = clipped ? 0.0 : -r * A, kl = 0.0;
   if (a.ref_logp) {
-    const double u = (double)k.ref_logp - logp, e = exp64(u);
-    kl = e - u - 1.0;
+    const double u = never ? (double)kInf : (double)k.ref_logp - logp, e = exp64(u);
+    kl = e == (double)kInf ? e : e - u - 1.0;  // not infinity less infinity
     if (a.kl != 0.0f) slope += (double)a.kl * (1.0 - e);
   }
   rows[0] = w * (a.kl != 0.0f ? pg + (double)a.kl * kl : pg);
@@ -325,6 +330,19 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : NV == 8 && R < 1024 ? 7 : 8) k
   }
   int thread = threadIdx.x;
   asm volatile("" : "+v"(thread));  // places computed anew: those of the loads are not kept
+  if (fabsf(g) == kInf) {  // an infinite KL term, mostly: 0 where there is no probability, not 0 times infinity
+    const double f = factor, S = slots_sum<R>(total);  // sum, which is not kept in registers for this
+    for_type(a.gt, [&](auto gt) {
+      for (int i = thread; i < V; i += R) {
+        float v[1];
+        load_elems<LT, 1>(row, i, v);
+        const double p = (double)__builtin_amdgcn_exp2f((v[0] - m) * k2) / S;
+        const float t[1] = {v[0] == -kInf ? 0.0f : (float)(i == (int)id ? f * (1.0 - p) : p == 0.0 ? 0.0 : -f * p)};
+        store_elems<gt, 1>(grow, i, t);
+      }
+    });
+    return;
+  }
   for_type(a.gt, [&](auto gt) {
     auto put = [&](const uint32_t(&w)[4], int i) {
       float v[E];
