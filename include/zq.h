@@ -470,7 +470,9 @@ int64_t zq_rms_norm_grad_bytes(int64_t T, int64_t D); /* -1 for sizes outside th
  * -infinity, names no token: logp 0, no loss, a gradient of zeros.
  *
  * zq_token_logp: logp[t] = scale * (z[a] - max z) - log(sum_v exp(scale * (z[v] - max z))),
- * a = ids[t]; exponentials in binary32, the rest in binary64, rounded once.
+ * a = ids[t]; exponentials and sums of 8 neighbours (4 of binary32 logits) in binary32, the
+ * rest in binary64, rounded once.  Where a's probability is above a half the sum of its
+ * neighbours is binary64 as well: one next to 1 keeps what the others leave of it.
  *   logits of dtype lt, ids [T] of type it = ZQ_I32 or ZQ_I64 (read), logp [T] (written)
  *   scale > 0: 1 / temperature.  V from 1 to 2^24, T <= 2^30 (ZQ_E_SIZE). */
 int zq_token_logp(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_t ld, const void* ids, zq_dtype it,

@@ -9,7 +9,8 @@
 // (64 to 1,024 threads, up to 16 vectors of 16 bytes each), and its gradient written
 // once (8,192 rows of 50,000 of bf16: 285 us, 5.5 TB/s).  exp is v_exp_f32 of a binary32 difference; it is taken twice, for the sum and for
 // the gradient, since a row's exponentials in binary32 would need twice the registers of
-// 16-bit logits.  A thread's sum is binary32 (up to 128 terms), sums over threads and what
+// 16-bit logits.  Sums of a vector's 4 or 8 exponentials are binary32 (but for a likely token's
+// vector, whose others are what its logarithm is made of), sums over vectors and threads and what
 // follows binary64: whether a token is clipped is decided at 1 +- clip, and its logarithm
 // is what the binary32 terms allow.  Rows too long for the registers are read again.
 #include <hip/hip_runtime.h>
@@ -21,6 +22,7 @@
 #include "zq.h"
 #include "zq_device.h"
 #include "zq_host.h"
+#include "zq_lanes.h"
 #include "zq_vec.h"
 
 #pragma clang fp contract(off)
@@ -119,7 +121,8 @@ __device__ __forceinline__ void for_type(int dt, F f) {
 
 template <int R>
 __device__ __forceinline__ float group_max(float v, float* slot) {
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  v = over_lanes<64>(v, [](float a, float b) { return fmaxf(a, b); });
+  if constexpr (R == 64) return v;
   if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
   __syncthreads();
   float m = slot[0];
@@ -128,18 +131,15 @@ __device__ __forceinline__ float group_max(float v, float* slot) {
   return m;
 }
 template <int R>
-__device__ __forceinline__ double slots_sum(const double* slot) {
+__device__ __forceinline__ double group_sum(double v, double* slot) {
+  v = lanes_sum<64>(v);
+  if constexpr (R == 64) return v;
+  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
+  __syncthreads();
   double s = slot[0];
 #pragma unroll
   for (int w = 1; w < R / 64; ++w) s += slot[w];
   return s;
-}
-template <int R>
-__device__ __forceinline__ double group_sum(double v, double* slot) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return slots_sum<R>(slot);
 }
 
 // exp and log of a token's few binary64 numbers, by their series: they run while a row
@@ -251,19 +251,24 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : NV == 8 && R < 1024 ? 7 : 8) k
 #pragma unroll
     for (int k = 0; k < E; ++k) m = fmaxf(m, v[k]);
   };
-  float za[1];
+  const int beside = (int)id & -E;  // the vector that the token's logit is in
+  float own[1] = {-kInf};           // one of its elements
   const Token token = token_of(a, t);  // not beside the id, which the row's loads wait for
+  auto load_own = [&]() {
+    const int i = beside + (int)(threadIdx.x & (E - 1));
+    if (i < V) load_elems<LT, 1>(row + (uint32_t)i * dt_size<LT>(), 0, own);
+  };
   if constexpr (NV > 0) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) load_vec<LT>(row, (j * R + (int)threadIdx.x) * E, V, z[j]);
-    load_elems<LT, 1>(row, id, za);
+    load_own();
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       max_of(z[j]);
       forget(z[j]);
     }
   } else {
-    load_elems<LT, 1>(row, id, za);
+    load_own();
     for (int i = threadIdx.x * E; i < V; i += STEP) {
       load_vec<LT>(row, i, V, z[0]);
       max_of(z[0]);
@@ -284,32 +289,41 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : NV == 8 && R < 1024 ? 7 : 8) k
   }
 
   double sum = 0.0;
-  auto sum_of = [&](const uint32_t(&w)[4]) {
-    float v[E], s = 0.0f;
+  auto add = [&](const uint32_t(&w)[4]) {
+    float v[E];
     widen<LT>(w, v);
 #pragma unroll
-    for (int k = 0; k < E; ++k) s += __builtin_amdgcn_exp2f((v[k] - m) * k2);
-    return s;
+    for (int k = 0; k < E; ++k) v[k] = __builtin_amdgcn_exp2f((v[k] - m) * k2);
+#pragma unroll
+    for (int o = 1; o < E; o *= 2) {  // in the order of lanes_sum
+#pragma unroll
+      for (int k = 0; k < E; k += 2 * o) v[k] += v[k + o];
+    }
+    sum += (double)v[0];
   };
   if constexpr (NV > 0) {
-    float s = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      s += sum_of(z[j]);
+      add(z[j]);
       forget(z[j]);
     }
-    sum = (double)s;
   } else {
     for (int i = threadIdx.x * E; i < V; i += STEP) {
       load_vec<LT>(row, i, V, z[0]);
-      sum += (double)sum_of(z[0]);
+      add(z[0]);
     }
   }
   sum = group_sum<R>(sum, total);
 
   // one wave's work, the others wait for it if they have a gradient to write
   if (threadIdx.x < 64) {
-    const double logp = (double)a.scale * ((double)za[0] - (double)m) - log64(sum);
+    const float za = u2f((uint32_t)__builtin_amdgcn_readlane((int)f2u(own[0]), (int)id - beside));
+    double S = sum;
+    if (za == m && sum < 2.0) {  // a likely token: its exponential is 1, and those of its vector were lost beside it
+      const float e = __builtin_amdgcn_exp2f((own[0] - m) * k2);
+      S += lanes_sum<E>((double)e) - (double)lanes_sum<E>(e);  // the vector's sum again, for what it was
+    }
+    const double logp = (double)a.scale * ((double)za - (double)m) - log64(S);
     double rows[4];
     const double g = a.rows ? token_terms(a, token, logp, rows) : 0.0;
     if (threadIdx.x == 0) {
@@ -331,12 +345,12 @@ __global__ void __launch_bounds__(R, NV > 8 ? 4 : NV == 8 && R < 1024 ? 7 : 8) k
   int thread = threadIdx.x;
   asm volatile("" : "+v"(thread));  // places computed anew: those of the loads are not kept
   if (fabsf(g) == kInf) {  // an infinite KL term, mostly: 0 where there is no probability, not 0 times infinity
-    const double f = factor, S = slots_sum<R>(total);  // sum, which is not kept in registers for this
+    const double f = factor;
     for_type(a.gt, [&](auto gt) {
       for (int i = thread; i < V; i += R) {
         float v[1];
         load_elems<LT, 1>(row, i, v);
-        const double p = (double)__builtin_amdgcn_exp2f((v[0] - m) * k2) / S;
+        const double p = (double)__builtin_amdgcn_exp2f((v[0] - m) * k2) / sum;
         const float t[1] = {v[0] == -kInf ? 0.0f : (float)(i == (int)id ? f * (1.0 - p) : p == 0.0 ? 0.0 : -f * p)};
         store_elems<gt, 1>(grow, i, t);
       }

@@ -21,6 +21,7 @@
 #include "zq.h"
 #include "zq_device.h"
 #include "zq_host.h"
+#include "zq_lanes.h"
 #include "zq_vec.h"
 
 #pragma clang fp contract(off)
@@ -129,29 +130,6 @@ constexpr int kind_bytes(int dt) { return dt == ZQ_F32 ? 4 : 2; }
 
 // ---------------------------------------------------------------- sums over a row's threads
 
-template <int CTRL>
-__device__ __forceinline__ float from_lane(float v) {
-  return u2f((uint32_t)__builtin_amdgcn_update_dpp(0, (int)f2u(v), CTRL, 0xF, 0xF, false));
-}
-template <int CTRL>
-__device__ __forceinline__ double from_lane(double v) {
-  const uint64_t u = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-// the sum over R lanes, 16 to 64, in all of them: within rows of 16 lanes through the ALUs
-// (a shuffle through LDS takes ten times as long), each lane from its mirror image
-template <int R, typename F>
-__device__ __forceinline__ F lanes_sum(F v) {
-  v += from_lane<0xB1>(v);   // quad_perm 1,0,3,2
-  v += from_lane<0x4E>(v);   // quad_perm 2,3,0,1
-  v += from_lane<0x141>(v);  // row_half_mirror
-  v += from_lane<0x140>(v);  // row_mirror
-  if constexpr (R >= 32) v += __shfl_xor(v, 16);
-  if constexpr (R >= 64) v += __shfl_xor(v, 32);
-  return v;
-}
 // the sum over a row's R threads, in all of them; `slot`: R / 64 values of LDS, written
 // again only after a barrier
 template <int R, typename F>

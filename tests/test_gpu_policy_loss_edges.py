@@ -67,3 +67,28 @@ def test_a_gradient_beyond_its_type():
     assert float(grad[0, 0]) == -INF and float(grad[0, 2]) == INF and float(grad[0, 3]) == 0.0
     # the exponential (4 roundings of its exponent of 60, an ulp), logp's rounding
     assert abs(float(grad[0, 1]) - want) <= (4 * 61 + 8) * 2.0**-24 * want
+
+
+@pytest.mark.parametrize("V,dt", itertools.product([2, 3, 64, 1000, 2049, 5001, 8200, 16411, 24577, 33000, 50000, 65537, 98000,
+                                                    131072, 140001], DT))
+def test_near_certain_tokens(V, dt):
+    """A token whose probability is 1 but for what the others' exponentials add up to, each
+    below half a step of 1 in binary32: none of them is lost beside it."""
+    at = torch.tensor(sorted({0, 1, V // 3, V // 2, V - 2, V - 1}), device=DEV)
+    z = (torch.randn(len(at), V, generator=torch.Generator().manual_seed(V)) * 0.5 - 20.0).to(DEV)
+    z[torch.arange(len(at)), at] = 0.0
+    z = z.to(DT[dt])
+    d = z.double()
+    e = torch.exp(d)
+    e[torch.arange(len(at)), at] = 0.0
+    rest = e.sum(1)
+    want = -torch.log1p(rest)
+    # an exponential: its exponent's 4 roundings, the instruction's 2^-22 to be safe, 3 additions
+    # of 8 neighbours; sums in binary64 of up to 256 and a 1,024th of the row's terms, one after
+    # the other; the result's rounding
+    U = 2.0**-24
+    off = (e * (4 * U * d.abs() + 2.0**-22 + 3 * U)).sum(1) + (256 + V / 1024) * 2.0**-53 + U * want.abs()
+    logp = zq.token_logp(z, at)
+    assert bool(((logp.double() - want).abs() <= 1.01 * off).all()), f"{logp.tolist()} {want.tolist()}"
+    row = torch.zeros(len(at), device=DEV)
+    assert torch.equal(zq.policy_loss(z, at, row, row)[1], logp)
