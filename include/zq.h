@@ -474,7 +474,8 @@ int64_t zq_rms_norm_grad_bytes(int64_t T, int64_t D); /* -1 for sizes outside th
  * rest in binary64, rounded once.  Where a's probability is above a half the sum of its
  * neighbours is binary64 as well: one next to 1 keeps what the others leave of it.
  *   logits of dtype lt, ids [T] of type it = ZQ_I32 or ZQ_I64 (read), logp [T] (written)
- *   scale > 0: 1 / temperature.  V from 1 to 2^24, T <= 2^30 (ZQ_E_SIZE). */
+ *   scale: 1 / temperature, above 0 and up to 2^127.  V from 1 to 2^24, T <= 2^30
+ *   (ZQ_E_SIZE).  Logits whose difference is beyond binary32 count as infinitely far. */
 int zq_token_logp(const void* logits, zq_dtype lt, int64_t T, int64_t V, int64_t ld, const void* ids, zq_dtype it,
                   float scale, float* logp, void* stream);
 
@@ -487,7 +488,7 @@ typedef struct {
   const float* ref_logp;   /* of the reference policy; needed where kl != 0 */
   float clip_low, clip_high; /* >= 0; clip_low <= 1 */
   float kl;                /* factor of the KL term, >= 0; 0: none */
-  float scale;             /* of the logits, > 0: 1 / temperature */
+  float scale;             /* of the logits: 1 / temperature, above 0 and up to 2^127 */
   float grad_scale;        /* of the gradient: a loss scale, the gradient of the loss */
   int32_t reserved;
 } zq_policy;

@@ -945,8 +945,8 @@ def _token_ids(ids, T):
 def token_logp(logits, ids, scale=1.0, out=None, stream=None):
     """Log-probability of one token a row: log_softmax(scale * logits)[..., ids], float32 of
     ids' shape.  logits f32 / f16 / bf16 [..., V], contiguous or a padded head's
-    logits[:, :V]; ids int32 or int64, one a row; scale is 1 / temperature.  An id outside
-    [0, V) gives 0."""
+    logits[:, :V]; ids int32 or int64, one a row; scale, above 0 and up to 2^127, is 1 /
+    temperature.  An id outside [0, V) gives 0."""
     l_at, T, V, ld = _logits(logits, "logits", _ELEM)
     ids_at = _token_ids(ids, T)
     _here(logits=logits, ids=ids, out=out)
@@ -980,7 +980,7 @@ def policy_loss(logits, ids, old_logp, advantages, weights=None, ref_logp=None, 
     a logit of -infinity masks its token: a gradient of 0; chosen all the same, a ratio of
     0 and an infinite KL term;
     old_logp, advantages, weights (None: 1 each; 0: masked), ref_logp (needed for kl)
-    float32, one a row; scale > 0 is 1 / temperature.
+    float32, one a row; scale, above 0 and up to 2^127, is 1 / temperature.
     grad: True (a tensor of logits' shape and of grad_dtype, logits' if not given), a
     tensor to write to (of logits' shape; logits itself for in place), or False (None is
     returned); times grad_scale.  workspace: uint8, policy_loss_bytes(rows) or more;

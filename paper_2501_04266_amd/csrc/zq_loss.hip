@@ -32,6 +32,7 @@ namespace {
 
 constexpr int64_t kMaxVocab = 1 << 24;
 constexpr int64_t kMaxPlaces = (int64_t)1 << 59;  // T * ld: bytes of all rows within 63 bits
+constexpr float kMaxScale = 0x1p127f;  // times log2 e a binary32 number
 constexpr float kInf = __builtin_inff();
 
 struct Loss {
@@ -452,7 +453,7 @@ int64_t span(int64_t T, int64_t V, int64_t ld, int64_t e) { return T > 0 ? ((T -
 int check_logits(const void* logits, int lt, int64_t T, int64_t V, int64_t ld, const void* ids, int it, float scale) {
   if (!dtype_ok(lt) || (it != ZQ_I32 && it != ZQ_I64)) return ZQ_E_DTYPE;
   if (T < 0 || T > (1 << 30) || V < 1 || V > kMaxVocab || ld < V || (T > 0 && ld > kMaxPlaces / T)) return ZQ_E_SIZE;
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return ZQ_E_SIZE;
+  if (!(scale > 0.0f && scale <= kMaxScale)) return ZQ_E_SIZE;
   if (T == 0) return ZQ_OK;
   if (!logits || !ids) return ZQ_E_NULL;
   if (!aligned(logits, elem_bytes(lt)) || !aligned(ids, it == ZQ_I64 ? 8 : 4)) return ZQ_E_ALIGN;
