@@ -44,8 +44,12 @@ constexpr int64_t kUnits = 256;  // CUs of the chip
 // new memory each time: the norm 140 us with its stores past them, 137 with its loads too
 // (but 37 and 35 us on 8,192 x 2,048 into INT8), 147 with neither; its gradient 137 with
 // both, 148 with its loads alone, 153 with neither.  The gradient's do so only where rows are
-// whole cache lines: else two rows share a line (5,003 rows of 2,051 of fp16: loads past them
-// 39 us, through them 32, with stores past them 4% more).
+// whole lines of 128 bytes, or with 16-bit elements alone whole halves of one: else two rows
+// share a line (5,003 rows of 2,051 of fp16: loads past them 39 us, through them 32, with stores
+// past them 4% more).  Whole halves, past them and through them: of bf16 a million rows of 96
+// 132 and 144 us, 24,000 of 4,128 140 and 147; of binary32 95,000 rows of 528 194 and 161,
+// 24,000 of 2,064 193 and 171.  Where dx starts does not matter as much as that its rows are
+// written whole (16,384 x 6,144 of bf16 from any element 138 us, through the caches 153).
 constexpr bool kNormLoadsPast = false, kNormStoresPast = true;
 
 // the words of 8 elements from element i on; zeros from element n on, a multiple of 8
@@ -335,12 +339,12 @@ struct NormGrad {
   int64_t T, D;
   int groups;   // of rows: group g has the rows g, g + groups, ...
   int8_t gt, wt;
-  bool lines;   // rows of whole cache lines, from the first byte of one
+  bool lines;   // rows of whole cache lines (or halves), from the first byte of one
 };
 
 // The rows of group g.  A thread keeps its columns' weight and sums of dw; AHEAD: the next
 // row's h and dy are loaded before the present row's sum is taken.  LINES: rows are whole
-// cache lines.  Where a workgroup has several groups (R <= 64) it adds their sums of dw, in the
+// cache lines or halves of them.  Where a workgroup has several groups (R <= 64) it adds their sums of dw, in the
 // groups' order and in binary64, and writes one: with each group's own, 16,384 of them at
 // D <= 128, 65,536 rows of 16 took 76 us and not 17, of 128 84 and not 20, of 512 67 and not 53.
 template <int XT, int R, int NV, bool SAME, bool AHEAD, bool LINES>
@@ -755,10 +759,11 @@ int zq_rms_norm_grad(const void* dy, zq_dtype gt, const void* h, zq_dtype xt, co
   const Range rdw = {dw, dw ? D * elem_bytes(dwt) : 0}, ws = {need ? workspace : nullptr, need};
   if (any_overlap({rdx, rdw, ws}, {rdy, rh, rw, rr, rdh})) return ZQ_E_ALIAS;
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const int64_t line = xt == ZQ_F32 || gt == ZQ_F32 ? 128 : 64;
   const NormGrad a = {dy, h, weight, rstd, dh, dx, dw ? static_cast<float*>(workspace) : nullptr, T, D,
                       (int)groups_for(T, D), (int8_t)gt, (int8_t)wt,
-                      D * e % 64 == 0 && D * elem_bytes(gt) % 64 == 0 && aligned(h, 64) && aligned(dy, 64) &&
-                          aligned(dh, 64)};
+                      D * e % line == 0 && D * elem_bytes(gt) % line == 0 && aligned(h, line) && aligned(dy, line) &&
+                          aligned(dh, line)};
   if (T > 0) {
     const int rc = xt == ZQ_F32 ? backward<ZQ_F32>(a, st) : xt == ZQ_F16 ? backward<ZQ_F16>(a, st) : backward<ZQ_BF16>(a, st);
     if (rc != ZQ_OK) return rc;
