@@ -6,9 +6,10 @@
 //   grad[v] = w scale (dloss/dlogp) ((v == a) - exp(scale (z[v] - m)) / S)
 //
 // Bound by memory: a row of logits is read once, kept in the registers of one workgroup
-// (64 to 1,024 threads, up to 16 vectors of 16 bytes each), and its gradient written
-// once (8,192 rows of 50,000 of bf16: 285 us, 5.5 TB/s).  exp is v_exp_f32 of a binary32 difference; it is taken twice, for the sum and for
-// the gradient, since a row's exponentials in binary32 would need twice the registers of
+// (64 to 1,024 threads, up to 16 vectors of 16 bytes each), and its gradient written once
+// (8,192 rows of 50,000 of bf16, a tenth of them without a token: 282 us, 5.5 TB/s).  exp is
+// v_exp_f32 of a binary32 difference; it is taken twice, for the sum and for the gradient,
+// since a row's exponentials in binary32 would need twice the registers of
 // 16-bit logits.  Sums of a vector's 4 or 8 exponentials are binary32 (but for a likely token's
 // vector, whose others are what its logarithm is made of), sums over vectors and threads and what
 // follows binary64: whether a token is clipped is decided at 1 +- clip, and its logarithm
@@ -411,7 +412,14 @@ __global__ void __launch_bounds__(1024) k_loss_sums(const double* __restrict__ r
 }
 
 // Threads of a row and their vectors, by the row's vectors of 16 bytes: the fewest
-// threads that hold them in 8 each (64 registers: 8 waves a SIMD), then 1,024 with more.
+// threads that hold them in 8 each, then 1,024 with more.  Up to 7 vectors fit the 64
+// registers of 8 waves a SIMD; 8 vectors take 7 waves, or with 1,024 threads 8 words of
+// scratch a thread.  Against the next more threads, loss with its gradient and log-probabilities
+// alone (us): 100,000 rows of 1,000 of bf16 112 and 42 with 64 threads, 212 and 104 with 256;
+// 32,768 of 2,500 66 and 31, 95 and 51; of 4,096 97 and 42, 110 and 52; 16,384 of 10,000 124
+// and 57 with 256, 129 and 74 with 512, of 16,384 202 and 89, 185 and 88; 8,192 of 20,000 120
+// and 55 with 512, 138 and 80 with 1,024, of 32,768 220 and 92, 195 and 96 (rows that fill 8
+// vectors would be better with more threads if they are written, not if they are only read).
 // Against 1,024 threads of 7 vectors, rows of 50,000 of bf16 took 1% longer with 512 of 13 and
 // with 256 of 25; of 16,411 of binary32, against 1,024 of 5, 4% with 512 of 9, 7% with 256 of 17.
 template <int LT, int R, int NV>
@@ -424,6 +432,8 @@ int rows_of(const Loss& a, hipStream_t st) {
   const auto per = [&](int64_t threads) { return (vecs + threads - 1) / threads; };
   if (per(64) <= 2) return rows_in<LT, 64, 2>(a, st);
   if (per(64) <= 4) return rows_in<LT, 64, 4>(a, st);
+  if (per(64) <= 6) return rows_in<LT, 64, 6>(a, st);
+  if (per(64) <= 8) return rows_in<LT, 64, 8>(a, st);
   if (per(256) <= 2) return rows_in<LT, 256, 2>(a, st);
   if (per(256) <= 3) return rows_in<LT, 256, 3>(a, st);
   if (per(256) <= 4) return rows_in<LT, 256, 4>(a, st);

@@ -92,3 +92,13 @@ def test_near_certain_tokens(V, dt):
     assert bool(((logp.double() - want).abs() <= 1.01 * off).all()), f"{logp.tolist()} {want.tolist()}"
     row = torch.zeros(len(at), device=DEV)
     assert torch.equal(zq.policy_loss(z, at, row, row)[1], logp)
+
+
+@pytest.mark.parametrize("V", [1023, 1025, 1400, 1537, 2048, 2500, 3073, 4095, 4097])
+@pytest.mark.parametrize("dt", DT)
+def test_rows_of_one_wave(V, dt):
+    """Rows that one wave holds in up to 8 vectors a thread, and the next longer ones."""
+    c = Case(7, V, dt, seed=9, offset=1)
+    sums, logp, grad = c.call()
+    c.check(sums, logp, grad)
+    assert torch.equal(zq.token_logp(c.logits, c.ids, c.scale), logp)
