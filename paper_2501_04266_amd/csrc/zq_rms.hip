@@ -665,14 +665,22 @@ int rms_norm(const void* x, const void* residual, int xt, const void* weight, in
 // Threads of a row in the gradient's kernels; 256 with up to 4 vectors each, as far as that
 // goes, are better than more with fewer: 16,384 rows of 6,144 took 134 us with 256 threads of
 // 3 vectors, 155 with 768 of one, 165 with 384 of 2.
+// From 8,193 to 16,384 elements 1,024 threads hold a row only with words in scratch (49 a thread
+// of 16 bits, 88 of unlike types, 170 of binary32): 6,144 rows of 16,384 take 145 us of bf16 (1.2
+// of their floor), 3,072 of binary32 198 (1.6), of bf16 with a binary32 dy 112 (1.5).
 int row_threads(int64_t D) {
   for (int r : {16, 32, 64, 128, 192, 256})
     if (D <= 8 * r) return r;
   return D <= 8192 ? 256 : 1024;
 }
-// Rows are dealt to groups, whose sums of dw are joined: the same number of
-// groups on each CU, as many as its registers hold (16 waves of one vector a thread, 12 of
-// two, 8 of more), as far as the sums stay within 16 MB.
+// Rows are dealt to groups, whose sums of dw are joined: the same number of groups for each
+// CU, by D alone (the workspace's size knows no types) and as far as the sums stay within 16 MB:
+// 16 waves' up to 2,048 elements a row, 12 to 4,096, 8 beyond.  The registers of a CU hold as
+// many at once of 16-bit rows with dy of their type up to 6,144 elements.  Of others they hold one
+// group fewer (binary32 and unlike types from 2,049 to 4,096, binary32 rows of 1,537 to 2,048
+// with dy of another type) or one of two (16-bit rows from 6,145 to 8,192; binary32 and unlike
+// types from 4,097, in 512 threads), and the rest run after them: 24,576 rows of 4,096 of
+// binary32 take 306 us, 1.25 of their floor.
 int64_t groups_for(int64_t T, int64_t D) {
   const int waves = D <= 2048 ? 16 : D <= 4096 ? 12 : 8;
   const int64_t g = kUnits * std::max(1, waves * 64 / row_threads(D));
